@@ -236,6 +236,102 @@ cusa_status cusa_decode_step(const cusa_params* params, int32_t n_layers, const 
                              void* const* out_layers, int32_t* idx, int32_t* cnt,
                              void* ws, size_t ws_bytes, void* stream);
 
+/* ---- decoding with trees of drafted tokens ---------------------------------------------------
+ * A speculative step: every sequence gets a small tree of drafted tokens behind its cached ones, one pass through the model
+ * checks them all, and the branch that the model agrees with stays.  Per step:
+ *   cusa_kv_plan      room for the drafted tokens: pages, lengths, the slots of the new rows
+ *   cusa_tree_masks   which nodes a node attends to, and the nodes' positions
+ *   per layer: cusa_kv_append (the nodes' K and V rows into their slots), cusa_tree_attn
+ *   cusa_kv_commit    the accepted branch's rows moved together; the next plan gives the rest back
+ * Rows of several sequences are packed: sequence b owns rows tok_start[b] .. tok_start[b+1]-1 of q, out, masks, slots and
+ * of the new K and V rows.  Lengths, counts, tables and masks are device memory and are read when the kernels run, so that a
+ * captured graph serves every step; the host knows bounds only.  Values out of range there (a table entry that names no
+ * page of the pool, a list entry outside the prefix, counts beyond the bounds) are left out or cut to the bounds; they
+ * never make a kernel read or write out of range. */
+
+/* A sequence's room in the cache.  Paged: pages come from, and go back to, a queue of free pages, `ring`: n_pages entries, of
+ * which state[1] are free pages, from entry state[0] on (mod n_pages).  */
+typedef struct {
+    int32_t        layout;          /* cusa_kv_layout                                                      */
+    int32_t        batch;
+    int32_t        capacity;        /* contiguous: positions of a sequence; unused when paged (16 * max_pages) */
+    int32_t*       block_table;     /* paged: device [batch][max_pages], changed                           */
+    int32_t        max_pages;
+    int32_t        page_size;       /* 16 */
+    int64_t        n_pages;         /* < 2^31 */
+    int32_t*       ring;            /* paged: device [n_pages], changed                                    */
+    const int32_t* state;           /* paged: device [2]: first free entry, number of free pages           */
+    int32_t*       state_out;       /* paged: device [2]: the same after the call; may be `state`          */
+} cusa_pool;
+
+/* Block tables and slot map from the sequences' lengths.  Sequence b holds pages for held[b] tokens, of which the first keep[b]
+ * stay, and asks for add[b] more (held is cut to [0, cap], keep to [0, held], add to >= 0; cap = 16 * max_pages or capacity).
+ * In order of b:
+ *   it fits           if keep + add <= cap and the add of all that do, up to and including b, come to max_tokens at most
+ *   it is granted     if it fits and needs no new page, or the new pages of all that fit, up to and including b, are free
+ *   lens[b]           keep + add if granted, else keep (and none of its add is in the outputs)
+ *   tok_start[b]      sum of granted add before b; tok_start[batch] the total
+ *   table entries     from ceil(held/16) to ceil(lens/16): pages from the front of the queue, in order of b and position;
+ *                     from ceil(lens/16) to ceil(held/16): pages that go to its end (the entries stay as they are)
+ *   slots[tok_start[b] + j]   where token keep + j of b goes: paged page * 16 + position % 16 (-1 for a table entry that names
+ *                     no page), contiguous b * 2^32 + position; -1 behind the last
+ * Pages given back by a call are not handed out by it.  held, keep, add, lens: device int32 [batch] (lens may be held or keep);
+ * tok_start: device int32 [batch + 1]; slots: device int64 [max_tokens].  One kernel, or two for max_tokens above 4096.
+ * ws: cusa_kv_plan_workspace_bytes(batch) bytes, 256-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL, LAUNCH. */
+size_t      cusa_kv_plan_workspace_bytes(int32_t batch);
+cusa_status cusa_kv_plan(const cusa_pool* pool, const int32_t* held, const int32_t* keep, const int32_t* add, int32_t max_tokens,
+                         int32_t* lens, int32_t* tok_start, int64_t* slots, void* ws, size_t ws_bytes, void* stream);
+
+typedef enum { CUSA_BF16 = 0, CUSA_F16 = 1, CUSA_F32 = 2 } cusa_dtype;
+
+/* New rows, host memory: element (r, kv, i) of K is k[r * stride_token + kv * stride_head + i], V the same. */
+typedef struct {
+    const void* k;
+    const void* v;
+    int32_t     dtype;              /* cusa_dtype; rounded to bf16 (nearest, ties to even) on the way */
+    int32_t     n;                  /* rows                                                           */
+    int64_t     stride_token, stride_head;   /* in elements; rows are 16-byte aligned                 */
+} cusa_rows;
+
+/* Row r goes to slots[r] (as cusa_kv_plan makes them) of one layer's cache, all KV heads; slots outside the pool, or at positions
+ * from max_seq_len on, are left out.  Two rows with the same slot leave either.  kv's seq_lens and block_table are not read. */
+cusa_status cusa_kv_append(const cusa_params* params, const cusa_kv* kv, const int64_t* slots, const cusa_rows* rows, void* stream);
+
+/* A batch of trees, host memory. */
+typedef struct {
+    const int32_t*  tok_start;      /* device [batch + 1]; rows per sequence at most max_nodes                */
+    const uint64_t* masks;          /* device [max_tokens][ceil(max_nodes / 64)]: bit i of row r: this node attends to node i of
+                                     * its sequence.  Any bits: a node need not attend to itself                */
+    int32_t         max_tokens;     /* rows of the packed arrays                                              */
+    int32_t         max_nodes;      /* 1 .. 256                                                               */
+    int64_t         q_stride;       /* elements between two rows of q, a multiple of 8 and >= n_q_heads * 128  */
+} cusa_tree;
+
+/* Masks and positions of trees given by parents: node j attends to itself and its ancestors, parents[r] is the parent's number in its tree
+ * if that is in [0, j), anything else (-1) hangs j on the cached prefix; positions[r] = base[b] + depth, 0 for the latter.
+ * base: device int32 [batch], tokens in front of the tree.  masks [max_tokens][ceil(max_nodes / 64)] and positions
+ * [max_tokens] (NULL: not wanted) are written for the rows of sequences.  batch <= 65535. */
+cusa_status cusa_tree_masks(int32_t batch, const int32_t* base, const int32_t* tok_start, const int32_t* parents, int32_t max_tokens,
+                            int32_t max_nodes, uint64_t* masks, int32_t* positions, void* stream);
+
+/* Attention of the trees' nodes: node j of sequence b, L = seq_lens[b] tokens in the cache with its n nodes as the last ones
+ * (cusa_kv_append comes first), P = L - n:  Eq. 1 restricted to the positions t < P and to P + i for the bits i of its mask.
+ * idx, cnt (both or neither): of the prefix only idx[b][0 .. cnt[b]) (as cusa_select makes them for the tree's first node: entries
+ * from P on, which the masks speak for, are left out); idx device int32 [batch][budget], cnt[b] in [0, budget].
+ * A node that attends to nothing gives zeros.  NaN and infinities in rows that a node does not attend to do not reach its output.
+ * q: device bf16, row r head h at q + r * q_stride + h * 128; out: device bf16 [max_tokens][n_q_heads][128]; rows of no
+ * sequence are not written.  ws: cusa_tree_workspace_bytes, 256-byte aligned, content not preserved.
+ * Errors as cusa_full_attn, and UNSUPPORTED for max_nodes > 256 and for pools of 2^31 or more rows. */
+cusa_status cusa_tree_workspace_bytes(const cusa_params* params, int32_t max_seq_len, int32_t max_tokens, int32_t max_nodes, size_t* bytes);
+cusa_status cusa_tree_attn(const cusa_params* params, const void* q, const cusa_kv* kv, const cusa_tree* tree, const int32_t* idx,
+                           const int32_t* cnt, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/* The accepted branches' rows moved together, in all layers: position base[b] + path[b][i] -> base[b] + i for i < n_path[b], K and V,
+ * all KV heads; path[b] ascending, and positions at or beyond max_seq_len are left out.  keep[b] = base[b] + n_path[b] (NULL: not
+ * wanted; may be base), what the next cusa_kv_plan keeps.  path: device int32 [batch][max_path]; base, n_path, keep: device int32 [batch]. */
+cusa_status cusa_kv_commit(const cusa_params* params, int32_t n_layers, const cusa_kv* kv_layers, const int32_t* base,
+                           const int32_t* path, int32_t max_path, const int32_t* n_path, int32_t* keep, void* stream);
+
 const char* cusa_strerror(cusa_status status);
 
 /* Digest of the sources this binary was compiled from (16 hex digits); a loader compares it

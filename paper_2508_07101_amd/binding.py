@@ -26,6 +26,8 @@ EXPORTS = [
     "cusa_full_attn", "cusa_decode_step", "cusa_strerror", "cusa_profile_num_kernels",
     "cusa_profile_kernel_name", "cusa_profile_enable", "cusa_profile_reset", "cusa_profile_read",
     "cusa_build_id", "cusa_probe_stream_read", "cusa_probe_traffic", "cusa_sparse_attn_noalloc", "cusa_noalloc_max_scratch_bytes",
+    "cusa_kv_plan_workspace_bytes", "cusa_kv_plan", "cusa_kv_append", "cusa_tree_masks", "cusa_tree_workspace_bytes", "cusa_tree_attn",
+    "cusa_kv_commit",
 ]
 
 
@@ -48,6 +50,22 @@ class CusaWsLayout(ctypes.Structure):
     _fields_ = [("scores_offset", ctypes.c_size_t), ("ld_scores", ctypes.c_int64),
                 ("rho_head_offset", ctypes.c_size_t), ("k", ctypes.c_int32), ("total_bytes", ctypes.c_size_t),
                 ("filtered_select", ctypes.c_int32), ("second_chance_offset", ctypes.c_size_t)]
+
+
+class CusaPool(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("batch", ctypes.c_int32), ("capacity", ctypes.c_int32), ("block_table", ctypes.c_void_p),
+                ("max_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int64), ("ring", ctypes.c_void_p),
+                ("state", ctypes.c_void_p), ("state_out", ctypes.c_void_p)]
+
+
+class CusaRows(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("n", ctypes.c_int32),
+                ("stride_token", ctypes.c_int64), ("stride_head", ctypes.c_int64)]
+
+
+class CusaTree(ctypes.Structure):
+    _fields_ = [("tok_start", ctypes.c_void_p), ("masks", ctypes.c_void_p), ("max_tokens", ctypes.c_int32), ("max_nodes", ctypes.c_int32),
+                ("q_stride", ctypes.c_int64)]
 
 
 class CusaError(RuntimeError):
@@ -120,6 +138,16 @@ def load():
     lib.cusa_sparse_attn_noalloc.restype = ctypes.c_int
     lib.cusa_noalloc_max_scratch_bytes.argtypes = []
     lib.cusa_noalloc_max_scratch_bytes.restype = sz
+    lib.cusa_kv_plan_workspace_bytes.argtypes = [i32]
+    lib.cusa_kv_plan_workspace_bytes.restype = sz
+    lib.cusa_kv_plan.argtypes = [P(CusaPool), vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+    lib.cusa_kv_append.argtypes = [P(CusaParams), P(CusaKv), vp, P(CusaRows), vp]
+    lib.cusa_tree_masks.argtypes = [i32, vp, vp, vp, i32, i32, vp, vp, vp]
+    lib.cusa_tree_workspace_bytes.argtypes = [P(CusaParams), i32, i32, i32, P(sz)]
+    lib.cusa_tree_attn.argtypes = [P(CusaParams), vp, P(CusaKv), P(CusaTree), vp, vp, vp, vp, sz, vp]
+    lib.cusa_kv_commit.argtypes = [P(CusaParams), i32, P(CusaKv), vp, vp, i32, vp, vp, vp]
+    for name in ("cusa_kv_plan", "cusa_kv_append", "cusa_tree_masks", "cusa_tree_workspace_bytes", "cusa_tree_attn", "cusa_kv_commit"):
+        getattr(lib, name).restype = ctypes.c_int
     lib.cusa_probe_stream_read.argtypes = [vp, sz, vp, vp]
     lib.cusa_probe_stream_read.restype = ctypes.c_int
     lib.cusa_probe_traffic.argtypes = [i32, vp, sz, vp, sz, vp]
@@ -288,6 +316,153 @@ class DecodeStep:
 
 def decode_step(params, layer_kind, q_layers, kv_layers, out_layers, idx, cnt, ws):
     DecodeStep(params, layer_kind, q_layers, kv_layers, out_layers, idx, cnt, ws).run()
+
+
+# ---- decoding with trees of drafted tokens -------------------------------------
+
+DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+@dataclass
+class PagePool:
+    """A paged cache's bookkeeping on the device: who holds which pages, and the queue of those that are free."""
+    block_table: torch.Tensor   # int32 [B, max_pages]
+    ring: torch.Tensor          # int32 [n_pages]
+    state: torch.Tensor         # int32 [2]: first free entry of the ring, number of free pages
+
+    @staticmethod
+    def empty(batch: int, max_pages: int, n_pages: int, device="cuda") -> "PagePool":
+        """A pool whose pages are all free."""
+        return PagePool(torch.full((batch, max_pages), -1, dtype=torch.int32, device=device),
+                        torch.arange(n_pages, dtype=torch.int32, device=device),
+                        torch.tensor([0, n_pages], dtype=torch.int32, device=device))
+
+    def desc(self, state_out: Optional[torch.Tensor] = None) -> CusaPool:
+        assert self.block_table.is_contiguous() and self.ring.is_contiguous()
+        b, max_pages = self.block_table.shape
+        return CusaPool(KV_PAGED, b, 0, self.block_table.data_ptr(), max_pages, 16, self.ring.numel(), self.ring.data_ptr(),
+                        self.state.data_ptr(), (self.state if state_out is None else state_out).data_ptr())
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _need_int(what: str, n: int, dtype, **tensors):
+    for name, t in tensors.items():
+        _need(t.dtype == dtype and t.is_contiguous() and t.numel() >= n, f"{what}: {name} holds {n} {dtype}, contiguous")
+
+
+def kv_plan_workspace_bytes(batch: int) -> int:
+    return int(load().cusa_kv_plan_workspace_bytes(batch))
+
+
+def alloc_plan_workspace(batch: int, device="cuda") -> torch.Tensor:
+    return torch.empty(kv_plan_workspace_bytes(batch), dtype=torch.uint8, device=device)
+
+
+def kv_plan(held, keep, add, lens, tok_start, slots, ws, pool: Optional[PagePool] = None, state_out=None, capacity: int = 0):
+    """Room for add[b] tokens behind the keep[b] first of the held[b] that sequence b has: block tables (pool, or a contiguous cache of
+    `capacity` positions a sequence), lens, tok_start and the slots of the new rows (int64, its length bounds the batch's tokens).
+    state_out: where the queue's state goes instead of back into the pool, to ask without taking."""
+    n = held.numel()
+    _need_int("kv_plan", n, torch.int32, held=held, keep=keep, add=add, lens=lens)
+    _need_int("kv_plan", n + 1, torch.int32, tok_start=tok_start)
+    _need_int("kv_plan", 0, torch.int64, slots=slots)
+    if pool is None:
+        d = CusaPool(KV_CONTIGUOUS, n, capacity, None, 0, 0, 0, None, None, None)
+    else:
+        _need(pool.block_table.shape[0] == n, "kv_plan: a row of the block table for each sequence")
+        d = pool.desc(state_out)
+    _check(load().cusa_kv_plan(ctypes.byref(d), _ptr(held), _ptr(keep), _ptr(add), slots.numel(), _ptr(lens), _ptr(tok_start),
+                               _ptr(slots), _ptr(ws), ws.numel(), _stream()), "cusa_kv_plan")
+
+
+def kv_append(params: CusaParams, kv: KvCache, slots, k_new, v_new):
+    """Rows k_new, v_new [n, G, 128] (bf16, fp16 or fp32; views with equal strides, as of a fused projection) to their slots in one layer's cache."""
+    n, heads, d = k_new.shape
+    _need(k_new.dtype in DTYPES and v_new.dtype == k_new.dtype and v_new.shape == k_new.shape and d == params.head_dim and
+          heads == params.n_kv_heads, "kv_append: new rows are [n, n_kv_heads, 128] in bf16, fp16 or fp32")
+    _need(k_new.stride(2) == 1 and k_new.stride() == v_new.stride(), "kv_append: K and V rows have the same strides, elements side by side")
+    _need_int("kv_append", n, torch.int64, slots=slots)
+    c = kv.desc()
+    r = CusaRows(_ptr(k_new), _ptr(v_new), DTYPES[k_new.dtype], n, k_new.stride(0), k_new.stride(1))
+    _check(load().cusa_kv_append(ctypes.byref(params), ctypes.byref(c), _ptr(slots), ctypes.byref(r), _stream()), "cusa_kv_append")
+
+
+def mask_words(max_nodes: int) -> int:
+    """64-bit words of a node's mask."""
+    return (max_nodes + 63) // 64
+
+
+def tree_masks(base, tok_start, parents, masks, positions, max_nodes: int):
+    """masks (int64 [tokens, mask_words], bit patterns) and positions (int32, or None) of trees given by their nodes' parents."""
+    n = parents.numel()
+    _need_int("tree_masks", tok_start.numel() - 1, torch.int32, base=base)
+    _need_int("tree_masks", 2, torch.int32, tok_start=tok_start)
+    _need_int("tree_masks", n, torch.int32, parents=parents, **({} if positions is None else {"positions": positions}))
+    _need_int("tree_masks", n * mask_words(max_nodes), torch.int64, masks=masks)
+    _check(load().cusa_tree_masks(tok_start.numel() - 1, _ptr(base), _ptr(tok_start), _ptr(parents), n, max_nodes, _ptr(masks),
+                                  _ptr(positions), _stream()), "cusa_tree_masks")
+
+
+@dataclass
+class Tree:
+    """The drafted trees of a step, the same for all layers."""
+    tok_start: torch.Tensor     # int32 [B + 1]
+    masks: torch.Tensor         # int64 [tokens, mask_words(max_nodes)]
+    max_nodes: int
+
+
+def tree_workspace_bytes(params: CusaParams, max_seq_len: int, max_tokens: int, max_nodes: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().cusa_tree_workspace_bytes(ctypes.byref(params), max_seq_len, max_tokens, max_nodes, ctypes.byref(n)), "cusa_tree_workspace_bytes")
+    return int(n.value)
+
+
+def alloc_tree_workspace(params: CusaParams, max_seq_len: int, max_tokens: int, max_nodes: int, device="cuda") -> torch.Tensor:
+    return torch.empty(tree_workspace_bytes(params, max_seq_len, max_tokens, max_nodes), dtype=torch.uint8, device=device)
+
+
+def tree_attn(params: CusaParams, q, kv: KvCache, tree: Tree, out, ws, idx=None, cnt=None):
+    """Attention of the trees' nodes, q [tokens, H, 128] (a view of a fused projection's rows, or contiguous), over the whole prefix or
+    over idx/cnt of it, and over the nodes that the masks name."""
+    n, heads, d = q.shape
+    _need(q.dtype == torch.bfloat16 and heads == params.n_q_heads and d == params.head_dim and q.stride(2) == 1 and q.stride(1) == d,
+          "tree_attn: q is bf16 [tokens, n_q_heads, 128], heads side by side")
+    _need(out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() >= n * heads * d, "tree_attn: out is bf16 [tokens, n_q_heads, 128], contiguous")
+    _need_int("tree_attn", params.batch + 1, torch.int32, tok_start=tree.tok_start)
+    _need_int("tree_attn", n * mask_words(tree.max_nodes), torch.int64, masks=tree.masks)
+    if idx is not None:
+        _need_int("tree_attn", params.batch * params.budget, torch.int32, idx=idx)
+        _need(cnt is not None, "tree_attn: idx comes with cnt")
+        _need_int("tree_attn", params.batch, torch.int32, cnt=cnt)
+    c = kv.desc()
+    t = CusaTree(_ptr(tree.tok_start), _ptr(tree.masks), n, tree.max_nodes, q.stride(0))
+    _check(load().cusa_tree_attn(ctypes.byref(params), _ptr(q), ctypes.byref(c), ctypes.byref(t), _ptr(idx), _ptr(cnt), _ptr(out), _ptr(ws),
+                                 ws.numel(), _stream()), "cusa_tree_attn")
+
+
+class KvCommit:
+    """Marshals the layers' caches once; run() moves the accepted branches' rows together in all of them."""
+
+    def __init__(self, params: CusaParams, kv_layers: Sequence[KvCache]):
+        self.params, self.n = params, len(kv_layers)
+        self._keep = list(kv_layers)
+        self.kvs = (CusaKv * self.n)(*[kv.desc() for kv in kv_layers])
+
+    def run(self, base, path, n_path, keep=None):
+        """Positions base[b] + path[b][i] -> base[b] + i for i < n_path[b]; keep (not base): base + n_path."""
+        b = self.params.batch
+        _need(path.dim() == 2 and path.shape[0] == b, "kv_commit: path is [batch, nodes]")
+        _need_int("kv_commit", b, torch.int32, base=base, path=path, n_path=n_path, **({} if keep is None else {"keep": keep}))
+        _check(load().cusa_kv_commit(ctypes.byref(self.params), self.n, self.kvs, _ptr(base), _ptr(path), path.shape[1], _ptr(n_path),
+                                     _ptr(keep), _stream()), "cusa_kv_commit")
+
+
+def kv_commit(params, kv_layers, base, path, n_path, keep=None):
+    KvCommit(params, kv_layers).run(base, path, n_path, keep)
 
 
 def probe_stream_read(src: torch.Tensor, sink: torch.Tensor):

@@ -9,12 +9,13 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libcusa.so")
-SOURCES = [os.path.join(CSRC, "cusa.hip")]
-HEADERS = [os.path.join(CSRC, "attn_plan.hpp"), os.path.join(CSRC, "call_tag.hpp"), os.path.join(CSRC, "cusa_kernels.hpp"),
-           os.path.join(os.path.dirname(_HERE), "include", "cusa.h")]
+SOURCES = [os.path.join(CSRC, f) for f in ("cusa.hip", "tree.hip", "build_id.hip")]
+HEADERS = [os.path.join(CSRC, f) for f in ("attn_plan.hpp", "cache_view.hpp", "call_tag.hpp", "cusa_kernels.hpp", "host.hpp", "tree_kernels.hpp",
+                                           "tree_plan.hpp")]
+HEADERS.append(os.path.join(os.path.dirname(_HERE), "include", "cusa.h"))
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # packed-FP32 forms are kept out of the generated code
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     # the leading kernel arguments arrive in SGPRs with the wave instead of through a first load
@@ -42,13 +43,23 @@ def source_id() -> str:
 
 
 def build_lib(force: bool = True, extra_flags=()) -> str:
-    """Compile the library; with force=False only when it is missing."""
+    """Compile the library, its sources side by side; with force=False only when it is missing."""
     if not force and os.path.exists(LIB):
         return LIB
     tmp = LIB + f".tmp{os.getpid()}"
-    cmd = [hipcc(), *HIPCC_FLAGS, f'-DCUSA_BUILD_ID="{source_id()}"', *extra_flags, "-o", tmp, *SOURCES]
-    subprocess.check_call(cmd)
-    os.replace(tmp, LIB)
+    objects = [f"{tmp}.{i}.o" for i in range(len(SOURCES))]
+    flags = [*HIPCC_FLAGS, f'-DCUSA_BUILD_ID="{source_id()}"', *extra_flags]
+    try:
+        jobs = [subprocess.Popen([hipcc(), *flags, "-c", "-o", obj, src]) for src, obj in zip(SOURCES, objects)]
+        for src, status in [(src, job.wait()) for src, job in zip(SOURCES, jobs)]:
+            if status:
+                raise subprocess.CalledProcessError(status, f"hipcc -c {src}")
+        subprocess.check_call([hipcc(), "--offload-arch=gfx950", "-shared", *extra_flags, "-o", tmp, *objects])
+        os.replace(tmp, LIB)
+    finally:
+        for f in objects + [tmp]:
+            if os.path.exists(f):
+                os.remove(f)
     return LIB
 
 

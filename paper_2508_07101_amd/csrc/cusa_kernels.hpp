@@ -23,21 +23,9 @@
 #include <stdint.h>
 
 #include "attn_plan.hpp"
+#include "cache_view.hpp"
 
 namespace cusa {
-
-constexpr int D = 128;        // head_dim
-constexpr int PAGE = 16;      // tokens per page of a paged cache
-
-struct KvView {
-    const uint16_t* k;
-    const uint16_t* v;
-    int64_t sb, sh, st;       // contiguous: element strides (batch, kv head, token)
-    const int32_t* bt;        // paged: block table [B][max_pages]
-    int32_t max_pages;
-    int32_t G;                // kv heads
-    const int32_t* seq_lens;  // [B]
-};
 
 template <bool PAGED>
 __device__ __forceinline__ int64_t row_offset(const KvView& kv, int b, int kvh, int pos) {
@@ -47,11 +35,6 @@ __device__ __forceinline__ int64_t row_offset(const KvView& kv, int b, int kvh, 
     }
     return (int64_t)b * kv.sb + (int64_t)kvh * kv.sh + (int64_t)pos * kv.st;
 }
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 // 16 bytes of a K or V row.  Every row is read once per pass, so the load carries the streaming
 // (non-temporal) hint: the caches need not keep what will not be asked for again.  On this machine that
@@ -68,15 +51,6 @@ __device__ __forceinline__ u32x4 row_load(const uint16_t* p) {
     return SHARED_ROWS ? *reinterpret_cast<const u32x4*>(p) : stream_load(p);
 }
 
-// A value at a wave-uniform address that no kernel of the launch writes: a scalar load.
-__device__ __forceinline__ int32_t uniform_load(const int32_t* p) {
-    return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)p;
-}
-
-// Where a running maximum of scores starts: no score of a tile needs to be finite.  (From -infinity, a first tile whose scores are all
-// -infinity makes NaN of its weights; from here they are 2^-infinity = 0.)
-constexpr float LOWEST = -3.402823466e38f;
-
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
@@ -85,13 +59,6 @@ __device__ __forceinline__ void unpack8(const uint4& w, float* f) {
     f[2] = bf16_lo(w.y); f[3] = bf16_hi(w.y);
     f[4] = bf16_lo(w.z); f[5] = bf16_hi(w.z);
     f[6] = bf16_lo(w.w); f[7] = bf16_hi(w.w);
-}
-
-__device__ __forceinline__ uint16_t f32_to_bf16_rne(float f) {
-    uint32_t u = __float_as_uint(f);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return 0x7fc0;   // NaN
-    u += 0x7fffu + ((u >> 16) & 1u);
-    return (uint16_t)(u >> 16);
 }
 
 // ---------------------------------------------------------------- scoring
