@@ -56,14 +56,13 @@ void launch_append(bool paged, dim3 grid, hipStream_t s, const AppendArgs& a) {
     else launch(KID_KV_APPEND, kv_append_kernel<DTYPE, false>, grid, APPEND_THREADS, 0, s, a);
 }
 
-template <int RT, int RG>
 void launch_tree(bool paged, dim3 grid, hipStream_t s, const TreeArgs& a) {
     if (a.idx) {
-        if (paged) launch(KID_TREE_ATTN, tree_attn_kernel<RT, RG, true, true>, grid, TREE_THREADS, 0, s, a);
-        else launch(KID_TREE_ATTN, tree_attn_kernel<RT, RG, false, true>, grid, TREE_THREADS, 0, s, a);
+        if (paged) launch(KID_TREE_ATTN, tree_attn_kernel<true, true>, grid, TREE_THREADS, 0, s, a);
+        else launch(KID_TREE_ATTN, tree_attn_kernel<false, true>, grid, TREE_THREADS, 0, s, a);
     } else {
-        if (paged) launch(KID_TREE_ATTN, tree_attn_kernel<RT, RG, true, false>, grid, TREE_THREADS, 0, s, a);
-        else launch(KID_TREE_ATTN, tree_attn_kernel<RT, RG, false, false>, grid, TREE_THREADS, 0, s, a);
+        if (paged) launch(KID_TREE_ATTN, tree_attn_kernel<true, false>, grid, TREE_THREADS, 0, s, a);
+        else launch(KID_TREE_ATTN, tree_attn_kernel<false, false>, grid, TREE_THREADS, 0, s, a);
     }
 }
 
@@ -213,12 +212,7 @@ cusa_status cusa_tree_attn(const cusa_params* params, const void* q, const cusa_
     const dim3 grid(pl.n_splits, G * pl.m_tiles, params->batch);
     const bool paged = kv->layout == CUSA_KV_PAGED;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    switch (pl.rows_wg) {
-        case 32: launch_tree<1, 1>(paged, grid, s, a); break;
-        case 64: launch_tree<2, 1>(paged, grid, s, a); break;
-        case 128: launch_tree<2, 2>(paged, grid, s, a); break;
-        default: launch_tree<2, 4>(paged, grid, s, a); break;
-    }
+    launch_tree(paged, grid, s, a);
     if (launch_status() != CUSA_OK) return CUSA_ERR_LAUNCH;
     if (pl.n_splits > 1) {
         const dim3 rows((unsigned)(((int64_t)tree->max_nodes * params->n_q_heads + 3) / 4), params->batch);

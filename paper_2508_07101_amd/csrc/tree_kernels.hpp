@@ -332,7 +332,7 @@ struct TreeArgs {
     int32_t max_tokens, max_nodes, words, budget, H, g_shift, m_tiles, n_splits;
 };
 
-constexpr int TREE_THREADS = 256;
+constexpr int TREE_WAVES = 8, TREE_THREADS = 64 * TREE_WAVES;
 
 // What a workgroup of one sequence has to do, the same in the attention and in the merge.
 struct TreeSpan {
@@ -352,7 +352,7 @@ __device__ __forceinline__ TreeSpan tree_work(const TreeArgs& a, int b, int unit
     s.chunk = max(piece + unit - 1, TREE_MIN_PIECE) / unit * unit;
     return s;
 }
-constexpr int TREE_UNIT = 128;             // tokens that a workgroup's waves take at a time, at most
+constexpr int TREE_UNIT = 256;             // tokens that a workgroup's waves take at a time, at most
 
 // Bits o .. o + 31 of a node's mask (o may be negative; bits before the first and behind the last are 0).
 __device__ __forceinline__ uint32_t mask_window(const uint64_t* row, int words, int o) {
@@ -366,245 +366,339 @@ __device__ __forceinline__ uint32_t mask_window(const uint64_t* row, int words, 
 
 __device__ __forceinline__ float other_half_max(float v) { return fmaxf(v, __shfl_xor(v, 32)); }
 
-// A wave's 32 RT rows against 32 tokens at a time, with V_MFMA_F32_32X32X16_BF16:
-//   S^T = K Q^T      operands: K's rows as they stand, Q's rows (in registers throughout); a lane gets one row's scores of 16 tokens, so that
-//                    the softmax runs along registers, with one exchange between the two halves of the wave
-//   O^T += V^T P^T   the scores' registers are P^T's operand as they are: 16 tokens of a product are taken in the order in which the lanes
-//                    hold them.  V's columns come by transposing LDS reads.
-// RG waves share a token tile and split the rows; 4 / RG such teams split the tokens and are added up in LDS at the end.
-template <int RT, int RG, bool PAGED, bool SPARSE>
-__global__ __launch_bounds__(TREE_THREADS, 1) void tree_attn_kernel(TreeArgs a) {
-    constexpr int TEAMS = 4 / RG;
-    constexpr int SUB = RG == 4 ? 2 : 1, TT = 32 * SUB;           // tokens of a team's tile
-    constexpr int ROWS = 32 * RT * RG;
-    constexpr int TILE_BYTES = TT * 256;                          // of K, and again of V
-    constexpr int LDS_TILES = TEAMS * 2 * 2 * TILE_BYTES, LDS_OUT = TEAMS * ROWS * D * 4;
-    __shared__ __attribute__((aligned(16))) unsigned char smem[LDS_TILES > LDS_OUT ? LDS_TILES : LDS_OUT];
-    __shared__ float sm_m[TEAMS][ROWS], sm_l[TEAMS][ROWS];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int team = wave / RG, mine = wave % RG, half = lane >> 5, col = lane & 31;
-    const int b = blockIdx.z, kvh = blockIdx.y / a.m_tiles, m_tile = blockIdx.y % a.m_tiles;
-    const TreeSpan s = tree_work<SPARSE>(a, b, TREE_UNIT);
-    const int g = 1 << a.g_shift, rows = s.n << a.g_shift, row0 = m_tile * ROWS;
-    const int begin = blockIdx.x * s.chunk;
-    if (row0 >= rows || begin >= s.all) return;
-    const int end = min(begin + s.chunk, s.all);
+// 16 bytes a lane from memory to LDS at `lds` + 16 * lane, past the registers.  Not the builtin: for that, the compiler lets every later
+// LDS read wait for all such loads, which leaves one tile under way at most.  Whoever uses the bytes waits for them (wait_tiles) and, where
+// another wave asked for them, meets it at a barrier.
+__device__ __forceinline__ void load_to_lds(const uint16_t* from, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+}
+// Until all but the newest `n` of this wave's requests of OPS each have arrived (n <= 2).
+template <int OPS>
+__device__ __forceinline__ void wait_tiles(int n) {
+    if (n >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * OPS) : "memory");
+    else if (n == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+__device__ __forceinline__ void wave_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
 
-    bf16x8 qf[RT][8];
-    int node[RT];
+constexpr int TREE_LIST = 4096;            // entries of a workgroup's list of rows: tokens of a chosen prefix, pages of a whole one
+constexpr int TREE_RING = 128 * 1024;      // bytes of LDS for token tiles
+struct TreeLds {
+    __attribute__((aligned(16))) unsigned char ring[TREE_RING];
+    int32_t list[TREE_LIST];
+    float m[TREE_ROWS], l[TREE_ROWS];      // of every row, a set for each team
+    uint32_t odd[TREE_MAX_NODES / 32];     // nodes among this workgroup's tokens with a value that is not finite
+};
+
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+
+// The state of a wave's 32 rows, one to a lane and its counterpart in the other half of the wave.
+struct TreeRow {
+    bf16x8 q[8];           // columns 16 k + 8 half ..
+    f32x16 o[4];           // columns 32 d + 8 (i / 4) + 4 half + i % 4
+    float m, l;            // reference of the weights in log2 units, the half's sum of weights
+};
+
+// 32 tokens: scores, weights, and their share of the output.  S^T = K Q^T takes K's rows as they stand in the tile; a lane gets its row's scores of
+// the 16 tokens 8 (i / 4) + 4 half + i % 4.  In that order they are O^T += V^T P^T's operand, with V's columns from transposing LDS reads.
+// A row's reference follows its maximum only when that has grown by more than 8 (weights of up to 2^8, in 32 bits until they are rounded to bf16 relative
+// to themselves): the output's 64 registers are hardly ever rescaled.
+// EDGE: the row attends to the tokens `allowed` (a bit each), and not every row to those outside `common`.  Values that are not finite must not meet
+// the weight 0 of a row that does not attend to them: outside `common` they are left out, and the lane's tokens with such values returned.
+template <bool EDGE>
+__device__ __forceinline__ uint32_t tree_step(TreeRow& r, const unsigned char* kt, const unsigned char* vt, uint32_t allowed, uint32_t common,
+                                              float scale_log2e, int lane) {
+    const int half = lane >> 5, col = lane & 31;
+    const unsigned char* const krow = kt + col * 256;
+    const int kx = (half ^ (col & 15)) << 4;                      // chunk 2 k + half of the row stands at (2 k + half) ^ (row & 15)
+    f32x16 x;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const int r = row0 + (mine * RT + rt) * 32 + col;
-        const bool there = r < rows;
-        node[rt] = there ? r >> a.g_shift : 0;
-        const uint16_t* p = a.q + (int64_t)(s.start + node[rt]) * a.q_stride + ((kvh << a.g_shift) + (r & (g - 1))) * D + half * 8;
+    for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+    bf16x8 kf[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            u32x4 v = *reinterpret_cast<const u32x4*>(p + k * 16);
-            if (!there) v = u32x4{0, 0, 0, 0};
-            qf[rt][k] = __builtin_bit_cast(bf16x8, v);
-        }
+    for (int k = 0; k < 8; ++k) kf[k] = *reinterpret_cast<const bf16x8*>(krow + (kx ^ (k << 5)));
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], r.q[k], x, 0, 0, 0);
+    // 16 lanes transpose 4 tokens by 16 columns: tokens 16 k + 4 half + .. and 8 further on
+    s16x8 vf[2][4];
+    const int tok = 4 * half + ((lane >> 2) & 3);
+    const unsigned char* const vrow = vt + tok * 256 + (lane & 1) * 8;
+    const int vx = (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) << 4, vs = ((lane >> 2) & 3) << 6;
+    auto values = [&](int k, int d) {
+        const unsigned char* at = vrow + k * 4096 + (vx | ((d << 6) ^ vs));
+        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)at);
+        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 2048));
+        return __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    if (!EDGE) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) vf[k][d] = values(k, d);
     }
-    f32x16 o[RT][4];
-    float m[RT], l[RT];
+    if (EDGE) {
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        m[rt] = LOWEST;
-        l[rt] = 0.0f;
+        for (int i = 0; i < 16; ++i)
+            if (!(allowed >> (8 * (i >> 2) + 4 * half + (i & 3)) & 1)) x[i] = -INFINITY;
+    }
+    float mx = x[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, x[i]);
+    mx = other_half_max(mx) * scale_log2e;
+    const bool raise = mx > r.m + 8.0f;
+    if (__any(raise)) {
+        const float to = raise ? mx : r.m, f = exp2f(r.m - to);  // a row's sums do not depend on its neighbours
+        r.m = to;
+        r.l *= f;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[rt][d][i] = 0.0f;
+            for (int i = 0; i < 16; ++i) r.o[d][i] *= f;
     }
-
-    // Tokens [t0, t0 + TT) of the team into its buffer `st`; returns which of them are there, a bit each.
-    auto tile_at = [&](int st, int which) -> unsigned char* { return smem + ((team * 2 + st) * 2 + which) * TILE_BYTES; };
-    auto load = [&](int t0, int st) -> uint64_t {
-        const int i = t0 + (lane & (TT - 1));
-        bool ok = i < end;
-        int pos = i;
-        if (SPARSE) {
-            pos = ok ? (i < s.pre ? a.idx[(int64_t)b * a.budget + i] : s.before + (i - s.pre)) : 0;
-            ok = ok && (i >= s.pre || (uint32_t)pos < (uint32_t)s.before);
-        }
-        if (!ok) pos = 0;
-        int row = cache_row<PAGED>(a.cache, b, kvh, pos);
-        if (row < 0) ok = false;
-        if (!ok) row = 0;
-        const uint64_t live = __ballot(ok);
+    bf16x8 p[2];
+    float sum = 0.0f;
 #pragma unroll
-        for (int n = 0; n < TT / RG / 4; ++n) {
-            const int r0 = mine * (TT / RG) + n * 4, r = r0 + (lane >> 4);
-            const int64_t off = cache_offset<PAGED>(a.cache, b, kvh, __shfl(row, r));
-            const int ck = (lane & 15) ^ (r & 15), cv = (lane & 15) ^ ((r & 3) << 2);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(a.cache.kv.k + off + ck * 8),
-                                             (__attribute__((address_space(3))) void*)(tile_at(st, 0) + r0 * 256), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(a.cache.kv.v + off + cv * 8),
-                                             (__attribute__((address_space(3))) void*)(tile_at(st, 1) + r0 * 256), 16, 0, 0);
-        }
-        return TT == 32 ? live & 0xffffffffull : live;
-    };
-
-    const int steps = (end - begin + TT * TEAMS - 1) / (TT * TEAMS);
-    uint64_t live = load(begin + team * TT, 0);
-    for (int it = 0; it < steps; ++it) {
-        __builtin_amdgcn_s_waitcnt(0x0f70);                       // vmcnt(0)
-        __syncthreads();
-        const int t0 = begin + (it * TEAMS + team) * TT, st = it & 1;
-        uint64_t next = 0;
-        if (it + 1 < steps) next = load(t0 + TEAMS * TT, st ^ 1);
-        const unsigned char* kt = tile_at(st, 0);
-        const unsigned char* vt = tile_at(st, 1);
+    for (int i = 0; i < 16; ++i) {
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], scale_log2e, -r.m));
+        sum += e;
+        p[i >> 3][i & 7] = (__bf16)e;
+    }
+    r.l += sum;
+    uint32_t odd = 0;
+    const uint32_t wash = ~common >> (4 * half);
 #pragma unroll
-        for (int sub = 0; sub < SUB; ++sub) {
-            const uint32_t there = (uint32_t)(live >> (32 * sub));
-            if (there == 0) continue;
-            const int t = t0 + 32 * sub;
-            const bool edge = there != 0xffffffffu || t + 32 > s.pre;
-            f32x16 x[RT];
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
+        for (int d = 0; d < 4; ++d) {
+            if (EDGE) {
+                u32x4 v = __builtin_bit_cast(u32x4, values(k, d));
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[rt][i] = 0.0f;
-            const int kr = sub * 32 + col;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + kr * 256 + (((2 * k + half) ^ (kr & 15)) << 4));
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) x[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[rt][k], x[rt], 0, 0, 0);
+                for (int j = 0; j < 4; ++j) {                     // two tokens a word
+                    const uint32_t at = 1u << (16 * k + 2 * (j & 1) + 8 * (j >> 1));
+                    if ((v[j] & 0x7f80u) == 0x7f80u && (wash & at)) {
+                        odd |= at;
+                        v[j] &= 0xffff0000u;
+                    }
+                    if ((v[j] & 0x7f800000u) == 0x7f800000u && (wash & at << 1)) {
+                        odd |= at << 1;
+                        v[j] &= 0xffffu;
+                    }
+                }
+                vf[k][d] = __builtin_bit_cast(s16x8, v);
+                asm volatile("" ::: "memory");                    // one operand at a time: no registers for more
             }
-            uint32_t allowed[RT];
-            if (edge) {
+            r.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[k][d]), p[k], r.o[d], 0, 0, 0);
+        }
+    odd <<= 4 * half;
+    return odd;
+}
+
+// A workgroup's rows against tokens [begin, end).  RG waves share a token tile and split the rows; 8 / RG such teams split the tokens and are added up in
+// LDS at the end.  Two waves to a SIMD: one's softmax runs beside the other's products.  Tiles come by loads from memory straight to LDS, several of
+// them under way.
+template <int RG, bool PAGED, bool SPARSE>
+__device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, TreeLds& lds, int b, int kvh, int row0, int begin, int end) {
+    constexpr int TEAMS = TREE_WAVES / RG;
+    constexpr int SUB = RG == 8 ? 2 : 1, TT = 32 * SUB;           // tokens of a team's tile
+    constexpr int ROWS = 32 * RG;
+    constexpr int TILE_BYTES = TT * 256;                          // of K, and again of V
+    constexpr int STAGES = TREE_RING / (TEAMS * 2 * TILE_BYTES);  // 1, 2, 4, 4
+    constexpr int AHEAD = RG == 1 ? 1 : STAGES - 1;               // tiles asked for before one is used
+    constexpr int MINE = TT / RG;                                 // rows that a wave loads
+    constexpr int OPS = 2 * MINE / 4;                             // its loads for a tile
+    constexpr bool LIST = PAGED || SPARSE;
+    static_assert(TEAMS * ROWS * D * 4 <= TREE_RING && TEAMS * ROWS <= TREE_ROWS && MINE % 4 == 0, "the teams' sums take the tiles' place");
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int team = wave / RG, mine = wave % RG, half = lane >> 5, col = lane & 31;
+    const int g = 1 << a.g_shift, rows = s.n << a.g_shift;
+    if (tid < TREE_MAX_NODES / 32) lds.odd[tid] = 0;
+    __syncthreads();
+
+    TreeRow row;
+    const int my_row = row0 + mine * 32 + col;
+    const bool mine_there = my_row < rows;
+    const int node = mine_there ? my_row >> a.g_shift : 0;
+    {
+        const uint16_t* p = a.q + (int64_t)(s.start + node) * a.q_stride + ((kvh << a.g_shift) + (my_row & (g - 1))) * D + half * 8;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            u32x4 v = *reinterpret_cast<const u32x4*>(p + k * 16);
+            if (!mine_there) v = u32x4{0, 0, 0, 0};
+            row.q[k] = __builtin_bit_cast(bf16x8, v);
+        }
+    }
+    row.m = LOWEST;
+    row.l = 0.0f;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) row.o[d][i] = 0.0f;
+    const bool idle = row0 + mine * 32 >= rows;                   // a wave without rows loads its share and computes nothing
+
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds.ring;
+    const uint16_t* const kbase = a.cache.kv.k + (PAGED ? 0 : (int64_t)b * a.cache.kv.sb + (int64_t)kvh * a.cache.kv.sh);
+    const uint16_t* const vbase = a.cache.kv.v + (PAGED ? 0 : (int64_t)b * a.cache.kv.sb + (int64_t)kvh * a.cache.kv.sh);
+    const int64_t stride = PAGED ? D : a.cache.kv.st;
+    // A lane's part of a row, in the order in which LDS holds it: K's 16-byte chunk c of row r stands at c ^ (r & 15), V's at c ^ (4 (r & 3)), so
+    // that neither the rows of an operand nor the transposing reads meet in a bank.
+    const int lr = lane >> 4, vchunk = (lane & 15) ^ (lr << 2);
+
+    for (int c0 = begin; c0 < end;) {                             // as many tokens as the list has room for
+        const int c1 = LIST ? min(end, c0 + (SPARSE ? TREE_LIST : TREE_LIST * PAGE)) : end;
+        const int steps = (c1 - c0 + TT * TEAMS - 1) / (TT * TEAMS);
+        bool good = true;
+        if (LIST) {
+            const int entries = SPARSE ? min(steps * TT * TEAMS, TREE_LIST) : (c1 - c0 + PAGE - 1) / PAGE;
+            bool bad = false;
+            for (int e = tid; e < entries; e += TREE_THREADS) {
+                int at = -1;
+                if (SPARSE) {
+                    const int i = c0 + e;
+                    if (i < c1) {
+                        const int pos = i < s.pre ? a.idx[(int64_t)b * a.budget + i] : s.before + (i - s.pre);
+                        if (i >= s.pre || (uint32_t)pos < (uint32_t)s.before) at = cache_row<PAGED>(a.cache, b, kvh, pos);
+                        bad |= at < 0;
+                    }
+                } else {
+                    at = cache_row<PAGED>(a.cache, b, kvh, c0 + e * PAGE);
+                    bad |= at < 0;
+                }
+                lds.list[e] = at;
+            }
+            good = !__syncthreads_or(bad);
+        }
+        auto request = [&](int it) {
+            const int t = c0 + (it * TEAMS + team) * TT, r0 = mine * MINE;
+            const uint32_t kt = ring + ((it % STAGES) * TEAMS + team) * (2 * TILE_BYTES) + r0 * 256, vt = kt + TILE_BYTES;
+#pragma unroll
+            for (int n = 0; n < MINE / 4; ++n) {
+                const int r = r0 + n * 4 + lr;
+                int at;
+                if (SPARSE) at = max(lds.list[min(t - c0 + r, TREE_LIST - 1)], 0);
+                else if (PAGED) at = max(lds.list[min((t - c0 + r) >> 4, TREE_LIST - 1)], 0) + (r & (PAGE - 1));
+                else at = min(t + r, end - 1);
+                if (PAGED && !SPARSE && t + r0 + n * 4 >= c1) at = 0;   // (behind the list's last entry)
+                const int64_t off = (int64_t)at * stride;
+                load_to_lds(kbase + off + (((lane & 15) ^ (r & 15)) << 3), kt + n * 1024);
+                load_to_lds(vbase + off + (vchunk << 3), vt + n * 1024);
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (i < steps) request(i);
+        auto arrive = [&](int it) {                               // tile `it` is there, for the team
+            wait_tiles<OPS>(min(steps - 1 - it, AHEAD - 1));
+            if (RG > 1) {
+                wave_barrier();
+                if (it + AHEAD < steps) request(it + AHEAD);
+            }
+        };
+        auto leave = [&](int it) {
+            if (RG == 1 && it + AHEAD < steps) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the buffer's last reads
+                request(it + AHEAD);
+            }
+        };
+        auto tile_of = [&](int it) -> const unsigned char* { return lds.ring + ((it % STAGES) * TEAMS + team) * (2 * TILE_BYTES); };
+        // Tiles that every row attends to as a whole, then the others.  (In one loop the two forms' registers got in each other's way.)
+        const int plain = good ? max(0, min(s.pre, c1) - c0) / (TT * TEAMS) : 0;
+#pragma unroll 1
+        for (int it = 0; it < plain; ++it) {
+            arrive(it);
+            const unsigned char* const kt = tile_of(it);
+            if (!idle) {
+#pragma unroll 1
+                for (int sub = 0; sub < SUB; ++sub) tree_step<false>(row, kt + sub * 8192, kt + TILE_BYTES + sub * 8192, 0, 0, a.scale_log2e, lane);
+            }
+            leave(it);
+        }
+#pragma unroll 1
+        for (int it = plain; it < steps; ++it) {
+            arrive(it);
+            const unsigned char* const kt = tile_of(it);
+#pragma unroll 1
+            for (int sub = 0; sub < SUB; ++sub) {
+                const int t = c0 + (it * TEAMS + team) * TT + 32 * sub;
+                uint32_t there = t + 32 <= c1 ? 0xffffffffu : t >= c1 ? 0u : (1u << (c1 - t)) - 1;
+                if (LIST && !good) {
+                    const int i = t - c0 + col;
+                    there = (uint32_t)__ballot(t + col < c1 && lds.list[SPARSE ? i : i >> 4] >= 0);
+                }
+                if (there == 0 || idle) continue;
                 const int from = s.pre - t;                       // tokens of the prefix in this step
                 const uint32_t prefix = from >= 32 ? 0xffffffffu : from <= 0 ? 0u : (1u << from) - 1;
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    const uint32_t own = mask_window(a.masks + (int64_t)(s.start + node[rt]) * a.words, a.words, t - s.pre);
-                    allowed[rt] = (prefix | own) & there;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (!(allowed[rt] >> (8 * (i >> 2) + 4 * half + (i & 3)) & 1)) x[rt][i] = -INFINITY;
+                const uint32_t own = mask_window(a.masks + (int64_t)(s.start + node) * a.words, a.words, t - s.pre);
+                uint32_t odd = tree_step<true>(row, kt + sub * 8192, kt + TILE_BYTES + sub * 8192, (prefix | own) & there, prefix & there, a.scale_log2e, lane);
+                for (odd &= there; odd; odd &= odd - 1) {         // nodes (what is not there stays away)
+                    const int i = t + __builtin_ctz(odd) - s.pre;
+                    atomicOr(&lds.odd[i >> 5], 1u << (i & 31));
                 }
             }
-            bool raise = false;
-            float mt[RT];
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                float mx = x[rt][0];
-#pragma unroll
-                for (int i = 1; i < 16; ++i) mx = fmaxf(mx, x[rt][i]);
-                mt[rt] = other_half_max(mx) * a.scale_log2e;
-                raise |= mt[rt] > m[rt] + 8.0f;
-            }
-            if (__any(raise)) {
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    const float to = mt[rt] > m[rt] + 8.0f ? mt[rt] : m[rt], f = exp2f(m[rt] - to);   // a row's sums do not depend on its neighbours
-                    m[rt] = to;
-                    l[rt] *= f;
-#pragma unroll
-                    for (int d = 0; d < 4; ++d)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[rt][d][i] *= f;
-                }
-            }
-            bf16x8 p[RT][2];
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[rt][i], a.scale_log2e, -m[rt]));
-                    l[rt] += e;
-                    p[rt][i >> 3][i & 7] = (__bf16)e;
-                }
-            uint32_t odd = 0;                                     // edge: this lane's tokens with a value that is not finite
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    const int tok = sub * 32 + 16 * k + 4 * half + ((lane >> 2) & 3);
-                    const int chunk = (4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (((lane >> 2) & 3) << 2);
-                    typedef __attribute__((address_space(3))) s16x4* lds_ptr;
-                    const unsigned char* at = vt + tok * 256 + (chunk << 4) + (lane & 1) * 8;
-                    const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at);
-                    const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 8 * 256));
-                    typedef short s16x8 __attribute__((ext_vector_type(8)));
-                    s16x8 v = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
-                    if (edge) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if ((v[j] & 0x7f80) == 0x7f80) {
-                                odd |= 1u << (16 * k + 4 * half + (j & 3) + 8 * (j >> 2));
-                                v[j] = 0;
-                            }
-                    }
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt)
-                        o[rt][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), p[rt][k], o[rt][d], 0, 0, 0);
-                }
-            if (edge && __any(odd != 0)) {
-                // Values that are not finite reach the rows that attend to them, and only those: a weight of 0 would make NaN of them.
-                // (They were left out above; what they give does not depend on the weight.)
-                for (int tok = 0; tok < 32; ++tok) {
-                    if (!__any(odd >> tok & 1)) continue;
-#pragma unroll
-                    for (int d = 0; d < 4; ++d)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int c = 32 * d + 8 * (i >> 2) + 4 * half + (i & 3), row = sub * 32 + tok;
-                            const uint16_t w = *reinterpret_cast<const uint16_t*>(vt + row * 256 + (((c >> 3) ^ ((row & 3) << 2)) << 4) + (c & 7) * 2);
-                            if ((w & 0x7f80) != 0x7f80) continue;
-#pragma unroll
-                            for (int rt = 0; rt < RT; ++rt)
-                                if (allowed[rt] >> tok & 1) o[rt][d][i] += __uint_as_float((uint32_t)w << 16);
-                        }
-                }
-            }
+            leave(it);
         }
-        live = next;
+        c0 = c1;
+        if (LIST && c0 < end) __syncthreads();                    // before the list's next entries, and the ring's first tiles
     }
 
     // The teams' sums, brought to a common maximum, meet in LDS and leave it row by row.
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        l[rt] += __shfl_xor(l[rt], 32);
+    row.l += __shfl_xor(row.l, 32);
+    {
+        const int r = team * ROWS + mine * 32 + col;
         if (half == 0) {
-            const int r = (mine * RT + rt) * 32 + col;
-            sm_m[team][r] = m[rt];
-            sm_l[team][r] = l[rt];
+            lds.m[r] = row.m;
+            lds.l[r] = row.l;
         }
     }
     __syncthreads();
+    {
+        const int r = mine * 32 + col;
+        float top = lds.m[r];
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const int r = (mine * RT + rt) * 32 + col;
-        float top = sm_m[0][r];
-#pragma unroll
-        for (int w = 1; w < TEAMS; ++w) top = fmaxf(top, sm_m[w][r]);
-        const float f = exp2f(m[rt] - top);
+        for (int w = 1; w < TEAMS; ++w) top = fmaxf(top, lds.m[w * ROWS + r]);
+        const float f = exp2f(row.m - top);
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
             for (int q4 = 0; q4 < 4; ++q4) {
                 const int c = 8 * d + 2 * q4 + half;              // 16 bytes of the row
-                *reinterpret_cast<f32x4*>(smem + (team * ROWS + r) * (D * 4) + ((c ^ (r & 31)) << 4)) =
-                    f32x4{o[rt][d][q4 * 4] * f, o[rt][d][q4 * 4 + 1] * f, o[rt][d][q4 * 4 + 2] * f, o[rt][d][q4 * 4 + 3] * f};
+                *reinterpret_cast<f32x4*>(lds.ring + (team * ROWS + r) * (D * 4) + ((c ^ (r & 31)) << 4)) =
+                    f32x4{row.o[d][q4 * 4] * f, row.o[d][q4 * 4 + 1] * f, row.o[d][q4 * 4 + 2] * f, row.o[d][q4 * 4 + 3] * f};
             }
     }
     __syncthreads();
     const bool whole = s.chunk >= s.all;
+    bool any_odd = false;
+#pragma unroll
+    for (int i = 0; i < TREE_MAX_NODES / 32; ++i) any_odd |= lds.odd[i] != 0;
     for (int item = tid; item < ROWS * 32; item += TREE_THREADS) {
         const int r = item >> 5, c = item & 31, row = row0 + r;
         if (row >= rows) break;
-        float top = sm_m[0][r];
+        float top = lds.m[r];
 #pragma unroll
-        for (int w = 1; w < TEAMS; ++w) top = fmaxf(top, sm_m[w][r]);
+        for (int w = 1; w < TEAMS; ++w) top = fmaxf(top, lds.m[w * ROWS + r]);
         float sum = 0.0f;
         f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int w = 0; w < TEAMS; ++w) {
-            sum += sm_l[w][r] * exp2f(sm_m[w][r] - top);
-            v += *reinterpret_cast<const f32x4*>(smem + (w * ROWS + r) * (D * 4) + ((c ^ (r & 31)) << 4));
+            sum += lds.l[w * ROWS + r] * exp2f(lds.m[w * ROWS + r] - top);
+            v += *reinterpret_cast<const f32x4*>(lds.ring + (w * ROWS + r) * (D * 4) + ((c ^ (r & 31)) << 4));
+        }
+        if (any_odd) {
+            // Nodes with values that are not finite: the rows that attend to them get those values (whatever the weight: it is not 0).
+            const uint64_t* mask = a.masks + (int64_t)(s.start + (row >> a.g_shift)) * a.words;
+            for (int i = 0; i < s.n; ++i) {
+                if (!(lds.odd[i >> 5] >> (i & 31) & 1) || !(mask[i >> 6] >> (i & 63) & 1)) continue;
+                const int at = cache_row<PAGED>(a.cache, b, kvh, s.before + i);
+                const u32x2 w = *reinterpret_cast<const u32x2*>(a.cache.kv.v + cache_offset<PAGED>(a.cache, b, kvh, max(at, 0)) + c * 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t x = (j & 1) ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16;
+                    if ((x & 0x7f800000u) == 0x7f800000u) v[j] += __uint_as_float(x);
+                }
+            }
         }
         const int64_t to = (int64_t)(s.start + (row >> a.g_shift)) * a.H + (kvh << a.g_shift) + (row & (g - 1));
         if (whole) {
@@ -618,6 +712,22 @@ __global__ __launch_bounds__(TREE_THREADS, 1) void tree_attn_kernel(TreeArgs a) 
             if (c == 0) *reinterpret_cast<f32x2*>(a.part_ml + piece * 2) = f32x2{top, sum};
         }
     }
+}
+
+// Which form a workgroup takes goes by the rows that its own tree has, not by the bound: trees of a batch differ.
+template <bool PAGED, bool SPARSE>
+__global__ __launch_bounds__(TREE_THREADS, 2) void tree_attn_kernel(TreeArgs a) {
+    __shared__ TreeLds lds;
+    const int b = blockIdx.z, kvh = blockIdx.y / a.m_tiles, row0 = (blockIdx.y % a.m_tiles) * TREE_ROWS;
+    const TreeSpan s = tree_work<SPARSE>(a, b, TREE_UNIT);
+    const int left = (s.n << a.g_shift) - row0;
+    const int begin = blockIdx.x * s.chunk;
+    if (left <= 0 || begin >= s.all) return;
+    const int end = min(begin + s.chunk, s.all);
+    if (left <= 32) tree_rows<1, PAGED, SPARSE>(a, s, lds, b, kvh, row0, begin, end);
+    else if (left <= 64) tree_rows<2, PAGED, SPARSE>(a, s, lds, b, kvh, row0, begin, end);
+    else if (left <= 128) tree_rows<4, PAGED, SPARSE>(a, s, lds, b, kvh, row0, begin, end);
+    else tree_rows<8, PAGED, SPARSE>(a, s, lds, b, kvh, row0, begin, end);
 }
 
 // A wave for a row: a lane for each piece's weight, then two columns a lane.

@@ -12,20 +12,16 @@ constexpr int TREE_MAX_SPLITS = 64;     // pieces of a sequence's tokens: one la
 constexpr int TREE_MIN_PIECE = 256;     // tokens
 constexpr int TREE_CUS = 256;
 
-// Rows (node, query head) of one KV head that a workgroup holds: the smallest form that takes all of a tree's, or the largest.
-inline int tree_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
+constexpr int TREE_ROWS = 256;          // rows (node, query head) of one KV head that a workgroup holds at most
 
 struct TreePlan {
-    int rows_wg;     // 32, 64, 128 or 256
     int m_tiles;     // workgroups that share a KV head's tokens
     int n_splits;    // pieces of a sequence's tokens at most; the kernel makes fewer of a short one
 };
 
 inline TreePlan plan_tree(int max_len, int pairs, int g, int max_nodes) {
     TreePlan p;
-    const int64_t rows = (int64_t)max_nodes * g;
-    p.rows_wg = tree_rows(rows);
-    p.m_tiles = (int)((rows + p.rows_wg - 1) / p.rows_wg);
+    p.m_tiles = (max_nodes * g + TREE_ROWS - 1) / TREE_ROWS;
     const int64_t wgs = (int64_t)pairs * p.m_tiles;
     const int64_t by_len = ((int64_t)max_len + TREE_MIN_PIECE - 1) / TREE_MIN_PIECE;
     p.n_splits = (int)std::max<int64_t>(1, std::min<int64_t>({TREE_CUS / wgs, by_len, (int64_t)TREE_MAX_SPLITS}));
@@ -40,8 +36,8 @@ struct TreeWs {
 inline TreeWs tree_workspace(int max_len, int batch, int H, int G, int max_tokens, int max_nodes) {
     const int g = H / G;
     size_t worst = 0;
-    for (int rows = 32;; rows *= 2) {
-        const int nodes = std::min(max_nodes, std::max(1, rows / g));
+    for (int tiles = 1;; ++tiles) {
+        const int nodes = std::min(max_nodes, tiles * TREE_ROWS / g);
         const TreePlan p = plan_tree(max_len, batch * G, g, nodes);
         const size_t tokens = (size_t)std::min<int64_t>(max_tokens, (int64_t)batch * nodes);
         if (p.n_splits > 1) worst = std::max(worst, tokens * H * p.n_splits);
