@@ -364,7 +364,11 @@ __device__ __forceinline__ uint32_t mask_window(const uint64_t* row, int words, 
     return (uint32_t)x;
 }
 
-__device__ __forceinline__ float other_half_max(float v) { return fmaxf(v, __shfl_xor(v, 32)); }
+// Of the lane's value and that of its counterpart in the other half of the wave.
+__device__ __forceinline__ float other_half_max(float v) {
+    const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+    return fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+}
 
 // 16 bytes a lane from memory to LDS at `lds` + 16 * lane, past the registers.  Not the builtin: for that, the compiler lets every later
 // LDS read wait for all such loads, which leaves one tile under way at most.  Whoever uses the bytes waits for them (wait_tiles) and, where
@@ -420,6 +424,7 @@ __device__ __forceinline__ uint32_t tree_step(TreeRow& r, const unsigned char* k
     bf16x8 kf[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) kf[k] = *reinterpret_cast<const bf16x8*>(krow + (kx ^ (k << 5)));
+    __builtin_amdgcn_sched_barrier(0);                            // all reads first: left alone, the products wait for one read after the other
 #pragma unroll
     for (int k = 0; k < 8; ++k) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], r.q[k], x, 0, 0, 0);
     // 16 lanes transpose 4 tokens by 16 columns: tokens 16 k + 4 half + .. and 8 further on
@@ -544,7 +549,8 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
     const int64_t stride = PAGED ? D : a.cache.kv.st;
     // A lane's part of a row, in the order in which LDS holds it: K's 16-byte chunk c of row r stands at c ^ (r & 15), V's at c ^ (4 (r & 3)), so
     // that neither the rows of an operand nor the transposing reads meet in a bank.
-    const int lr = lane >> 4, vchunk = (lane & 15) ^ (lr << 2);
+    const int lr = lane >> 4, vchunk = (lane & 15) ^ (lr << 2), koff = ((lane & 15) ^ ((mine * MINE + lr) & 15)) << 3;
+    const int64_t lane_off = (mine * MINE + lr) * stride;
 
     for (int c0 = begin; c0 < end;) {                             // as many tokens as the list has room for
         const int c1 = LIST ? min(end, c0 + (SPARSE ? TREE_LIST : TREE_LIST * PAGE)) : end;
@@ -575,14 +581,18 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
             const uint32_t kt = ring + ((it % STAGES) * TEAMS + team) * (2 * TILE_BYTES) + r0 * 256, vt = kt + TILE_BYTES;
 #pragma unroll
             for (int n = 0; n < MINE / 4; ++n) {
-                const int r = r0 + n * 4 + lr;
-                int at;
-                if (SPARSE) at = max(lds.list[min(t - c0 + r, TREE_LIST - 1)], 0);
-                else if (PAGED) at = max(lds.list[min((t - c0 + r) >> 4, TREE_LIST - 1)], 0) + (r & (PAGE - 1));
-                else at = min(t + r, end - 1);
-                if (PAGED && !SPARSE && t + r0 + n * 4 >= c1) at = 0;   // (behind the list's last entry)
-                const int64_t off = (int64_t)at * stride;
-                load_to_lds(kbase + off + (((lane & 15) ^ (r & 15)) << 3), kt + n * 1024);
+                const int r = n * 4 + lr;                         // (K's chunks are turned by r0 + r: koff)
+                int64_t off;
+                if (SPARSE) {
+                    off = (int64_t)max(lds.list[min(t - c0 + r0 + r, TREE_LIST - 1)], 0) * stride;
+                } else if (PAGED) {
+                    // a wave's rows of a tile share pages of 16; behind the list's last entry row 0 has to do
+                    const int page = (t - c0 + r0 + n * 4) >> 4;
+                    off = (int64_t)((t + r0 + n * 4 < c1 ? max(lds.list[page], 0) : 0) + ((r0 + n * 4) & (PAGE - 1)) + lr) * D;
+                } else {
+                    off = t + TT <= end ? (t + n * 4) * stride + lane_off : min(t + r0 + r, end - 1) * stride;
+                }
+                load_to_lds(kbase + off + (koff ^ ((n * 4 & 15) << 3)), kt + n * 1024);
                 load_to_lds(vbase + off + (vchunk << 3), vt + n * 1024);
             }
         };
