@@ -321,7 +321,8 @@ cusa_status cusa_tree_masks(int32_t batch, const int32_t* base, const int32_t* t
  * A node that attends to nothing gives zeros.  NaN and infinities in rows that a node does not attend to do not reach its output.
  * q: device bf16, row r head h at q + r * q_stride + h * 128; out: device bf16 [max_tokens][n_q_heads][128]; rows of no
  * sequence are not written.  ws: cusa_tree_workspace_bytes, 256-byte aligned, content not preserved.
- * Errors as cusa_full_attn, and UNSUPPORTED for max_nodes > 256 and for pools of 2^31 or more rows. */
+ * Errors as cusa_full_attn, and UNSUPPORTED for max_nodes > 256, pools of 2^31 or more rows, max_seq_len above 5242880 and, with idx, budget + max_nodes
+ * above 327680. */
 cusa_status cusa_tree_workspace_bytes(const cusa_params* params, int32_t max_seq_len, int32_t max_tokens, int32_t max_nodes, size_t* bytes);
 cusa_status cusa_tree_attn(const cusa_params* params, const void* q, const cusa_kv* kv, const cusa_tree* tree, const int32_t* idx,
                            const int32_t* cnt, void* out, void* ws, size_t ws_bytes, void* stream);

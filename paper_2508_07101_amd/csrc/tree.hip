@@ -10,6 +10,7 @@ using namespace cusa;
 namespace {
 
 constexpr int MAX_BATCH = 65535;           // a dimension of the grids
+constexpr int64_t MAX_STRIDE = 1 << 26;    // elements between two tokens: some rows' offset fits 32 bits of bytes
 
 size_t plan_ws_bytes(int batch) { return 256 + align256((size_t)batch * sizeof(PlanSeq)); }
 
@@ -24,7 +25,7 @@ cusa_status check_pool(const cusa_pool* p) {
     return CUSA_OK;
 }
 
-// A cache that these kernels can address: check_kv's rules, and row numbers that fit 31 bits.
+// A cache that these kernels can address: check_kv's rules, row numbers and a token's stride that fit 31 bits.
 cusa_status check_cache(const cusa_params* p, const cusa_kv* kv, bool reads_tables) {
     cusa_kv c;
     if (!kv) return CUSA_ERR_INVALID_ARG;
@@ -37,6 +38,7 @@ cusa_status check_cache(const cusa_params* p, const cusa_kv* kv, bool reads_tabl
     const cusa_status st = check_kv(p, &c);
     if (st != CUSA_OK) return st;
     if (p->batch > MAX_BATCH || p->n_kv_heads > MAX_BATCH || kv->max_seq_len > (1 << 30)) return CUSA_ERR_UNSUPPORTED;
+    if (kv->layout == CUSA_KV_CONTIGUOUS && kv->stride_token > MAX_STRIDE) return CUSA_ERR_UNSUPPORTED;
     if (kv->layout == CUSA_KV_PAGED && kv->n_pages > 0x7fffffff / PAGE / p->n_kv_heads) return CUSA_ERR_UNSUPPORTED;
     return CUSA_OK;
 }
@@ -72,8 +74,8 @@ cusa_status check_tree_sizes(int32_t max_tokens, int32_t max_nodes) {
 }
 
 // Tokens of a sequence that a pass may have to look at.
-int tree_len(const cusa_params* p, int32_t max_seq_len, int32_t max_nodes, bool sparse) {
-    return sparse ? (int)std::min<int64_t>((int64_t)p->budget + max_nodes, (int64_t)max_seq_len + max_nodes) : max_seq_len;
+int64_t tree_len(const cusa_params* p, int32_t max_seq_len, int32_t max_nodes, TreeKind kind) {
+    return kind == TREE_CHOSEN ? (int64_t)p->budget + max_nodes : max_seq_len;
 }
 
 }  // namespace
@@ -169,8 +171,13 @@ cusa_status cusa_tree_workspace_bytes(const cusa_params* params, int32_t max_seq
     if (st != CUSA_OK) return st;
     if ((st = check_tree_sizes(max_tokens, max_nodes)) != CUSA_OK) return st;
     if (!bytes || max_seq_len < 1) return CUSA_ERR_INVALID_ARG;
-    const int len = std::max(tree_len(params, max_seq_len, max_nodes, true), max_seq_len);
-    *bytes = tree_workspace(len, params->batch, params->n_q_heads, params->n_kv_heads, max_tokens, max_nodes).total;
+    size_t most = 0;
+    for (const TreeKind kind : {TREE_FULL, TREE_CHOSEN}) {   // of those that are served
+        const int64_t len = tree_len(params, max_seq_len, max_nodes, kind);
+        if (!tree_len_served(kind, len)) continue;
+        most = std::max(most, tree_workspace(kind, (int)len, params->batch, params->n_q_heads, params->n_kv_heads, max_tokens, max_nodes).total);
+    }
+    *bytes = most;
     return CUSA_OK;
 }
 
@@ -184,11 +191,12 @@ cusa_status cusa_tree_attn(const cusa_params* params, const void* q, const cusa_
     if (tree->q_stride < (int64_t)params->n_q_heads * D || (tree->q_stride & 7)) return CUSA_ERR_INVALID_ARG;
     if (!ws || ((uintptr_t)ws & 255)) return CUSA_ERR_INVALID_ARG;
     const int g = params->n_q_heads / params->n_kv_heads, G = params->n_kv_heads;
-    const int len = tree_len(params, kv->max_seq_len, tree->max_nodes, idx != nullptr);
-    const TreeWs w = tree_workspace(len, params->batch, params->n_q_heads, G, tree->max_tokens, tree->max_nodes);
+    const TreeKind kind = idx ? TREE_CHOSEN : TREE_FULL;
+    const int64_t len = tree_len(params, kv->max_seq_len, tree->max_nodes, kind);
+    if (!tree_len_served(kind, len)) return CUSA_ERR_UNSUPPORTED;
+    const TreeWs w = tree_workspace(kind, (int)len, params->batch, params->n_q_heads, G, tree->max_tokens, tree->max_nodes);
     if (ws_bytes < w.total) return CUSA_ERR_WORKSPACE_TOO_SMALL;
-    const TreePlan pl = plan_tree(len, params->batch * G, g, tree->max_nodes);
-    if ((int64_t)G * pl.m_tiles > MAX_BATCH) return CUSA_ERR_UNSUPPORTED;
+    const TreePlan pl = plan_tree(kind, (int)len, params->batch, G, g, tree->max_nodes);
     TreeArgs a;
     a.cache = cache_args(params, kv);
     a.q = static_cast<const uint16_t*>(q);
@@ -200,6 +208,7 @@ cusa_status cusa_tree_attn(const cusa_params* params, const void* q, const cusa_
     a.out = static_cast<uint16_t*>(out);
     a.part_acc = ws_ptr<float>(ws, w.acc);
     a.part_ml = ws_ptr<float>(ws, w.ml);
+    a.pieces = ws_ptr<int32_t>(ws, w.pieces);
     a.scale_log2e = params->sm_scale * 1.4426950408889634f;
     a.max_tokens = tree->max_tokens;
     a.max_nodes = tree->max_nodes;
@@ -209,15 +218,17 @@ cusa_status cusa_tree_attn(const cusa_params* params, const void* q, const cusa_
     a.g_shift = g == 1 ? 0 : g == 2 ? 1 : g == 4 ? 2 : 3;
     a.m_tiles = pl.m_tiles;
     a.n_splits = pl.n_splits;
-    const dim3 grid(pl.n_splits, G * pl.m_tiles, params->batch);
+    a.batch = params->batch;
+    const int64_t units = ((int64_t)pl.n_splits * G * params->batch + 7) / 8 * 8;
+    if (units * pl.m_tiles > 0x7fffffff) return CUSA_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)(units * pl.m_tiles));
     const bool paged = kv->layout == CUSA_KV_PAGED;
     hipStream_t s = static_cast<hipStream_t>(stream);
     launch_tree(paged, grid, s, a);
     if (launch_status() != CUSA_OK) return CUSA_ERR_LAUNCH;
-    if (pl.n_splits > 1) {
-        const dim3 rows((unsigned)(((int64_t)tree->max_nodes * params->n_q_heads + 3) / 4), params->batch);
-        if (idx) launch(KID_TREE_REDUCE, tree_reduce_kernel<true>, rows, 256, 0, s, a);
-        else launch(KID_TREE_REDUCE, tree_reduce_kernel<false>, rows, 256, 0, s, a);
+    if (pl.n_splits > 1) {                 // as many workgroups as have a row each, but not more than a few rounds of the chip
+        const int64_t rows = ((int64_t)tree->max_nodes * params->n_q_heads + REDUCE_WAVES - 1) / REDUCE_WAVES, most = std::max(1, 8192 / params->batch);
+        launch(KID_TREE_REDUCE, tree_reduce_kernel, dim3((unsigned)std::min(rows, most), params->batch), 64 * REDUCE_WAVES, 0, s, a);
     }
     return launch_status();
 }

@@ -8,6 +8,8 @@
 //   tree_reduce_kernel  merges the pieces of a long prefix
 //   kv_commit_kernel    an accepted branch's rows moved together, all layers
 #pragma once
+#include <type_traits>
+
 #include "cache_view.hpp"
 #include "tree_plan.hpp"
 
@@ -328,11 +330,13 @@ struct TreeArgs {
     const uint64_t* masks;
     uint16_t* out;
     float *part_acc, *part_ml;
+    int32_t* pieces;       // of each sequence's tokens, for the merge
     float scale_log2e;
-    int32_t max_tokens, max_nodes, words, budget, H, g_shift, m_tiles, n_splits;
+    int32_t batch, max_tokens, max_nodes, words, budget, H, g_shift, m_tiles, n_splits;
 };
 
 constexpr int TREE_WAVES = 8, TREE_THREADS = 64 * TREE_WAVES;
+constexpr int TREE_TILE = 32;              // tokens of a tile: pieces are whole tiles
 
 // What a workgroup of one sequence has to do, the same in the attention and in the merge.
 struct TreeSpan {
@@ -341,18 +345,63 @@ struct TreeSpan {
     int chunk;             // tokens of a piece
 };
 template <bool SPARSE>
-__device__ __forceinline__ TreeSpan tree_work(const TreeArgs& a, int b, int unit) {
+__device__ __forceinline__ TreeSpan tree_span(const TreeArgs& a, int b) {
     TreeSpan s;
     const int L = clampi(a.cache.kv.seq_lens[b], 0, a.cache.max_len);
     s.n = min(tree_span(a.tok_start, b, a.max_tokens, a.max_nodes, s.start), L);
     s.before = L - s.n;
     s.pre = SPARSE ? clampi(a.cnt[b], 0, a.budget) : s.before;
-    s.all = s.pre + s.n;
-    const int piece = (s.all + a.n_splits - 1) / a.n_splits;
-    s.chunk = max(piece + unit - 1, TREE_MIN_PIECE) / unit * unit;
+    s.all = s.n > 0 ? s.pre + s.n : 0;
     return s;
 }
-constexpr int TREE_UNIT = 256;             // tokens that a workgroup's waves take at a time, at most
+__device__ __forceinline__ int tiles_of(int tokens) { return (tokens + TREE_TILE - 1) / TREE_TILE; }
+// The batch's pieces are of one length, which goes by the lengths that there are.  With the tiles T of all KV heads' sequences, W of these in number
+// and at most M tiles in one, pieces of ceil(M / floor(R / W)) tiles are R at most, and so are pieces of T / (R - W) tiles (a last piece each is shorter):
+// the first is exact for sequences of one length, the second close for any.  R: one to eight workgroups for each CU; more are better balanced, but
+// each costs about TREE_PIECE_COST tiles besides its own (its start, and partial sums written and read).
+template <bool SPARSE>
+__device__ __forceinline__ TreeSpan tree_work(const TreeArgs& a, int b) {
+    TreeSpan s = tree_span<SPARSE>(a, b);
+    int piece = tiles_of(s.all);
+    if (a.n_splits > 1) {
+        int total = 0, pairs = 0, most = 0;
+        for (int i = threadIdx.x & 63; i < a.batch; i += 64) {
+            const TreeSpan o = tree_span<SPARSE>(a, i);
+            const int wgs = a.cache.kv.G * (((o.n << a.g_shift) + TREE_ROWS - 1) / TREE_ROWS), t = tiles_of(o.all);
+            total += t * wgs;
+            pairs += wgs;
+            most = max(most, t);
+        }
+        if (a.batch > 1) {
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                total += __shfl_xor(total, o);
+                pairs += __shfl_xor(pairs, o);
+                most = max(most, __shfl_xor(most, o));
+            }
+        }
+        total = __builtin_amdgcn_readfirstlane(total);
+        pairs = max(__builtin_amdgcn_readfirstlane(pairs), 1);
+        most = __builtin_amdgcn_readfirstlane(most);
+        int best = 0x7fffffff;
+#pragma unroll 1
+        for (int r = 1; r <= (a.batch > 1 ? 8 : 1); ++r) {
+            const int wgs = r * TREE_CUS;
+            if (wgs < pairs) continue;
+            int c = (most + wgs / pairs - 1) / (wgs / pairs);
+            if (wgs > pairs) c = min(c, (total + wgs - pairs - 1) / (wgs - pairs));
+            c = max(c, TREE_MIN_PIECE / TREE_TILE);
+            if (r * (c + TREE_PIECE_COST) < best) {
+                best = r * (c + TREE_PIECE_COST);
+                piece = c;
+            }
+        }
+        piece = min(piece, (SPARSE ? TREE_LIST : TREE_LIST * PAGE) / TREE_TILE);   // what a workgroup's list has room for
+        piece = max(piece, (tiles_of(s.all) + a.n_splits - 1) / a.n_splits);       // what the launch has workgroups for
+    }
+    s.chunk = piece * TREE_TILE;
+    return s;
+}
 
 // Bits o .. o + 31 of a node's mask (o may be negative; bits before the first and behind the last are 0).
 __device__ __forceinline__ uint32_t mask_window(const uint64_t* row, int words, int o) {
@@ -373,21 +422,31 @@ __device__ __forceinline__ float other_half_max(float v) {
 // 16 bytes a lane from memory to LDS at `lds` + 16 * lane, past the registers.  Not the builtin: for that, the compiler lets every later
 // LDS read wait for all such loads, which leaves one tile under way at most.  Whoever uses the bytes waits for them (wait_tiles) and, where
 // another wave asked for them, meets it at a barrier.
-__device__ __forceinline__ void load_to_lds(const uint16_t* from, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+// `once`: nobody else reads these bytes, so the caches need not keep them (a copy of 128 MB to LDS by 256 workgroups: 24.4 us, so 19.7).
+__device__ __forceinline__ void load_to_lds(const uint16_t* from, uint32_t lds, bool once) {
+    if (once) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(lds), "v"(from) : "memory");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
 }
-// Until all but the newest `n` of this wave's requests of OPS each have arrived (n <= 2).
-template <int OPS>
+// The same from a uniform address and 32 bits of offset a lane.
+__device__ __forceinline__ void load_to_lds(const uint16_t* base, uint32_t offset, uint32_t lds, bool once) {
+    if (once) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+}
+// Until all but the newest min(n, MOST) of this wave's requests of OPS loads each have arrived.
+template <int OPS, int MOST>
 __device__ __forceinline__ void wait_tiles(int n) {
-    if (n >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * OPS) : "memory");
-    else if (n == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS) : "memory");
+    static_assert(OPS * MOST < 64, "the counter's range");
+    if (MOST > 0 && n >= MOST) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS * MOST) : "memory");
+        return;
+    }
+    if constexpr (MOST > 1) wait_tiles<OPS, MOST - 1>(n);
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 __device__ __forceinline__ void wave_barrier() {
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-constexpr int TREE_LIST = 4096;            // entries of a workgroup's list of rows: tokens of a chosen prefix, pages of a whole one
 constexpr int TREE_RING = 128 * 1024;      // bytes of LDS for token tiles
 struct TreeLds {
     __attribute__((aligned(16))) unsigned char ring[TREE_RING];
@@ -399,122 +458,191 @@ struct TreeLds {
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
 
-// The state of a wave's 32 rows, one to a lane and its counterpart in the other half of the wave.
+// The state of a wave's 32 rows: a lane and its counterpart in the other half of the wave have one row.
 struct TreeRow {
     bf16x8 q[8];           // columns 16 k + 8 half ..
     f32x16 o[4];           // columns 32 d + 8 (i / 4) + 4 half + i % 4
     float m, l;            // reference of the weights in log2 units, the half's sum of weights
 };
 
-// 32 tokens: scores, weights, and their share of the output.  S^T = K Q^T takes K's rows as they stand in the tile; a lane gets its row's scores of
-// the 16 tokens 8 (i / 4) + 4 half + i % 4.  In that order they are O^T += V^T P^T's operand, with V's columns from transposing LDS reads.
-// A row's reference follows its maximum only when that has grown by more than 8 (weights of up to 2^8, in 32 bits until they are rounded to bf16 relative
-// to themselves): the output's 64 registers are hardly ever rescaled.
-// EDGE: the row attends to the tokens `allowed` (a bit each), and not every row to those outside `common`.  Values that are not finite must not meet
-// the weight 0 of a row that does not attend to them: outside `common` they are left out, and the lane's tokens with such values returned.
-template <bool EDGE>
-__device__ __forceinline__ uint32_t tree_step(TreeRow& r, const unsigned char* kt, const unsigned char* vt, uint32_t allowed, uint32_t common,
-                                              float scale_log2e, int lane) {
-    const int half = lane >> 5, col = lane & 31;
-    const unsigned char* const krow = kt + col * 256;
-    const int kx = (half ^ (col & 15)) << 4;                      // chunk 2 k + half of the row stands at (2 k + half) ^ (row & 15)
+// S^T = K Q^T of 32 tokens: K's rows as they stand in the tile; a lane gets its row's scores of the tokens 8 (i / 4) + 4 half + i % 4.
+struct TreeKeys {
+    bf16x8 f[8];
+};
+// Where a lane reads in a tile, for the tile at LDS address 0: chunk 2 k + half of K's row `col` stands at (2 k + half) ^ (col & 15).  V's columns 32 d .. of
+// the tokens 16 k .. come in the order in which the lanes hold the scores: 16 lanes transpose 4 tokens by 16 columns, tokens 16 k + 4 half + .. and
+// 8 further on.
+__device__ __forceinline__ uint32_t key_at(int lane, int k) { return (lane & 31) * 256 + ((((lane >> 5) ^ (lane & 15)) << 4) ^ (k << 5)); }
+__device__ __forceinline__ uint32_t value_at(int lane, int d) {
+    const int row4 = (lane >> 2) & 3;
+    return (4 * (lane >> 5) + row4) * 256 + (lane & 1) * 8 + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) << 4) | ((d ^ row4) << 6));
+}
+typedef const __attribute__((address_space(3))) bf16x8* lds_bf16x8;
+__device__ __forceinline__ bf16x8 read_key(uint32_t at) { return *(lds_bf16x8)(uintptr_t)at; }
+__device__ __forceinline__ s16x8 read_value(uint32_t at) {
+    const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)at);
+    const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(at + 2048));
+    return __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+__device__ __forceinline__ void read_keys(TreeKeys& kf, uint32_t kt, int lane) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) kf.f[k] = read_key(kt + key_at(lane, k));
+}
+__device__ __forceinline__ f32x16 score(const TreeRow& r, const TreeKeys& kf) {
     f32x16 x;
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = 0.0f;
-    bf16x8 kf[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) kf[k] = *reinterpret_cast<const bf16x8*>(krow + (kx ^ (k << 5)));
-    __builtin_amdgcn_sched_barrier(0);                            // all reads first: left alone, the products wait for one read after the other
+    for (int k = 0; k < 8; ++k) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf.f[k], r.q[k], x, 0, 0, 0);
+    return x;
+}
+struct TreeValues {
+    s16x8 f[2][4];
+};
+__device__ __forceinline__ void read_values(TreeValues& vf, uint32_t vt, int lane) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], r.q[k], x, 0, 0, 0);
-    // 16 lanes transpose 4 tokens by 16 columns: tokens 16 k + 4 half + .. and 8 further on
-    s16x8 vf[2][4];
-    const int tok = 4 * half + ((lane >> 2) & 3);
-    const unsigned char* const vrow = vt + tok * 256 + (lane & 1) * 8;
-    const int vx = (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) << 4, vs = ((lane >> 2) & 3) << 6;
-    auto values = [&](int k, int d) {
-        const unsigned char* at = vrow + k * 4096 + (vx | ((d << 6) ^ vs));
-        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)at);
-        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 2048));
-        return __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
-    if (!EDGE) {
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int d = 0; d < 4; ++d) vf.f[k][d] = read_value(vt + 4096 * k + value_at(lane, d));
+}
+// O^T += V^T P^T: the weights are the product's operand in the order in which the lanes hold them.
+struct TreeWeights {
+    bf16x8 f[2];
+};
+template <int K>
+__device__ __forceinline__ void add_values(TreeRow& r, const TreeValues& vf, const TreeWeights& p) {
 #pragma unroll
-            for (int d = 0; d < 4; ++d) vf[k][d] = values(k, d);
+    for (int d = 0; d < 4; ++d) r.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf.f[K][d]), p.f[K], r.o[d], 0, 0, 0);
+}
+__device__ __forceinline__ void add_values(TreeRow& r, const TreeValues& vf, const TreeWeights& p) {
+    add_values<0>(r, vf, p);
+    add_values<1>(r, vf, p);
+}
+// The weights 2^(scale x - m), rounded to bf16 for the product (2^-8 of each at most), and their sum in 32 bits.  (The sum by two-element dot products
+// halves its instructions, but these wait for the matrix pipe: a product with two of them takes 53 cycles instead of 32.)
+template <int FROM = 0, int TO = 16>
+__device__ __forceinline__ float weigh(float m, const f32x16& x, float scale_log2e, TreeWeights& p) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = FROM; i < TO; ++i) {
+        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], scale_log2e, -m));
+        p.f[i >> 3][i & 7] = (__bf16)w;
+        sum += w;
     }
-    if (EDGE) {
+    return sum;
+}
+// A row's reference m follows its scores only when their weights have outgrown 2^8 (they are held in 32 bits until they are rounded relative to
+// themselves, so that nothing is lost up to there): the weights' sum, which is needed anyway, tells, and no maximum is taken otherwise.
+// From LOWEST, any score does.  NaN scores come here at every step.
+constexpr float TREE_RAISE = 256.0f;
+__device__ __forceinline__ void raise_and_weigh(TreeRow& r, const f32x16& x, float scale_log2e, TreeWeights& p, float sum) {
+    if (__any(!(sum <= TREE_RAISE))) {
+        float mx = x[0];
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (!(allowed >> (8 * (i >> 2) + 4 * half + (i & 3)) & 1)) x[i] = -INFINITY;
-    }
-    float mx = x[0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, x[i]);
-    mx = other_half_max(mx) * scale_log2e;
-    const bool raise = mx > r.m + 8.0f;
-    if (__any(raise)) {
-        const float to = raise ? mx : r.m, f = exp2f(r.m - to);  // a row's sums do not depend on its neighbours
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, x[i]);
+        mx = other_half_max(mx) * scale_log2e;
+        // a row's sums do not depend on its neighbours
+        const float grown = other_half_max(sum <= TREE_RAISE ? 0.0f : 1.0f), to = grown != 0.0f ? fmaxf(mx, r.m) : r.m, f = exp2f(r.m - to);
         r.m = to;
         r.l *= f;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) r.o[d][i] *= f;
-    }
-    bf16x8 p[2];
-    float sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], scale_log2e, -r.m));
-        sum += e;
-        p[i >> 3][i & 7] = (__bf16)e;
+        sum = weigh(to, x, scale_log2e, p);
     }
     r.l += sum;
+}
+
+// One step of a run of tiles that every row attends to as a whole: this tile's weights p from its scores x, and beside them, independent of them, the
+// next tile's scores y and the last tile's share of the output (weights p_last).  The tiles' buffers stand NEXT_K, LAST_V behind the lane's
+// addresses: a constant of the instruction, where the loop is unrolled over the buffers.
+template <int NEXT_K, int LAST_V>
+__device__ __forceinline__ void tree_step(TreeRow& r, const f32x16& x, f32x16& y, TreeWeights& p, const TreeWeights& p_last, const uint32_t (&key)[8],
+                                          const uint32_t (&value)[4], float scale_log2e) {
+    TreeKeys kf;
+    TreeValues vf;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) vf.f[k][d] = read_value(value[d] + LAST_V + 4096 * k);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) kf.f[k] = read_key(key[k] + NEXT_K);
+    __builtin_amdgcn_sched_barrier(0);
+    float sum = weigh<0, 8>(r.m, x, scale_log2e, p);              // (while the operands are on their way)
+    __builtin_amdgcn_sched_barrier(0);
+    // products and softmax in turn: in this order they issue, and neither pipe waits for the other
+    add_values<0>(r, vf, p_last);
+    sum += weigh<8, 12>(r.m, x, scale_log2e, p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 4; k < 8; ++k) kf.f[k] = read_key(key[k] + NEXT_K);   // (in the first values' registers)
+    __builtin_amdgcn_sched_barrier(0);
+    add_values<1>(r, vf, p_last);
+    sum += weigh<12, 16>(r.m, x, scale_log2e, p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    y = score(r, kf);
+    __builtin_amdgcn_sched_barrier(0);
+    raise_and_weigh(r, x, scale_log2e, p, sum);
+}
+// A tile that not every row attends to as a whole: scores of the tokens outside `allowed` (a bit each) weigh nothing.
+__device__ __forceinline__ void mask_scores(f32x16& x, uint32_t allowed, int half) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (!(allowed >> (8 * (i >> 2) + 4 * half + (i & 3)) & 1)) x[i] = -INFINITY;
+}
+// Its share of the output.  Values that are not finite must not meet the weight 0 of a row that does not attend to them: those of the tokens in `wash`,
+// which not every row attends to, are left out, and the lane's tokens with such values returned.
+__device__ __forceinline__ uint32_t add_washed(TreeRow& r, const TreeWeights& p, uint32_t vt, uint32_t wash, int lane) {
+    const int half = lane >> 5;
     uint32_t odd = 0;
-    const uint32_t wash = ~common >> (4 * half);
+    wash >>= 4 * half;
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
-            if (EDGE) {
-                u32x4 v = __builtin_bit_cast(u32x4, values(k, d));
+            u32x4 v = __builtin_bit_cast(u32x4, read_value(vt + 4096 * k + value_at(lane, d)));
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {                     // two tokens a word
-                    const uint32_t at = 1u << (16 * k + 2 * (j & 1) + 8 * (j >> 1));
-                    if ((v[j] & 0x7f80u) == 0x7f80u && (wash & at)) {
-                        odd |= at;
-                        v[j] &= 0xffff0000u;
-                    }
-                    if ((v[j] & 0x7f800000u) == 0x7f800000u && (wash & at << 1)) {
-                        odd |= at << 1;
-                        v[j] &= 0xffffu;
-                    }
+            for (int j = 0; j < 4; ++j) {                         // two tokens a word
+                const uint32_t at = 1u << (16 * k + 2 * (j & 1) + 8 * (j >> 1));
+                if ((v[j] & 0x7f80u) == 0x7f80u && (wash & at)) {
+                    odd |= at;
+                    v[j] &= 0xffff0000u;
                 }
-                vf[k][d] = __builtin_bit_cast(s16x8, v);
-                asm volatile("" ::: "memory");                    // one operand at a time: no registers for more
+                if ((v[j] & 0x7f800000u) == 0x7f800000u && (wash & at << 1)) {
+                    odd |= at << 1;
+                    v[j] &= 0xffffu;
+                }
             }
-            r.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[k][d]), p[k], r.o[d], 0, 0, 0);
+            asm volatile("" ::: "memory");                        // one operand at a time: no registers for more
+            r.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), p.f[k], r.o[d], 0, 0, 0);
         }
-    odd <<= 4 * half;
-    return odd;
+    return odd << (4 * half);
 }
 
 // A workgroup's rows against tokens [begin, end).  RG waves share a token tile and split the rows; 8 / RG such teams split the tokens and are added up in
-// LDS at the end.  Two waves to a SIMD: one's softmax runs beside the other's products.  Tiles come by loads from memory straight to LDS, several of
-// them under way.
+// LDS at the end.  Two waves to a SIMD.  Tiles come by loads from memory straight to LDS, several of them under way.
 template <int RG, bool PAGED, bool SPARSE>
-__device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, TreeLds& lds, int b, int kvh, int row0, int begin, int end) {
+__device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, TreeLds& lds, int b, int kvh, int row0, int split, int begin, int end) {
     constexpr int TEAMS = TREE_WAVES / RG;
-    constexpr int SUB = RG == 8 ? 2 : 1, TT = 32 * SUB;           // tokens of a team's tile
+    constexpr int TT = TREE_TILE;                                 // tokens of a team's tile
     constexpr int ROWS = 32 * RG;
-    constexpr int TILE_BYTES = TT * 256;                          // of K, and again of V
-    constexpr int STAGES = TREE_RING / (TEAMS * 2 * TILE_BYTES);  // 1, 2, 4, 4
-    constexpr int AHEAD = RG == 1 ? 1 : STAGES - 1;               // tiles asked for before one is used
+    constexpr int TILE_BYTES = TT * 256;                          // of K or V
+    constexpr int STAGES = TREE_RING / 2 / (TEAMS * TILE_BYTES);  // buffers of K, and of V: as many as waves in a team
     constexpr int MINE = TT / RG;                                 // rows that a wave loads
-    constexpr int OPS = 2 * MINE / 4;                             // its loads for a tile
+    constexpr int OPS = 2 * MINE / 4;                             // its loads for a tile of K and one of V
     constexpr bool LIST = PAGED || SPARSE;
+    static_assert(TREE_LIST % (TT * TEAMS) == 0, "a full list is whole steps");
     static_assert(TEAMS * ROWS * D * 4 <= TREE_RING && TEAMS * ROWS <= TREE_ROWS && MINE % 4 == 0, "the teams' sums take the tiles' place");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int team = wave / RG, mine = wave % RG, half = lane >> 5, col = lane & 31;
@@ -524,14 +652,14 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
 
     TreeRow row;
     const int my_row = row0 + mine * 32 + col;
-    const bool mine_there = my_row < rows;
-    const int node = mine_there ? my_row >> a.g_shift : 0;
+    const bool there = my_row < rows;
+    const int node = there ? my_row >> a.g_shift : 0;
     {
         const uint16_t* p = a.q + (int64_t)(s.start + node) * a.q_stride + ((kvh << a.g_shift) + (my_row & (g - 1))) * D + half * 8;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             u32x4 v = *reinterpret_cast<const u32x4*>(p + k * 16);
-            if (!mine_there) v = u32x4{0, 0, 0, 0};
+            if (!there) v = u32x4{0, 0, 0, 0};
             row.q[k] = __builtin_bit_cast(bf16x8, v);
         }
     }
@@ -546,121 +674,295 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds.ring;
     const uint16_t* const kbase = a.cache.kv.k + (PAGED ? 0 : (int64_t)b * a.cache.kv.sb + (int64_t)kvh * a.cache.kv.sh);
     const uint16_t* const vbase = a.cache.kv.v + (PAGED ? 0 : (int64_t)b * a.cache.kv.sb + (int64_t)kvh * a.cache.kv.sh);
-    const int64_t stride = PAGED ? D : a.cache.kv.st;
+    const uint32_t stride = PAGED ? D : (uint32_t)a.cache.kv.st;   // (below 2^31: the host checks)
     // A lane's part of a row, in the order in which LDS holds it: K's 16-byte chunk c of row r stands at c ^ (r & 15), V's at c ^ (4 (r & 3)), so
     // that neither the rows of an operand nor the transposing reads meet in a bank.
-    const int lr = lane >> 4, vchunk = (lane & 15) ^ (lr << 2), koff = ((lane & 15) ^ ((mine * MINE + lr) & 15)) << 3;
-    const int64_t lane_off = (mine * MINE + lr) * stride;
+    const int lr = lane >> 4, vchunk = ((lane & 15) ^ (lr << 2)) << 3, kchunk = ((lane & 15) ^ ((mine * MINE + lr) & 15)) << 3;
+    const uint64_t lane_off = (uint64_t)(uint32_t)(mine * MINE + lr) * stride;
 
-    for (int c0 = begin; c0 < end;) {                             // as many tokens as the list has room for
-        const int c1 = LIST ? min(end, c0 + (SPARSE ? TREE_LIST : TREE_LIST * PAGE)) : end;
-        const int steps = (c1 - c0 + TT * TEAMS - 1) / (TT * TEAMS);
-        bool good = true;
-        if (LIST) {
-            const int entries = SPARSE ? min(steps * TT * TEAMS, TREE_LIST) : (c1 - c0 + PAGE - 1) / PAGE;
-            bool bad = false;
-            for (int e = tid; e < entries; e += TREE_THREADS) {
-                int at = -1;
-                if (SPARSE) {
-                    const int i = c0 + e;
-                    if (i < c1) {
-                        const int pos = i < s.pre ? a.idx[(int64_t)b * a.budget + i] : s.before + (i - s.pre);
-                        if (i >= s.pre || (uint32_t)pos < (uint32_t)s.before) at = cache_row<PAGED>(a.cache, b, kvh, pos);
-                        bad |= at < 0;
-                    }
-                } else {
-                    at = cache_row<PAGED>(a.cache, b, kvh, c0 + e * PAGE);
+    const int steps = (end - begin + TT * TEAMS - 1) / (TT * TEAMS);
+    const bool once = a.m_tiles == 1;
+    bool good = true;
+    if (LIST) {
+        const int entries = SPARSE ? steps * TT * TEAMS : (end - begin + PAGE - 1) / PAGE;
+        bool bad = false;
+        for (int e = tid; e < entries; e += TREE_THREADS) {
+            int at = -1;
+            if (SPARSE) {
+                const int i = begin + e;
+                if (i < end) {
+                    const int pos = i < s.pre ? a.idx[(int64_t)b * a.budget + i] : s.before + (i - s.pre);
+                    if (i >= s.pre || (uint32_t)pos < (uint32_t)s.before) at = cache_row<PAGED>(a.cache, b, kvh, pos);
                     bad |= at < 0;
                 }
-                lds.list[e] = at;
+            } else {
+                at = cache_row<PAGED>(a.cache, b, kvh, begin + e * PAGE);
+                bad |= at < 0;
             }
-            good = !__syncthreads_or(bad);
+            lds.list[e] = at;
         }
-        auto request = [&](int it) {
-            const int t = c0 + (it * TEAMS + team) * TT, r0 = mine * MINE;
-            const uint32_t kt = ring + ((it % STAGES) * TEAMS + team) * (2 * TILE_BYTES) + r0 * 256, vt = kt + TILE_BYTES;
+        good = !__syncthreads_or(bad);
+    }
+    auto k_at = [&](int it) { return ((it % STAGES) * TEAMS + team) * TILE_BYTES; };
+    auto v_at = [&](int it) { return TREE_RING / 2 + ((it % STAGES) * TEAMS + team) * TILE_BYTES; };
+    auto request = [&](int it, bool values) {
+        const int t = begin + (it * TEAMS + team) * TT, r0 = mine * MINE;
+        const uint32_t to = ring + (values ? v_at(it) : k_at(it)) + r0 * 256;
+        int chunk = values ? vchunk : kchunk;
+        asm volatile("" : "+v"(chunk));                           // else every row's address parts are kept in registers all along
 #pragma unroll
-            for (int n = 0; n < MINE / 4; ++n) {
-                const int r = n * 4 + lr;                         // (K's chunks are turned by r0 + r: koff)
-                int64_t off;
-                if (SPARSE) {
-                    off = (int64_t)max(lds.list[min(t - c0 + r0 + r, TREE_LIST - 1)], 0) * stride;
-                } else if (PAGED) {
-                    // a wave's rows of a tile share pages of 16; behind the list's last entry row 0 has to do
-                    const int page = (t - c0 + r0 + n * 4) >> 4;
-                    off = (int64_t)((t + r0 + n * 4 < c1 ? max(lds.list[page], 0) : 0) + ((r0 + n * 4) & (PAGE - 1)) + lr) * D;
-                } else {
-                    off = t + TT <= end ? (t + n * 4) * stride + lane_off : min(t + r0 + r, end - 1) * stride;
-                }
-                load_to_lds(kbase + off + (koff ^ ((n * 4 & 15) << 3)), kt + n * 1024);
-                load_to_lds(vbase + off + (vchunk << 3), vt + n * 1024);
+        for (int n = 0; n < MINE / 4; ++n) {
+            const int r = n * 4 + lr;                             // (K's chunks are turned by r0 + r: kchunk)
+            int64_t off;
+            if (SPARSE) {
+                off = (int64_t)((uint64_t)(uint32_t)max(lds.list[t - begin + r0 + r], 0) * stride);
+            } else if (PAGED) {
+                // a wave's rows of a tile share pages of 16; behind the list's last entry row 0 has to do
+                const int page = (t - begin + r0 + n * 4) >> 4;
+                off = (int64_t)((t + r0 + n * 4 < end ? max(lds.list[page], 0) : 0) + ((r0 + n * 4) & (PAGE - 1)) + lr) * D;
+            } else {
+                off = (int64_t)(t + TT <= end ? (uint64_t)(uint32_t)(t + n * 4) * stride + lane_off : (uint64_t)(uint32_t)min(t + r0 + r, end - 1) * stride);
+            }
+            load_to_lds((values ? vbase : kbase) + off + (values ? chunk : chunk ^ ((n * 4 & 15) << 3)), to + n * 1024, once);
+        }
+    };
+    // Which tokens of tile `it` are there, and which of them this wave's rows attend to (`common`: all of them).
+    auto attended = [&](int it, uint32_t& there, uint32_t& common) -> uint32_t {
+        const int t = begin + (it * TEAMS + team) * TT;
+        there = t + 32 <= end ? 0xffffffffu : t >= end ? 0u : (1u << (end - t)) - 1;
+        if (LIST && !good) there = (uint32_t)__ballot(t + col < end && lds.list[SPARSE ? t - begin + col : (t - begin + col) >> 4] >= 0);
+        const int from = s.pre - t;                               // tokens of the prefix in this step
+        const uint32_t prefix = from >= 32 ? 0xffffffffu : from <= 0 ? 0u : (1u << from) - 1;
+        common = prefix & there;
+        return (prefix | mask_window(a.masks + (int64_t)(s.start + node) * a.words, a.words, t - s.pre)) & there;
+    };
+    auto note_odd = [&](int it, uint32_t odd) {                   // nodes with values that were left out
+        const int t = begin + (it * TEAMS + team) * TT;
+        for (; odd; odd &= odd - 1) {
+            const int i = t + __builtin_ctz(odd) - s.pre;
+            atomicOr(&lds.odd[i >> 5], 1u << (i & 31));
+        }
+    };
+    const int plain = good ? max(0, min(s.pre, end) - begin) / (TT * TEAMS) : 0;   // tiles that every row attends to as a whole: the first ones
+    if constexpr (RG < 4) {
+        // Few rows: the products are short, and what counts is that tiles keep coming.  A tile is a step.  A wave on its own asks for the next when it
+        // has read one, while seven others are elsewhere; a team of two has a second buffer for it.
+        auto request_tile = [&](int n) {
+            if (n < steps) {
+                request(n, false);
+                request(n, true);
             }
         };
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-            if (i < steps) request(i);
-        auto arrive = [&](int it) {                               // tile `it` is there, for the team
-            wait_tiles<OPS>(min(steps - 1 - it, AHEAD - 1));
+        auto arrive = [&](int it) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             if (RG > 1) {
                 wave_barrier();
-                if (it + AHEAD < steps) request(it + AHEAD);
+                request_tile(it + 1);
             }
         };
         auto leave = [&](int it) {
-            if (RG == 1 && it + AHEAD < steps) {
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the buffer's last reads
-                request(it + AHEAD);
+            if (RG == 1) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the buffers' last reads
+                request_tile(it + 1);
             }
         };
-        auto tile_of = [&](int it) -> const unsigned char* { return lds.ring + ((it % STAGES) * TEAMS + team) * (2 * TILE_BYTES); };
-        // Tiles that every row attends to as a whole, then the others.  (In one loop the two forms' registers got in each other's way.)
-        const int plain = good ? max(0, min(s.pre, c1) - c0) / (TT * TEAMS) : 0;
+        request_tile(0);
+        int it = 0;
+        // (Two loops: in one, the two forms' registers get in each other's way.)
 #pragma unroll 1
-        for (int it = 0; it < plain; ++it) {
+        for (; it < plain; ++it) {
             arrive(it);
-            const unsigned char* const kt = tile_of(it);
             if (!idle) {
-#pragma unroll 1
-                for (int sub = 0; sub < SUB; ++sub) tree_step<false>(row, kt + sub * 8192, kt + TILE_BYTES + sub * 8192, 0, 0, a.scale_log2e, lane);
+                TreeKeys kf;
+                TreeValues vf;
+                TreeWeights p;
+                read_keys(kf, ring + k_at(it), lane);
+                f32x16 x = score(row, kf);
+                read_values(vf, ring + v_at(it), lane);
+                const float sum = weigh(row.m, x, a.scale_log2e, p);
+                raise_and_weigh(row, x, a.scale_log2e, p, sum);
+                add_values(row, vf, p);
             }
             leave(it);
         }
 #pragma unroll 1
-        for (int it = plain; it < steps; ++it) {
+        for (; it < steps; ++it) {
             arrive(it);
-            const unsigned char* const kt = tile_of(it);
-#pragma unroll 1
-            for (int sub = 0; sub < SUB; ++sub) {
-                const int t = c0 + (it * TEAMS + team) * TT + 32 * sub;
-                uint32_t there = t + 32 <= c1 ? 0xffffffffu : t >= c1 ? 0u : (1u << (c1 - t)) - 1;
-                if (LIST && !good) {
-                    const int i = t - c0 + col;
-                    there = (uint32_t)__ballot(t + col < c1 && lds.list[SPARSE ? i : i >> 4] >= 0);
-                }
-                if (there == 0 || idle) continue;
-                const int from = s.pre - t;                       // tokens of the prefix in this step
-                const uint32_t prefix = from >= 32 ? 0xffffffffu : from <= 0 ? 0u : (1u << from) - 1;
-                const uint32_t own = mask_window(a.masks + (int64_t)(s.start + node) * a.words, a.words, t - s.pre);
-                uint32_t odd = tree_step<true>(row, kt + sub * 8192, kt + TILE_BYTES + sub * 8192, (prefix | own) & there, prefix & there, a.scale_log2e, lane);
-                for (odd &= there; odd; odd &= odd - 1) {         // nodes (what is not there stays away)
-                    const int i = t + __builtin_ctz(odd) - s.pre;
-                    atomicOr(&lds.odd[i >> 5], 1u << (i & 31));
-                }
+            uint32_t there, common;
+            const uint32_t allowed = attended(it, there, common);
+            if (!idle && there != 0) {
+                TreeKeys kf;
+                TreeWeights p;
+                read_keys(kf, ring + k_at(it), lane);
+                f32x16 x = score(row, kf);
+                mask_scores(x, allowed, half);
+                const float sum = weigh(row.m, x, a.scale_log2e, p);
+                raise_and_weigh(row, x, a.scale_log2e, p, sum);
+                note_odd(it, add_washed(row, p, ring + v_at(it), ~common, lane) & there);
             }
             leave(it);
         }
-        c0 = c1;
-        if (LIST && c0 < end) __syncthreads();                    // before the list's next entries, and the ring's first tiles
+    } else {
+        // Step `it` takes tile it's weights, the next tile's scores and the last tile's share of the output: it needs K of tile it + 1 and V of tile
+        // it - 1.  After the first two K, V of tile n and K of tile n + 2 are asked for together, as pair n, for step n + 1; a block of half
+        // the buffers at a time: while the team works on one, the next is under way.  The waves meet once a block only: in between, one of a SIMD's two
+        // is ahead, at its softmax while the other has the products.  (Meeting at every step, both wait for the same pipe: 2030 cycles a step of 256 rows,
+        // of which the products are 1024.)
+        constexpr int BLOCK = STAGES / 2;
+        auto request_pair = [&](int n) {
+            if (n < steps) request(n, true);
+            if (n + 2 < steps) request(n + 2, false);
+        };
+        const int full = (end - begin) / (TT * TEAMS);            // whole tiles
+        uint32_t part_k[MINE / 4], part_v[MINE / 4];              // the lane's part of a row's address
+#pragma unroll
+        for (int i = 0; i < MINE / 4; ++i) {
+            const uint32_t at = SPARSE ? 0 : ((PAGED ? (mine * MINE) & (PAGE - 1) : 0) + i * 4 + lr) * stride;
+            part_k[i] = (at + (kchunk ^ ((i * 4 & 15) << 3))) * 2;
+            part_v[i] = (at + vchunk) * 2;
+        }
+        // Pairs n .. n + BLOCK - 1.  Whole tiles of a whole prefix: the rows of a wave's part are one after the other, in a page or in the sequence, and a
+        // uniform address serves.  Of a chosen prefix each lane has its own; the list's entries come all at once.
+        auto request_block = [&](int n) {
+            if (!good || n + BLOCK + 2 > full) {
+#pragma unroll
+                for (int j = 0; j < BLOCK; ++j) request_pair(n + j);
+                return;
+            }
+            const int t = (n * TEAMS + team) * TT + mine * MINE;  // the wave's first row of tile n
+            int entry[BLOCK + 2][SPARSE ? MINE / 4 : 1];
+            if (LIST) {
+#pragma unroll
+                for (int j = 0; j < BLOCK + 2; ++j)
+#pragma unroll
+                    for (int i = 0; i < (SPARSE ? MINE / 4 : 1); ++i)
+                        entry[j][i] = lds.list[SPARSE ? t + j * (TEAMS * TT) + i * 4 + lr : (t + j * (TEAMS * TT)) >> 4];
+            }
+            auto row_at = [&](int j) {                            // the first of the wave's rows of tile n + j, in elements
+                if (PAGED) return (int64_t)__builtin_amdgcn_readfirstlane(entry[j][0]) * D;
+                return (int64_t)((uint64_t)(uint32_t)(begin + t + j * (TEAMS * TT)) * stride);
+            };
+#pragma unroll
+            for (int j = 0; j < BLOCK; ++j) {
+                const uint32_t kt = ring + k_at(n + j + 2) + mine * MINE * 256, vt = ring + v_at(n + j) + mine * MINE * 256;
+                if constexpr (SPARSE) {
+#pragma unroll
+                    for (int i = 0; i < MINE / 4; ++i) {
+                        load_to_lds(vbase + (uint64_t)(uint32_t)entry[j][i] * stride + part_v[i] / 2, vt + i * 1024, once);
+                        load_to_lds(kbase + (uint64_t)(uint32_t)entry[j + 2][i] * stride + part_k[i] / 2, kt + i * 1024, once);
+                    }
+                } else {
+                    const uint16_t *v = vbase + row_at(j), *k = kbase + row_at(j + 2);
+#pragma unroll
+                    for (int i = 0; i < MINE / 4; ++i) {
+                        load_to_lds(v, part_v[i], vt + i * 1024, once);
+                        load_to_lds(k, part_k[i], kt + i * 1024, once);
+                    }
+                }
+            }
+        };
+        // Before the first step of a block (it - 1 a multiple of BLOCK): its pairs have arrived, for the whole team, and what the last block read is free.
+        auto begin_block = [&](int it) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            wave_barrier();
+            request_block(it - 1 + BLOCK);
+        };
+        request(0, false);
+        if (steps > 1) request(1, false);
+#pragma unroll
+        for (int n = 0; n < BLOCK; ++n) request_pair(n);
+        wait_tiles<OPS, BLOCK>(steps - 2);                        // (pairs without K do not count as under way)
+        wave_barrier();
+        f32x16 x;
+        TreeWeights p;
+        uint32_t there = 0xffffffffu, common = 0xffffffffu;       // of the tile that p belongs to
+        int it = 0;
+        if (!idle) {
+            TreeKeys kf;
+            read_keys(kf, ring + k_at(0), lane);
+            x = score(row, kf);
+        }
+        // One step, by dynamic addresses: the first, those of a broken block, and where rows attend to parts of a tile.
+        auto any_step = [&]() {
+            if (it > 0) {
+                if (common == 0xffffffffu) {
+                    TreeValues vf;
+                    read_values(vf, ring + v_at(it - 1), lane);
+                    add_values(row, vf, p);
+                } else if (there != 0) {
+                    note_odd(it - 1, add_washed(row, p, ring + v_at(it - 1), ~common, lane) & there);
+                }
+            }
+            if (it >= steps) return;
+            there = common = 0xffffffffu;
+            if (it >= plain) mask_scores(x, attended(it, there, common), half);
+            const float sum = weigh(row.m, x, a.scale_log2e, p);
+            raise_and_weigh(row, x, a.scale_log2e, p, sum);
+            if (it + 1 < steps) {
+                TreeKeys kf;
+                read_keys(kf, ring + k_at(it + 1), lane);
+                x = score(row, kf);
+            }
+        };
+        if (!idle) any_step();
+        it = 1;
+        {
+            // Whole blocks, unrolled: the buffers' places are constants of the instructions then, and two steps' registers change places.
+            static_assert(BLOCK == 2 || BLOCK == 4, "the loop's steps");
+            uint32_t key[8], value[4];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) key[k] = ring + k_at(0) + key_at(lane, k);
+#pragma unroll
+            for (int d = 0; d < 4; ++d) value[d] = ring + v_at(0) + value_at(lane, d);
+            constexpr int NEXT = TEAMS * TILE_BYTES;              // bytes from one buffer of a team to the next
+            f32x16 y;
+            TreeWeights p2;
+            // The buffers' two halves take turns: K goes over to the other in the middle of a block (it is two tiles ahead), V between blocks.
+            int k_other = BLOCK * NEXT, v_other = BLOCK * NEXT;
+            auto step = [&](auto place) {                         // it = 1 + place, mod BLOCK
+                constexpr int J = decltype(place)::value;
+                if (J == 0) begin_block(it);
+                if (J + 2 == BLOCK) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) key[k] += k_other;
+                    k_other = -k_other;
+                }
+                constexpr int K = (J + 2) % BLOCK * NEXT, V = J * NEXT;
+                if (!idle) {
+                    if (J & 1) tree_step<K, V>(row, y, x, p, p2, key, value, a.scale_log2e);
+                    else tree_step<K, V>(row, x, y, p2, p, key, value, a.scale_log2e);
+                }
+                if (J + 1 == BLOCK) {
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) value[d] += v_other;
+                    v_other = -v_other;
+                }
+                ++it;
+            };
+            const int until = min(plain, steps - 1);              // (a step makes the next tile's scores)
+#pragma unroll 1
+            while (it + BLOCK <= until) {
+                step(std::integral_constant<int, 0>());
+                step(std::integral_constant<int, 1>());
+                if constexpr (BLOCK == 4) {
+                    step(std::integral_constant<int, 2>());
+                    step(std::integral_constant<int, 3>());
+                }
+            }
+        }
+#pragma unroll 1
+        for (; it <= steps; ++it) {                               // (the last: only the last tile's share)
+            if ((it - 1) % BLOCK == 0) begin_block(it);
+            if (!idle) any_step();
+        }
     }
 
     // The teams' sums, brought to a common maximum, meet in LDS and leave it row by row.
     row.l += __shfl_xor(row.l, 32);
-    {
+    if (half == 0) {
         const int r = team * ROWS + mine * 32 + col;
-        if (half == 0) {
-            lds.m[r] = row.m;
-            lds.l[r] = row.l;
-        }
+        lds.m[r] = row.m;
+        lds.l[r] = row.l;
     }
     __syncthreads();
     {
@@ -717,7 +1019,7 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
                              (uint32_t)f32_to_bf16_rne(v[2] * inv) | (uint32_t)f32_to_bf16_rne(v[3] * inv) << 16};
             *reinterpret_cast<u32x2*>(a.out + to * D + c * 4) = w;
         } else {
-            const int64_t piece = to * a.n_splits + blockIdx.x;
+            const int64_t piece = to * a.n_splits + split;
             *reinterpret_cast<f32x4*>(a.part_acc + piece * D + c * 4) = v;
             if (c == 0) *reinterpret_cast<f32x2*>(a.part_ml + piece * 2) = f32x2{top, sum};
         }
@@ -728,49 +1030,72 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
 template <bool PAGED, bool SPARSE>
 __global__ __launch_bounds__(TREE_THREADS, 2) void tree_attn_kernel(TreeArgs a) {
     __shared__ TreeLds lds;
-    const int b = blockIdx.z, kvh = blockIdx.y / a.m_tiles, row0 = (blockIdx.y % a.m_tiles) * TREE_ROWS;
-    const TreeSpan s = tree_work<SPARSE>(a, b, TREE_UNIT);
+    // Workgroups go to the 8 XCDs in turn: those that share a KV head's tokens come 8 apart, to the same L2.  First pieces first: behind them come
+    // those that short sequences do not have.
+    const uint32_t turn = blockIdx.x >> 3, m_tile = turn % (uint32_t)a.m_tiles, unit = turn / (uint32_t)a.m_tiles * 8 + (blockIdx.x & 7);
+    const uint32_t G = a.cache.kv.G, pairs = G * (uint32_t)a.batch, pair = unit % pairs;
+    const int split = unit / pairs, b = pair / G, kvh = pair - b * G, row0 = m_tile * TREE_ROWS;
+    if (split >= a.n_splits) return;
+    const TreeSpan s = tree_work<SPARSE>(a, b);
     const int left = (s.n << a.g_shift) - row0;
-    const int begin = blockIdx.x * s.chunk;
+    const int begin = split * s.chunk;
     if (left <= 0 || begin >= s.all) return;
+    // (a piece has no more tokens or pages than the list has room for: plan_tree)
     const int end = min(begin + s.chunk, s.all);
-    if (left <= 32) tree_rows<1, PAGED, SPARSE>(a, s, lds, b, kvh, row0, begin, end);
-    else if (left <= 64) tree_rows<2, PAGED, SPARSE>(a, s, lds, b, kvh, row0, begin, end);
-    else if (left <= 128) tree_rows<4, PAGED, SPARSE>(a, s, lds, b, kvh, row0, begin, end);
-    else tree_rows<8, PAGED, SPARSE>(a, s, lds, b, kvh, row0, begin, end);
+    if (a.n_splits > 1 && split == 0 && kvh == 0 && m_tile == 0 && threadIdx.x == 0) a.pieces[b] = (s.all + s.chunk - 1) / s.chunk;
+    if (left <= 32) tree_rows<1, PAGED, SPARSE>(a, s, lds, b, kvh, row0, split, begin, end);
+    else if (left <= 64) tree_rows<2, PAGED, SPARSE>(a, s, lds, b, kvh, row0, split, begin, end);
+    else if (left <= 128) tree_rows<4, PAGED, SPARSE>(a, s, lds, b, kvh, row0, split, begin, end);
+    else tree_rows<8, PAGED, SPARSE>(a, s, lds, b, kvh, row0, split, begin, end);
 }
 
 // A wave for a row: a lane for each piece's weight, then two columns a lane.
-template <bool SPARSE>
-__global__ __launch_bounds__(256) void tree_reduce_kernel(TreeArgs a) {
+constexpr int REDUCE_WAVES = 4;
+__global__ __launch_bounds__(64 * REDUCE_WAVES) void tree_reduce_kernel(TreeArgs a) {
     const int lane = threadIdx.x & 63, b = blockIdx.y;
-    const TreeSpan s = tree_work<SPARSE>(a, b, TREE_UNIT);
-    const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (s.chunk >= s.all || r >= s.n * a.H) return;
-    const int pieces = (s.all + s.chunk - 1) / s.chunk;
-    const int64_t row = (int64_t)s.start * a.H + r, first = row * a.n_splits;
-    float m = LOWEST, l = 0.0f;
-    if (lane < pieces) {
-        const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + (first + lane) * 2);
-        m = ml[0];
-        l = ml[1];
-    }
-    float top = m;
+    int start;
+    const int n = min(tree_span(a.tok_start, b, a.max_tokens, a.max_nodes, start), clampi(a.cache.kv.seq_lens[b], 0, a.cache.max_len));
+    if (n == 0) return;                                           // (without a node, nobody has written how many pieces there are)
+    const int pieces = a.pieces[b];
+    if (pieces <= 1) return;
+    for (int r = blockIdx.x * REDUCE_WAVES + (threadIdx.x >> 6); r < n * a.H; r += gridDim.x * REDUCE_WAVES) {
+        const int64_t row = (int64_t)start * a.H + r, first = row * a.n_splits;
+        float m = LOWEST, l = 0.0f;
+        if (lane < pieces) {
+            const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + (first + lane) * 2);
+            m = ml[0];
+            l = ml[1];
+        }
+        float top = m;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const float w = exp2f(m - top);
-    float sum = lane < pieces ? w * l : 0.0f;
+        for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+        const float w = exp2f(m - top);
+        float sum = lane < pieces ? w * l : 0.0f;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-    f32x2 acc = {0.0f, 0.0f};
-    for (int p = 0; p < pieces; ++p) {
-        const f32x2 v = *reinterpret_cast<const f32x2*>(a.part_acc + (first + p) * D + lane * 2);
-        const float wp = __shfl(w, p);
-        acc[0] += wp * v[0];
-        acc[1] += wp * v[1];
+        for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+        f32x2 acc = {0.0f, 0.0f};
+        const float* part = a.part_acc + first * D + lane * 2;
+        int p = 0;
+        for (; p + 8 <= pieces; p += 8) {                         // eight at a time under way
+            f32x2 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const f32x2*>(part + (p + i) * D);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float wp = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), p + i));
+                acc[0] += wp * v[i][0];
+                acc[1] += wp * v[i][1];
+            }
+        }
+        for (; p < pieces; ++p) {
+            const f32x2 v = *reinterpret_cast<const f32x2*>(part + p * D);
+            const float wp = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), p));
+            acc[0] += wp * v[0];
+            acc[1] += wp * v[1];
+        }
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        *reinterpret_cast<uint32_t*>(a.out + row * D + lane * 2) = (uint32_t)f32_to_bf16_rne(acc[0] * inv) | (uint32_t)f32_to_bf16_rne(acc[1] * inv) << 16;
     }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    *reinterpret_cast<uint32_t*>(a.out + row * D + lane * 2) = (uint32_t)f32_to_bf16_rne(acc[0] * inv) | (uint32_t)f32_to_bf16_rne(acc[1] * inv) << 16;
 }
 
 // ---------------------------------------------------------------- commit

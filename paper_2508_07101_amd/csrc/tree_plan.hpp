@@ -10,35 +10,45 @@ namespace cusa {
 constexpr int TREE_MAX_NODES = 256;
 constexpr int TREE_MAX_SPLITS = 64;     // pieces of a sequence's tokens: one lane each in the merge
 constexpr int TREE_MIN_PIECE = 256;     // tokens
-constexpr int TREE_CUS = 256;
+constexpr int TREE_CUS = 256;           // with a workgroup each at a time
+constexpr int TREE_PIECE_COST = 16;     // tiles of 32 tokens that a piece costs besides its own
 
 constexpr int TREE_ROWS = 256;          // rows (node, query head) of one KV head that a workgroup holds at most
+
+// Entries of a workgroup's list of cache rows: tokens of a chosen prefix, pages of 16 of a whole one.
+constexpr int TREE_LIST = 5120;
+enum TreeKind { TREE_FULL, TREE_CHOSEN };
+inline int tree_piece_most(TreeKind kind) { return kind == TREE_CHOSEN ? TREE_LIST : TREE_LIST * 16; }
+inline bool tree_len_served(TreeKind kind, int64_t len) { return len <= (int64_t)tree_piece_most(kind) * TREE_MAX_SPLITS; }
 
 struct TreePlan {
     int m_tiles;     // workgroups that share a KV head's tokens
     int n_splits;    // pieces of a sequence's tokens at most; the kernel makes fewer of a short one
 };
 
-inline TreePlan plan_tree(int max_len, int pairs, int g, int max_nodes) {
+inline TreePlan plan_tree(TreeKind kind, int max_len, int batch, int G, int g, int max_nodes) {
+    const int pairs = batch * G;
     TreePlan p;
     p.m_tiles = (max_nodes * g + TREE_ROWS - 1) / TREE_ROWS;
-    const int64_t wgs = (int64_t)pairs * p.m_tiles;
-    const int64_t by_len = ((int64_t)max_len + TREE_MIN_PIECE - 1) / TREE_MIN_PIECE;
-    p.n_splits = (int)std::max<int64_t>(1, std::min<int64_t>({TREE_CUS / wgs, by_len, (int64_t)TREE_MAX_SPLITS}));
+    // One sequence: a piece for each CU.  Several: room for as many as make up for their lengths' differences (64 of 8192 to 32768 tokens, 8 KV heads:
+    // pieces of the longest alone 1437 us, see tree_work).
+    const int64_t wgs = (int64_t)pairs * p.m_tiles, want = batch == 1 ? TREE_CUS / wgs : wgs >= 8 * TREE_CUS ? 1 : std::max<int64_t>(4, 4 * TREE_CUS / wgs);
+    const int64_t by_len = ((int64_t)max_len + TREE_MIN_PIECE - 1) / TREE_MIN_PIECE, by_list = ((int64_t)max_len + tree_piece_most(kind) - 1) / tree_piece_most(kind);
+    p.n_splits = (int)std::max<int64_t>({1, by_list, std::min<int64_t>({want, by_len, (int64_t)TREE_MAX_SPLITS})});
     return p;
 }
 
 // Bytes of partial results: 128 sums, a maximum and a denominator per row and piece.  Trees of fewer nodes may be cut into more
 // pieces, but have fewer rows: the bound is over all of them, so that a workspace serves every smaller batch of tokens as well.
 struct TreeWs {
-    size_t acc, ml, total;
+    size_t acc, ml, pieces, total;
 };
-inline TreeWs tree_workspace(int max_len, int batch, int H, int G, int max_tokens, int max_nodes) {
+inline TreeWs tree_workspace(TreeKind kind, int max_len, int batch, int H, int G, int max_tokens, int max_nodes) {
     const int g = H / G;
     size_t worst = 0;
     for (int tiles = 1;; ++tiles) {
         const int nodes = std::min(max_nodes, tiles * TREE_ROWS / g);
-        const TreePlan p = plan_tree(max_len, batch * G, g, nodes);
+        const TreePlan p = plan_tree(kind, max_len, batch, G, g, nodes);
         const size_t tokens = (size_t)std::min<int64_t>(max_tokens, (int64_t)batch * nodes);
         if (p.n_splits > 1) worst = std::max(worst, tokens * H * p.n_splits);
         if (nodes == max_nodes) break;
@@ -46,7 +56,8 @@ inline TreeWs tree_workspace(int max_len, int batch, int H, int G, int max_token
     TreeWs w;
     w.acc = 0;
     w.ml = (worst * 128 * 4 + 255) / 256 * 256;
-    w.total = w.ml + (worst * 2 * 4 + 255) / 256 * 256 + 256;
+    w.pieces = w.ml + (worst * 2 * 4 + 255) / 256 * 256;
+    w.total = w.pieces + ((size_t)batch * 4 + 255) / 256 * 256;
     return w;
 }
 
