@@ -219,9 +219,9 @@ cusa_status cusa_tree_attn(const cusa_params* params, const void* q, const cusa_
     a.m_tiles = pl.m_tiles;
     a.n_splits = pl.n_splits;
     a.batch = params->batch;
-    const int64_t units = ((int64_t)pl.n_splits * G * params->batch + 7) / 8 * 8;
-    if (units * pl.m_tiles > 0x7fffffff) return CUSA_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)(units * pl.m_tiles));
+    const int64_t units = ((int64_t)pl.n_splits * G * params->batch + 7) / 8 * 8 * pl.m_tiles;
+    if (units > 0x7fffffff) return CUSA_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)units);
     const bool paged = kv->layout == CUSA_KV_PAGED;
     hipStream_t s = static_cast<hipStream_t>(stream);
     launch_tree(paged, grid, s, a);

@@ -360,44 +360,55 @@ __device__ __forceinline__ int tiles_of(int tokens) { return (tokens + TREE_TILE
 // the first is exact for sequences of one length, the second close for any.  R: one to eight workgroups for each CU; more are better balanced, but
 // each costs about TREE_PIECE_COST tiles besides its own (its start, and partial sums written and read).
 template <bool SPARSE>
-__device__ __forceinline__ TreeSpan tree_work(const TreeArgs& a, int b) {
-    TreeSpan s = tree_span<SPARSE>(a, b);
-    int piece = tiles_of(s.all);
-    if (a.n_splits > 1) {
-        int total = 0, pairs = 0, most = 0;
-        for (int i = threadIdx.x & 63; i < a.batch; i += 64) {
-            const TreeSpan o = tree_span<SPARSE>(a, i);
-            const int wgs = a.cache.kv.G * (((o.n << a.g_shift) + TREE_ROWS - 1) / TREE_ROWS), t = tiles_of(o.all);
-            total += t * wgs;
-            pairs += wgs;
-            most = max(most, t);
-        }
-        if (a.batch > 1) {
+__device__ __forceinline__ int tree_piece(const TreeArgs& a) {                 // tiles; 0: no sequence is cut
+    if (a.n_splits == 1) return 0;
+    int total = 0, pairs = 0, most = 0, piece = 0;
+    for (int i = threadIdx.x & 63; i < a.batch; i += 64) {
+        const TreeSpan o = tree_span<SPARSE>(a, i);
+        const int wgs = a.cache.kv.G * (((o.n << a.g_shift) + TREE_ROWS - 1) / TREE_ROWS), t = tiles_of(o.all);
+        total += t * wgs;
+        pairs += wgs;
+        most = max(most, t);
+    }
+    if (a.batch > 1) {
 #pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                total += __shfl_xor(total, o);
-                pairs += __shfl_xor(pairs, o);
-                most = max(most, __shfl_xor(most, o));
-            }
+        for (int o = 1; o < 64; o <<= 1) {
+            total += __shfl_xor(total, o);
+            pairs += __shfl_xor(pairs, o);
+            most = max(most, __shfl_xor(most, o));
         }
-        total = __builtin_amdgcn_readfirstlane(total);
-        pairs = max(__builtin_amdgcn_readfirstlane(pairs), 1);
-        most = __builtin_amdgcn_readfirstlane(most);
-        int best = 0x7fffffff;
-#pragma unroll 1
-        for (int r = 1; r <= (a.batch > 1 ? 8 : 1); ++r) {
-            const int wgs = r * TREE_CUS;
-            if (wgs < pairs) continue;
-            int c = (most + wgs / pairs - 1) / (wgs / pairs);
-            if (wgs > pairs) c = min(c, (total + wgs - pairs - 1) / (wgs - pairs));
-            c = max(c, TREE_MIN_PIECE / TREE_TILE);
-            if (r * (c + TREE_PIECE_COST) < best) {
-                best = r * (c + TREE_PIECE_COST);
-                piece = c;
-            }
+    }
+    total = __builtin_amdgcn_readfirstlane(total);
+    pairs = max(__builtin_amdgcn_readfirstlane(pairs), 1);
+    most = __builtin_amdgcn_readfirstlane(most);
+    // a lane for each R, of which the first eight count (the others repeat them); one sequence takes R = 1
+    const int r = (threadIdx.x & (a.batch > 1 ? 7 : 0)) + 1, wgs = r * TREE_CUS;
+    int cost = 0x7fffffff;
+    if (wgs >= pairs) {
+        piece = (most + wgs / pairs - 1) / (wgs / pairs);
+        if (wgs > pairs) piece = min(piece, (total + wgs - pairs - 1) / (wgs - pairs));
+        piece = max(piece, TREE_MIN_PIECE / TREE_TILE);
+        cost = r * (piece + TREE_PIECE_COST);
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+        const int other_cost = __shfl_xor(cost, o), other_piece = __shfl_xor(piece, o);
+        if (other_cost < cost || (other_cost == cost && other_piece > piece)) {
+            cost = other_cost;
+            piece = other_piece;
         }
+    }
+    piece = __builtin_amdgcn_readfirstlane(piece);
+    return piece > 0 ? piece : most;                              // (0: more sequences than pieces would balance, which stay whole)
+}
+template <bool SPARSE>
+__device__ __forceinline__ TreeSpan tree_work(const TreeArgs& a, int b, int piece) {
+    TreeSpan s = tree_span<SPARSE>(a, b);
+    if (a.n_splits == 1) {
+        piece = tiles_of(s.all);
+    } else {
         piece = min(piece, (SPARSE ? TREE_LIST : TREE_LIST * PAGE) / TREE_TILE);   // what a workgroup's list has room for
-        piece = max(piece, (tiles_of(s.all) + a.n_splits - 1) / a.n_splits);       // what the launch has workgroups for
+        piece = max(piece, (tiles_of(s.all) + a.n_splits - 1) / a.n_splits);       // what the launch has pieces for
     }
     s.chunk = piece * TREE_TILE;
     return s;
@@ -422,15 +433,13 @@ __device__ __forceinline__ float other_half_max(float v) {
 // 16 bytes a lane from memory to LDS at `lds` + 16 * lane, past the registers.  Not the builtin: for that, the compiler lets every later
 // LDS read wait for all such loads, which leaves one tile under way at most.  Whoever uses the bytes waits for them (wait_tiles) and, where
 // another wave asked for them, meets it at a barrier.
-// `once`: nobody else reads these bytes, so the caches need not keep them (a copy of 128 MB to LDS by 256 workgroups: 24.4 us, so 19.7).
-__device__ __forceinline__ void load_to_lds(const uint16_t* from, uint32_t lds, bool once) {
-    if (once) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(lds), "v"(from) : "memory");
-    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+// With the streaming hint: the caches need not keep what is read once (a copy of 128 MB to LDS by 256 workgroups: 24.4 us, so 19.7).
+__device__ __forceinline__ void load_to_lds(const uint16_t* from, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(lds), "v"(from) : "memory");
 }
 // The same from a uniform address and 32 bits of offset a lane.
-__device__ __forceinline__ void load_to_lds(const uint16_t* base, uint32_t offset, uint32_t lds, bool once) {
-    if (once) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds), "v"(offset), "s"(base) : "memory");
-    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+__device__ __forceinline__ void load_to_lds(const uint16_t* base, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds), "v"(offset), "s"(base) : "memory");
 }
 // Until all but the newest min(n, MOST) of this wave's requests of OPS loads each have arrived.
 template <int OPS, int MOST>
@@ -453,6 +462,7 @@ struct TreeLds {
     int32_t list[TREE_LIST];
     float m[TREE_ROWS], l[TREE_ROWS];      // of every row, a set for each team
     uint32_t odd[TREE_MAX_NODES / 32];     // nodes among this workgroup's tokens with a value that is not finite
+    int32_t first_bad;                     // entry of the list that names no row
 };
 
 typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -648,6 +658,7 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
     const int team = wave / RG, mine = wave % RG, half = lane >> 5, col = lane & 31;
     const int g = 1 << a.g_shift, rows = s.n << a.g_shift;
     if (tid < TREE_MAX_NODES / 32) lds.odd[tid] = 0;
+    if (tid == 0) lds.first_bad = 0x7fffffff;
     __syncthreads();
 
     TreeRow row;
@@ -681,11 +692,9 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
     const uint64_t lane_off = (uint64_t)(uint32_t)(mine * MINE + lr) * stride;
 
     const int steps = (end - begin + TT * TEAMS - 1) / (TT * TEAMS);
-    const bool once = a.m_tiles == 1;
-    bool good = true;
+    int good = end;                                               // tokens before this one are all there
     if (LIST) {
         const int entries = SPARSE ? steps * TT * TEAMS : (end - begin + PAGE - 1) / PAGE;
-        bool bad = false;
         for (int e = tid; e < entries; e += TREE_THREADS) {
             int at = -1;
             if (SPARSE) {
@@ -693,15 +702,17 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
                 if (i < end) {
                     const int pos = i < s.pre ? a.idx[(int64_t)b * a.budget + i] : s.before + (i - s.pre);
                     if (i >= s.pre || (uint32_t)pos < (uint32_t)s.before) at = cache_row<PAGED>(a.cache, b, kvh, pos);
-                    bad |= at < 0;
+                    if (at < 0) atomicMin(&lds.first_bad, e);
                 }
             } else {
                 at = cache_row<PAGED>(a.cache, b, kvh, begin + e * PAGE);
-                bad |= at < 0;
+                if (at < 0) atomicMin(&lds.first_bad, e);
             }
             lds.list[e] = at;
         }
-        good = !__syncthreads_or(bad);
+        __syncthreads();
+        const int bad = __builtin_amdgcn_readfirstlane(lds.first_bad);
+        if (bad != 0x7fffffff) good = begin + (SPARSE ? bad : bad * PAGE);   // (a list that ends with the tree's first node has one in its last tile)
     }
     auto k_at = [&](int it) { return ((it % STAGES) * TEAMS + team) * TILE_BYTES; };
     auto v_at = [&](int it) { return TREE_RING / 2 + ((it % STAGES) * TEAMS + team) * TILE_BYTES; };
@@ -723,14 +734,14 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
             } else {
                 off = (int64_t)(t + TT <= end ? (uint64_t)(uint32_t)(t + n * 4) * stride + lane_off : (uint64_t)(uint32_t)min(t + r0 + r, end - 1) * stride);
             }
-            load_to_lds((values ? vbase : kbase) + off + (values ? chunk : chunk ^ ((n * 4 & 15) << 3)), to + n * 1024, once);
+            load_to_lds((values ? vbase : kbase) + off + (values ? chunk : chunk ^ ((n * 4 & 15) << 3)), to + n * 1024);
         }
     };
     // Which tokens of tile `it` are there, and which of them this wave's rows attend to (`common`: all of them).
     auto attended = [&](int it, uint32_t& there, uint32_t& common) -> uint32_t {
         const int t = begin + (it * TEAMS + team) * TT;
         there = t + 32 <= end ? 0xffffffffu : t >= end ? 0u : (1u << (end - t)) - 1;
-        if (LIST && !good) there = (uint32_t)__ballot(t + col < end && lds.list[SPARSE ? t - begin + col : (t - begin + col) >> 4] >= 0);
+        if (LIST && t + 32 > good) there = (uint32_t)__ballot(t + col < end && lds.list[SPARSE ? t - begin + col : (t - begin + col) >> 4] >= 0);
         const int from = s.pre - t;                               // tokens of the prefix in this step
         const uint32_t prefix = from >= 32 ? 0xffffffffu : from <= 0 ? 0u : (1u << from) - 1;
         common = prefix & there;
@@ -743,7 +754,7 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
             atomicOr(&lds.odd[i >> 5], 1u << (i & 31));
         }
     };
-    const int plain = good ? max(0, min(s.pre, end) - begin) / (TT * TEAMS) : 0;   // tiles that every row attends to as a whole: the first ones
+    const int plain = max(0, min(s.pre, good) - begin) / (TT * TEAMS);   // tiles that every row attends to as a whole: the first ones
     if constexpr (RG < 4) {
         // Few rows: the products are short, and what counts is that tiles keep coming.  A tile is a step.  A wave on its own asks for the next when it
         // has read one, while seven others are elsewhere; a team of two has a second buffer for it.
@@ -813,7 +824,7 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
             if (n < steps) request(n, true);
             if (n + 2 < steps) request(n + 2, false);
         };
-        const int full = (end - begin) / (TT * TEAMS);            // whole tiles
+        const int full = (good - begin) / (TT * TEAMS);           // whole tiles
         uint32_t part_k[MINE / 4], part_v[MINE / 4];              // the lane's part of a row's address
 #pragma unroll
         for (int i = 0; i < MINE / 4; ++i) {
@@ -823,19 +834,20 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
         }
         // Pairs n .. n + BLOCK - 1.  Whole tiles of a whole prefix: the rows of a wave's part are one after the other, in a page or in the sequence, and a
         // uniform address serves.  Of a chosen prefix each lane has its own; the list's entries come all at once.
+        constexpr int GROUPS = MINE / 4;
         auto request_block = [&](int n) {
-            if (!good || n + BLOCK + 2 > full) {
+            if (n + BLOCK + 2 > full) {
 #pragma unroll
                 for (int j = 0; j < BLOCK; ++j) request_pair(n + j);
                 return;
             }
             const int t = (n * TEAMS + team) * TT + mine * MINE;  // the wave's first row of tile n
-            int entry[BLOCK + 2][SPARSE ? MINE / 4 : 1];
+            int entry[BLOCK + 2][SPARSE ? GROUPS : 1];
             if (LIST) {
 #pragma unroll
                 for (int j = 0; j < BLOCK + 2; ++j)
 #pragma unroll
-                    for (int i = 0; i < (SPARSE ? MINE / 4 : 1); ++i)
+                    for (int i = 0; i < (SPARSE ? GROUPS : 1); ++i)
                         entry[j][i] = lds.list[SPARSE ? t + j * (TEAMS * TT) + i * 4 + lr : (t + j * (TEAMS * TT)) >> 4];
             }
             auto row_at = [&](int j) {                            // the first of the wave's rows of tile n + j, in elements
@@ -847,16 +859,16 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
                 const uint32_t kt = ring + k_at(n + j + 2) + mine * MINE * 256, vt = ring + v_at(n + j) + mine * MINE * 256;
                 if constexpr (SPARSE) {
 #pragma unroll
-                    for (int i = 0; i < MINE / 4; ++i) {
-                        load_to_lds(vbase + (uint64_t)(uint32_t)entry[j][i] * stride + part_v[i] / 2, vt + i * 1024, once);
-                        load_to_lds(kbase + (uint64_t)(uint32_t)entry[j + 2][i] * stride + part_k[i] / 2, kt + i * 1024, once);
+                    for (int i = 0; i < GROUPS; ++i) {
+                        load_to_lds(vbase + (uint64_t)(uint32_t)entry[j][i] * stride + part_v[i] / 2, vt + i * 1024);
+                        load_to_lds(kbase + (uint64_t)(uint32_t)entry[j + 2][i] * stride + part_k[i] / 2, kt + i * 1024);
                     }
                 } else {
                     const uint16_t *v = vbase + row_at(j), *k = kbase + row_at(j + 2);
 #pragma unroll
-                    for (int i = 0; i < MINE / 4; ++i) {
-                        load_to_lds(v, part_v[i], vt + i * 1024, once);
-                        load_to_lds(k, part_k[i], kt + i * 1024, once);
+                    for (int i = 0; i < GROUPS; ++i) {
+                        load_to_lds(v, part_v[i], vt + i * 1024);
+                        load_to_lds(k, part_k[i], kt + i * 1024);
                     }
                 }
             }
@@ -1036,9 +1048,8 @@ __global__ __launch_bounds__(TREE_THREADS, 2) void tree_attn_kernel(TreeArgs a) 
     const uint32_t G = a.cache.kv.G, pairs = G * (uint32_t)a.batch, pair = unit % pairs;
     const int split = unit / pairs, b = pair / G, kvh = pair - b * G, row0 = m_tile * TREE_ROWS;
     if (split >= a.n_splits) return;
-    const TreeSpan s = tree_work<SPARSE>(a, b);
-    const int left = (s.n << a.g_shift) - row0;
-    const int begin = split * s.chunk;
+    const TreeSpan s = tree_work<SPARSE>(a, b, tree_piece<SPARSE>(a));
+    const int left = (s.n << a.g_shift) - row0, begin = split * s.chunk;
     if (left <= 0 || begin >= s.all) return;
     // (a piece has no more tokens or pages than the list has room for: plan_tree)
     const int end = min(begin + s.chunk, s.all);
