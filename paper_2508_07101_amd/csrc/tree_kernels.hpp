@@ -341,14 +341,19 @@ constexpr int TREE_TILE = 32;              // tokens of a tile: pieces are whole
 // What a workgroup of one sequence has to do, the same in the attention and in the merge.
 struct TreeSpan {
     int start, n;          // its nodes' rows in the packed arrays
+    int part;              // its first row among the partial results
     int before, pre, all;  // P; tokens of the prefix that are looked at; the same and the nodes
     int chunk;             // tokens of a piece
 };
+// The workspace has rows for max_nodes nodes of a sequence.  A sequence that owns more rows of the packed arrays has only its first max_nodes looked at:
+// the next one's start there may lie behind the workspace's rows, and its partial results move up (to rows of their own: starts are apart by as much).
+__device__ __forceinline__ int part_row(const TreeArgs& a, int b, int start) { return min(start, b * a.max_nodes); }
 template <bool SPARSE>
 __device__ __forceinline__ TreeSpan tree_span(const TreeArgs& a, int b) {
     TreeSpan s;
     const int L = clampi(a.cache.kv.seq_lens[b], 0, a.cache.max_len);
     s.n = min(tree_span(a.tok_start, b, a.max_tokens, a.max_nodes, s.start), L);
+    s.part = part_row(a, b, s.start);
     s.before = L - s.n;
     s.pre = SPARSE ? clampi(a.cnt[b], 0, a.budget) : s.before;
     s.all = s.n > 0 ? s.pre + s.n : 0;
@@ -1024,14 +1029,15 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
                 }
             }
         }
-        const int64_t to = (int64_t)(s.start + (row >> a.g_shift)) * a.H + (kvh << a.g_shift) + (row & (g - 1));
+        const int head = (kvh << a.g_shift) + (row & (g - 1));
         if (whole) {
+            const int64_t to = (int64_t)(s.start + (row >> a.g_shift)) * a.H + head;
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
             const u32x2 w = {(uint32_t)f32_to_bf16_rne(v[0] * inv) | (uint32_t)f32_to_bf16_rne(v[1] * inv) << 16,
                              (uint32_t)f32_to_bf16_rne(v[2] * inv) | (uint32_t)f32_to_bf16_rne(v[3] * inv) << 16};
             *reinterpret_cast<u32x2*>(a.out + to * D + c * 4) = w;
         } else {
-            const int64_t piece = to * a.n_splits + split;
+            const int64_t piece = ((int64_t)(s.part + (row >> a.g_shift)) * a.H + head) * a.n_splits + split;
             *reinterpret_cast<f32x4*>(a.part_acc + piece * D + c * 4) = v;
             if (c == 0) *reinterpret_cast<f32x2*>(a.part_ml + piece * 2) = f32x2{top, sum};
         }
@@ -1070,7 +1076,7 @@ __global__ __launch_bounds__(64 * REDUCE_WAVES) void tree_reduce_kernel(TreeArgs
     const int pieces = a.pieces[b];
     if (pieces <= 1) return;
     for (int r = blockIdx.x * REDUCE_WAVES + (threadIdx.x >> 6); r < n * a.H; r += gridDim.x * REDUCE_WAVES) {
-        const int64_t row = (int64_t)start * a.H + r, first = row * a.n_splits;
+        const int64_t row = (int64_t)start * a.H + r, first = ((int64_t)part_row(a, b, start) * a.H + r) * a.n_splits;
         float m = LOWEST, l = 0.0f;
         if (lane < pieces) {
             const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + (first + lane) * 2);

@@ -27,12 +27,12 @@ struct TreePlan {
 };
 
 inline TreePlan plan_tree(TreeKind kind, int max_len, int batch, int G, int g, int max_nodes) {
-    const int pairs = batch * G;
+    const int64_t pairs = (int64_t)batch * G;
     TreePlan p;
     p.m_tiles = (max_nodes * g + TREE_ROWS - 1) / TREE_ROWS;
     // One sequence: a piece for each CU.  Several: room for as many as make up for their lengths' differences (64 of 8192 to 32768 tokens, 8 KV heads:
     // pieces of the longest alone 1437 us, see tree_work).
-    const int64_t wgs = (int64_t)pairs * p.m_tiles, want = batch == 1 ? TREE_CUS / wgs : wgs >= 8 * TREE_CUS ? 1 : std::max<int64_t>(4, 2 * TREE_CUS / wgs);
+    const int64_t wgs = pairs * p.m_tiles, want = batch == 1 ? TREE_CUS / wgs : wgs >= 8 * TREE_CUS ? 1 : std::max<int64_t>(4, 2 * TREE_CUS / wgs);
     const int64_t by_len = ((int64_t)max_len + TREE_MIN_PIECE - 1) / TREE_MIN_PIECE, by_list = ((int64_t)max_len + tree_piece_most(kind) - 1) / tree_piece_most(kind);
     p.n_splits = (int)std::max<int64_t>({1, by_list, std::min<int64_t>({want, by_len, (int64_t)TREE_MAX_SPLITS})});
     return p;

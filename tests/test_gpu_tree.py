@@ -327,6 +327,23 @@ def test_trees_longer_than_the_bounds_are_cut():
     assert torch.isfinite(out.float()).all()
 
 
+@pytest.mark.parametrize("H,G", [(8, 2), (32, 8)])
+def test_rows_between_trees_beyond_the_bound_need_no_workspace(H, G):
+    """A sequence that owns more rows than max_nodes: the next one's rows start behind batch * max_nodes, its pieces' partial results do not."""
+    c = _Case("paged", H, G, [3000, 2500], [4, 4], 6, max_nodes=4)
+    want = c.check()
+    q, masks = (torch.zeros((100,) + x.shape[1:], dtype=x.dtype, device=DEV) for x in (c.q, c.tree.masks))
+    for x, y in ((q, c.q), (masks, c.tree.masks)):
+        x[:4], x[90:94] = y[:4], y[4:]
+    out = torch.full((100, H, 128), 9.0, dtype=torch.bfloat16, device=DEV)
+    need = cb.tree_workspace_bytes(c.params, c.max_len, 100, 4)
+    ws = torch.full((need + 64 * H * 128 * 100,), 255, dtype=torch.uint8, device=DEV)
+    cb.tree_attn(c.params, q, c.kv(), cb.Tree(_i32([0, 90, 94]), masks, 4), out, ws[:need])
+    torch.cuda.synchronize()
+    assert torch.equal(out[:4], want[:4]) and torch.equal(out[90:94], want[4:])
+    assert (out[4:90] == 9).all() and (out[94:] == 9).all() and (ws[need:] == 255).all()
+
+
 @pytest.mark.parametrize("budget", [0, 4000])
 def test_long_prefixes_and_bounds_far_above_the_lengths(budget):
     for before, nodes, H in (([40000], [60], 32), ([131000], [3], 8), ([20000, 100, 7000], [17, 30, 1], 32)):
