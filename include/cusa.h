@@ -276,7 +276,7 @@ typedef struct {
  *   slots[tok_start[b] + j]   where token keep + j of b goes: paged page * 16 + position % 16 (-1 for a table entry that names
  *                     no page), contiguous b * 2^32 + position; -1 behind the last
  * Pages given back by a call are not handed out by it.  held, keep, add, lens: device int32 [batch] (lens may be held or keep);
- * tok_start: device int32 [batch + 1]; slots: device int64 [max_tokens].  One kernel, or two for max_tokens above 4096.
+ * tok_start: device int32 [batch + 1]; slots: device int64 [max_tokens].  One kernel, or two for max_tokens above 4096 or batch above 1024.
  * ws: cusa_kv_plan_workspace_bytes(batch) bytes, 256-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL, LAUNCH. */
 size_t      cusa_kv_plan_workspace_bytes(int32_t batch);
 cusa_status cusa_kv_plan(const cusa_pool* pool, const int32_t* held, const int32_t* keep, const int32_t* add, int32_t max_tokens,
@@ -319,6 +319,8 @@ cusa_status cusa_tree_masks(int32_t batch, const int32_t* base, const int32_t* t
  * idx, cnt (both or neither): of the prefix only idx[b][0 .. cnt[b]) (as cusa_select makes them for the tree's first node: entries
  * from P on, which the masks speak for, are left out); idx device int32 [batch][budget], cnt[b] in [0, budget].
  * A node that attends to nothing gives zeros.  NaN and infinities in rows that a node does not attend to do not reach its output.
+ * Scores and sums are binary32; weights are rounded to bf16 for their product with V, and count as 0 below 2^-126 of the row's reference, which is at most
+ * 2^8 times smaller than the largest weight.
  * q: device bf16, row r head h at q + r * q_stride + h * 128; out: device bf16 [max_tokens][n_q_heads][128]; rows of no
  * sequence are not written.  ws: cusa_tree_workspace_bytes, 256-byte aligned, content not preserved.
  * Errors as cusa_full_attn, and UNSUPPORTED for max_nodes > 256, pools of 2^31 or more rows, max_seq_len above 5242880 and, with idx, budget + max_nodes
@@ -329,7 +331,7 @@ cusa_status cusa_tree_attn(const cusa_params* params, const void* q, const cusa_
 
 /* The accepted branches' rows moved together, in all layers: position base[b] + path[b][i] -> base[b] + i for i < n_path[b], K and V,
  * all KV heads; path[b] ascending, and positions at or beyond max_seq_len are left out.  keep[b] = base[b] + n_path[b] (NULL: not
- * wanted; may be base), what the next cusa_kv_plan keeps.  path: device int32 [batch][max_path]; base, n_path, keep: device int32 [batch]. */
+ * wanted; neither base nor n_path), what the next cusa_kv_plan keeps.  path: device int32 [batch][max_path]; base, n_path, keep: device int32 [batch]. */
 cusa_status cusa_kv_commit(const cusa_params* params, int32_t n_layers, const cusa_kv* kv_layers, const int32_t* base,
                            const int32_t* path, int32_t max_path, const int32_t* n_path, int32_t* keep, void* stream);
 

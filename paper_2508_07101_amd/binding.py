@@ -349,9 +349,11 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
-def _need_int(what: str, n: int, dtype, **tensors):
-    for name, t in tensors.items():
-        _need(t.dtype == dtype and t.is_contiguous() and t.numel() >= n, f"{what}: {name} holds {n} {dtype}, contiguous")
+def _need_int(what: str, n: int, dtype, *tensors):
+    """Every tensor holds n contiguous numbers of this type at least.  (A step makes these calls once a layer: the message is made when it is needed.)"""
+    for t in tensors:
+        if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
+            raise ValueError(f"{what}: a tensor of {n} or more {dtype}, contiguous, was expected, not {tuple(t.shape)} {t.dtype}")
 
 
 def kv_plan_workspace_bytes(batch: int) -> int:
@@ -367,9 +369,9 @@ def kv_plan(held, keep, add, lens, tok_start, slots, ws, pool: Optional[PagePool
     `capacity` positions a sequence), lens, tok_start and the slots of the new rows (int64, its length bounds the batch's tokens).
     state_out: where the queue's state goes instead of back into the pool, to ask without taking."""
     n = held.numel()
-    _need_int("kv_plan", n, torch.int32, held=held, keep=keep, add=add, lens=lens)
-    _need_int("kv_plan", n + 1, torch.int32, tok_start=tok_start)
-    _need_int("kv_plan", 0, torch.int64, slots=slots)
+    _need_int("kv_plan", n, torch.int32, held, keep, add, lens)
+    _need_int("kv_plan", n + 1, torch.int32, tok_start)
+    _need_int("kv_plan", 0, torch.int64, slots)
     if pool is None:
         d = CusaPool(KV_CONTIGUOUS, n, capacity, None, 0, 0, 0, None, None, None)
     else:
@@ -385,7 +387,7 @@ def kv_append(params: CusaParams, kv: KvCache, slots, k_new, v_new):
     _need(k_new.dtype in DTYPES and v_new.dtype == k_new.dtype and v_new.shape == k_new.shape and d == params.head_dim and
           heads == params.n_kv_heads, "kv_append: new rows are [n, n_kv_heads, 128] in bf16, fp16 or fp32")
     _need(k_new.stride(2) == 1 and k_new.stride() == v_new.stride(), "kv_append: K and V rows have the same strides, elements side by side")
-    _need_int("kv_append", n, torch.int64, slots=slots)
+    _need_int("kv_append", n, torch.int64, slots)
     c = kv.desc()
     r = CusaRows(_ptr(k_new), _ptr(v_new), DTYPES[k_new.dtype], n, k_new.stride(0), k_new.stride(1))
     _check(load().cusa_kv_append(ctypes.byref(params), ctypes.byref(c), _ptr(slots), ctypes.byref(r), _stream()), "cusa_kv_append")
@@ -399,11 +401,12 @@ def mask_words(max_nodes: int) -> int:
 def tree_masks(base, tok_start, parents, masks, positions, max_nodes: int):
     """masks (int64 [tokens, mask_words], bit patterns) and positions (int32, or None) of trees given by their nodes' parents."""
     n = parents.numel()
-    _need_int("tree_masks", tok_start.numel() - 1, torch.int32, base=base)
-    _need_int("tree_masks", 2, torch.int32, tok_start=tok_start)
-    _need_int("tree_masks", n, torch.int32, parents=parents, **({} if positions is None else {"positions": positions}))
-    _need_int("tree_masks", n * mask_words(max_nodes), torch.int64, masks=masks)
-    _check(load().cusa_tree_masks(tok_start.numel() - 1, _ptr(base), _ptr(tok_start), _ptr(parents), n, max_nodes, _ptr(masks),
+    batch = tok_start.numel() - 1
+    _need_int("tree_masks", batch, torch.int32, base)
+    _need_int("tree_masks", 2, torch.int32, tok_start)
+    _need_int("tree_masks", n, torch.int32, parents, parents if positions is None else positions)
+    _need_int("tree_masks", n * mask_words(max_nodes), torch.int64, masks)
+    _check(load().cusa_tree_masks(batch, _ptr(base), _ptr(tok_start), _ptr(parents), n, max_nodes, _ptr(masks),
                                   _ptr(positions), _stream()), "cusa_tree_masks")
 
 
@@ -432,12 +435,12 @@ def tree_attn(params: CusaParams, q, kv: KvCache, tree: Tree, out, ws, idx=None,
     _need(q.dtype == torch.bfloat16 and heads == params.n_q_heads and d == params.head_dim and q.stride(2) == 1 and q.stride(1) == d,
           "tree_attn: q is bf16 [tokens, n_q_heads, 128], heads side by side")
     _need(out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() >= n * heads * d, "tree_attn: out is bf16 [tokens, n_q_heads, 128], contiguous")
-    _need_int("tree_attn", params.batch + 1, torch.int32, tok_start=tree.tok_start)
-    _need_int("tree_attn", n * mask_words(tree.max_nodes), torch.int64, masks=tree.masks)
+    _need_int("tree_attn", params.batch + 1, torch.int32, tree.tok_start)
+    _need_int("tree_attn", n * mask_words(tree.max_nodes), torch.int64, tree.masks)
     if idx is not None:
-        _need_int("tree_attn", params.batch * params.budget, torch.int32, idx=idx)
+        _need_int("tree_attn", params.batch * params.budget, torch.int32, idx)
         _need(cnt is not None, "tree_attn: idx comes with cnt")
-        _need_int("tree_attn", params.batch, torch.int32, cnt=cnt)
+        _need_int("tree_attn", params.batch, torch.int32, cnt)
     c = kv.desc()
     t = CusaTree(_ptr(tree.tok_start), _ptr(tree.masks), n, tree.max_nodes, q.stride(0))
     _check(load().cusa_tree_attn(ctypes.byref(params), _ptr(q), ctypes.byref(c), ctypes.byref(t), _ptr(idx), _ptr(cnt), _ptr(out), _ptr(ws),
@@ -456,7 +459,7 @@ class KvCommit:
         """Positions base[b] + path[b][i] -> base[b] + i for i < n_path[b]; keep (not base): base + n_path."""
         b = self.params.batch
         _need(path.dim() == 2 and path.shape[0] == b, "kv_commit: path is [batch, nodes]")
-        _need_int("kv_commit", b, torch.int32, base=base, path=path, n_path=n_path, **({} if keep is None else {"keep": keep}))
+        _need_int("kv_commit", b, torch.int32, base, path, n_path, n_path if keep is None else keep)
         _check(load().cusa_kv_commit(ctypes.byref(self.params), self.n, self.kvs, _ptr(base), _ptr(path), path.shape[1], _ptr(n_path),
                                      _ptr(keep), _stream()), "cusa_kv_commit")
 

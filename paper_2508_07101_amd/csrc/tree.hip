@@ -111,13 +111,13 @@ cusa_status cusa_kv_plan(const cusa_pool* pool, const int32_t* held, const int32
     a.n_pages = (int32_t)pool->n_pages;
     a.cap = paged ? (int32_t)std::min<int64_t>((int64_t)pool->max_pages * PAGE, 0x7fffffff) : pool->capacity;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (max_tokens <= PLAN_ONE_LAUNCH) {
+    if (max_tokens <= PLAN_ONE_LAUNCH && pool->batch <= PLAN_THREADS) {
         launch(KID_KV_PLAN, kv_plan_kernel<true>, 1, PLAN_THREADS, 0, s, a);
         return launch_status();
     }
     launch(KID_KV_PLAN, kv_plan_kernel<false>, 1, PLAN_THREADS, 0, s, a);
     if (launch_status() != CUSA_OK) return CUSA_ERR_LAUNCH;
-    const int64_t wgs = std::min<int64_t>(((int64_t)max_tokens + FILL_THREADS - 1) / FILL_THREADS, 2048);
+    const int64_t wgs = std::min<int64_t>(((int64_t)max_tokens + FILL_THREADS * FILL_RUN - 1) / (FILL_THREADS * FILL_RUN), 2048);
     launch(KID_KV_FILL, kv_fill_kernel, dim3((unsigned)wgs), FILL_THREADS, 0, s, a);
     return launch_status();
 }

@@ -47,74 +47,129 @@ struct PlanArgs {
     int32_t batch, max_tokens, max_pages, n_pages, cap;
 };
 
-// Sum over the workgroup's threads before this one; total: of all.  scratch: a word for each wave, and a barrier before its next use.
-__device__ __forceinline__ int64_t plan_scan(int64_t v, int64_t* scratch, int64_t& total) {
+// Sums over the workgroup's threads before this one, of two values at once; total: of all.  Only the first `waves` waves hold values.  scratch: two words
+// for each wave, not in use by the call before.
+__device__ __forceinline__ void plan_scan(int64_t (&v)[2], int64_t (&total)[2], int64_t (*scratch)[PLAN_THREADS / 64], int waves) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t x = v;
+    int64_t x[2] = {v[0], v[1]};
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const int64_t y = __shfl_up(x, o);
-        if (lane >= o) x += y;
+        const int64_t y0 = __shfl_up(x[0], o), y1 = __shfl_up(x[1], o);
+        if (lane >= o) {
+            x[0] += y0;
+            x[1] += y1;
+        }
     }
-    if (lane == 63) scratch[wave] = x;
+    if (lane == 63) {
+        scratch[0][wave] = x[0];
+        scratch[1][wave] = x[1];
+    }
     __syncthreads();
-    int64_t before = 0, all = 0;
+    int64_t before[2] = {0, 0}, all[2] = {0, 0};
+#pragma unroll 1
+    for (int w = 0; w < waves; ++w) {
 #pragma unroll
-    for (int w = 0; w < PLAN_THREADS / 64; ++w) {
-        const int64_t s = scratch[w];
-        if (w < wave) before += s;
-        all += s;
+        for (int i = 0; i < 2; ++i) {
+            if (w == wave) before[i] = all[i];
+            all[i] += scratch[i][w];
+        }
     }
-    __syncthreads();
-    total = all;
-    return before + x - v;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        v[i] = (wave < waves ? before[i] : all[i]) + x[i] - v[i];
+        total[i] = all[i];
+    }
+}
+__device__ __forceinline__ int64_t plan_scan(int64_t v, int64_t& total, int64_t (*scratch)[PLAN_THREADS / 64], int waves) {
+    int64_t x[2] = {v, 0}, t[2];
+    plan_scan(x, t, scratch, waves);                     // (what is not used is not computed)
+    total = t[0];
+    return x[0];
+}
+// A place of the queue, which has n entries, from a number that is mostly below 2 n (the division of 64 bits is long).
+__device__ __forceinline__ int64_t ring_at(int64_t x, int64_t n) {
+    if (x >= n) x -= n;
+    if (x >= n) x %= n;
+    return x;
 }
 
-// Slots of tokens and pages from the queue, by thread `at` of `step`; pages to the queue's end.
-__device__ __forceinline__ void plan_fill(const PlanArgs& a, int64_t at, int64_t step, int seq_at, int seq_step, int lane, int lanes) {
-    const int total = a.tok_start[a.batch];
-    const int first = a.table ? a.head->first : 0, avail = a.table ? a.head->avail : 0;
-    for (int64_t r = at; r < a.max_tokens; r += step) {
-        if (r >= total) {
-            a.slots[r] = -1;
-            continue;
+constexpr int FILL_RUN = 4;                              // consecutive tokens of a thread: mostly of one page
+// Slots of tokens and pages from the queue, by thread `at` of `step`; pages to the queue's end.  starts, seq, lens: in LDS where they fit.
+__device__ __forceinline__ void plan_fill(const PlanArgs& a, const int32_t* starts, const PlanSeq* seq, const int32_t* lens, int first, int avail, int64_t at,
+                                          int64_t step, int seq_at, int seq_step, int lane, int lanes) {
+    const int total = starts[a.batch];
+    const bool wide = ((uintptr_t)a.slots & 15) == 0;
+    for (int64_t r0 = at * FILL_RUN; r0 < a.max_tokens; r0 += step * FILL_RUN) {
+        int64_t slot[FILL_RUN];
+        int lo = 0, hi = a.batch - 1;                    // the last sequence that starts at or before r0
+        if (r0 < total) {
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (starts[mid] <= r0) lo = mid;
+                else hi = mid - 1;
+            }
         }
-        int lo = 0, hi = a.batch - 1;                    // the last sequence that starts at or before r and is not empty: tok_start[lo] <= r < tok_start[lo + 1]
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (a.tok_start[mid] <= r) lo = mid;
-            else hi = mid - 1;
+        PlanSeq s = seq[lo];
+        int32_t start = starts[lo], next = starts[lo + 1], id = -1;
+        bool held = false;                               // id is the page of the token before
+#pragma unroll
+        for (int j = 0; j < FILL_RUN; ++j) {
+            const int64_t r = r0 + j;
+            slot[j] = -1;
+            if (r >= total) continue;
+            if (r >= next) {
+                do next = starts[++lo + 1];              // (total lies behind r: one comes)
+                while (r >= next);
+                s = seq[lo];
+                start = starts[lo];
+                held = false;
+            }
+            const int64_t pos = s.keep + (r - start);
+            if (!a.table) {
+                slot[j] = ((int64_t)lo << 32) + pos;
+                continue;
+            }
+            if (!held || (pos & (PAGE - 1)) == 0) {
+                const int page = (int)(pos >> 4);
+                int32_t* const entry = a.table + (int64_t)lo * a.max_pages + page;
+                if (page < s.old_pages) {
+                    id = *entry;
+                } else {
+                    uint32_t from = (uint32_t)first + (uint32_t)(s.pop + (page - s.old_pages));   // (what is granted was free: below n_pages each)
+                    if (from >= (uint32_t)a.n_pages) from -= a.n_pages;
+                    id = a.ring[from];
+                    if ((pos & (PAGE - 1)) == 0) *entry = id;   // a new page's first token is always among the new ones
+                }
+                held = true;
+            }
+            if ((uint32_t)id < (uint32_t)a.n_pages) slot[j] = (int64_t)id * PAGE + (pos & (PAGE - 1));
         }
-        const PlanSeq s = a.seq[lo];
-        const int64_t pos = s.keep + (r - a.tok_start[lo]);
-        if (!a.table) {
-            a.slots[r] = ((int64_t)lo << 32) + pos;
-            continue;
-        }
-        const int page = (int)(pos >> 4);
-        int32_t* const entry = a.table + (int64_t)lo * a.max_pages + page;
-        int32_t id;
-        if (page < s.old_pages) {
-            id = *entry;
+        if (wide && r0 + FILL_RUN <= a.max_tokens) {
+            typedef int64_t i64x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+            for (int j = 0; j < FILL_RUN; j += 2) *reinterpret_cast<i64x2*>(a.slots + r0 + j) = i64x2{slot[j], slot[j + 1]};
         } else {
-            id = a.ring[((int64_t)first + s.pop + (page - s.old_pages)) % a.n_pages];
-            if ((pos & (PAGE - 1)) == 0) *entry = id;    // a new page's first token is always among the new ones
+#pragma unroll
+            for (int j = 0; j < FILL_RUN; ++j)
+                if (r0 + j < a.max_tokens) a.slots[r0 + j] = slot[j];
         }
-        a.slots[r] = (uint32_t)id < (uint32_t)a.n_pages ? (int64_t)id * PAGE + (pos & (PAGE - 1)) : -1;
     }
     if (!a.table) return;
     for (int b = seq_at; b < a.batch; b += seq_step) {
-        const PlanSeq s = a.seq[b];
-        const int now = pages_of(a.lens[b]);
+        const PlanSeq s = seq[b];
+        const int now = pages_of(lens[b]);
         for (int i = lane; i < s.old_pages - now; i += lanes)
-            a.ring[((int64_t)first + avail + s.push + i) % a.n_pages] = a.table[(int64_t)b * a.max_pages + now + i];
+            a.ring[ring_at((int64_t)first + avail + s.push + i, a.n_pages)] = a.table[(int64_t)b * a.max_pages + now + i];
     }
 }
 
-// A thread for each sequence, 1024 at a time.  Latency is all: a few dependent reads and the three sums.
+// A thread for each sequence, 1024 at a time.  Latency is all: a read of the numbers, three sums, a search, a page's entry.  What the slots need of
+// up to 1024 sequences stays in LDS (searched in memory, 64 sequences' 2000 slots took 10.9 us in all, so 7.1).
 template <bool FILL>
 __global__ __launch_bounds__(PLAN_THREADS) void kv_plan_kernel(PlanArgs a) {
-    __shared__ int64_t scratch[PLAN_THREADS / 64];
+    __shared__ int64_t scratch[3][2][PLAN_THREADS / 64];
+    __shared__ int32_t starts[PLAN_THREADS + 1], lengths[PLAN_THREADS];
+    __shared__ PlanSeq seqs[PLAN_THREADS];
     const int tid = threadIdx.x;
     int64_t asked = 0, needed = 0, granted = 0, taken = 0, returned = 0;   // of the sequences before this round's
     int first = 0, avail = 0;
@@ -130,52 +185,64 @@ __global__ __launch_bounds__(PLAN_THREADS) void kv_plan_kernel(PlanArgs a) {
         const int keep = here ? clampi(a.keep[b], 0, held) : 0;
         const int add = here ? max(a.add[b], 0) : 0;
         const bool fits = (int64_t)keep + add <= a.cap;
+        const int waves = min((a.batch - base + 63) >> 6, PLAN_THREADS / 64);
         int64_t sum;
-        const int64_t tokens = fits ? add : 0, tokens_before = asked + plan_scan(tokens, scratch, sum);
+        const int64_t tokens = fits ? add : 0, tokens_before = asked + plan_scan(tokens, sum, scratch[0], waves);
         asked += sum;
         bool ok = fits && tokens_before + tokens <= a.max_tokens;
         const int old_pages = pages_of(held);
         if (a.table) {
-            const int64_t need = ok ? max(pages_of(keep + add) - old_pages, 0) : 0, need_before = needed + plan_scan(need, scratch, sum);
+            const int64_t need = ok ? max(pages_of(keep + add) - old_pages, 0) : 0, need_before = needed + plan_scan(need, sum, scratch[1], waves);
             needed += sum;
             ok = ok && (need == 0 || need_before + need <= avail);
         }
-        const int n = ok ? add : 0, len = keep + n;
-        const int64_t start = granted + plan_scan(n, scratch, sum);
-        granted += sum;
-        int64_t pop = 0, push = 0;
-        if (a.table) {
-            const int change = pages_of(len) - old_pages;
-            int64_t both;                                // taken and given back: 32 bits each (n_pages < 2^31)
-            const int64_t v = ((int64_t)max(-change, 0) << 32) + max(change, 0), before = plan_scan(v, scratch, both);
-            pop = taken + (before & 0xffffffff);
-            push = returned + (before >> 32);
-            taken += both & 0xffffffff;
-            returned += both >> 32;
-        }
+        const int n = ok ? add : 0, len = keep + n, change = a.table ? pages_of(len) - old_pages : 0;
+        // tokens; pages taken and given back, 32 bits each (n_pages < 2^31)
+        int64_t v[2] = {n, ((int64_t)max(-change, 0) << 32) + max(change, 0)}, both[2];
+        plan_scan(v, both, scratch[2], waves);
+        const int start = (int)(granted + v[0]);
+        const PlanSeq s = {keep, old_pages, (int)(taken + (v[1] & 0xffffffff)), (int)(returned + (v[1] >> 32))};
+        granted += both[0];
+        taken += both[1] & 0xffffffff;
+        returned += both[1] >> 32;
         if (here) {
             a.lens[b] = len;
-            a.tok_start[b] = (int)start;
-            a.seq[b] = PlanSeq{keep, old_pages, (int)pop, (int)push};
+            a.tok_start[b] = start;
+            if (!FILL) a.seq[b] = s;
+            if (FILL) {
+                lengths[tid] = len;
+                starts[tid] = start;
+                seqs[tid] = s;
+            }
         }
     }
     if (tid == 0) {
         a.tok_start[a.batch] = (int)granted;
+        if (FILL) starts[a.batch] = (int)granted;
         if (a.table) {
-            *a.head = PlanHead{first, avail};
-            a.state_out[0] = (int)(((int64_t)first + taken) % a.n_pages);
+            if (!FILL) *a.head = PlanHead{first, avail};
+            a.state_out[0] = (int)ring_at((int64_t)first + taken, a.n_pages);
             a.state_out[1] = (int)min((int64_t)avail - taken + returned, (int64_t)a.n_pages);
         }
     }
-    if (FILL) {
+    if (FILL) {                                          // (up to PLAN_THREADS sequences)
         __syncthreads();
-        plan_fill(a, tid, PLAN_THREADS, tid >> 6, PLAN_THREADS / 64, tid & 63, 64);
+        plan_fill(a, starts, seqs, lengths, first, avail, tid, PLAN_THREADS, tid >> 6, PLAN_THREADS / 64, tid & 63, 64);
     }
 }
 
 constexpr int FILL_THREADS = 256;
 __global__ __launch_bounds__(FILL_THREADS) void kv_fill_kernel(PlanArgs a) {
-    plan_fill(a, (int64_t)blockIdx.x * FILL_THREADS + threadIdx.x, (int64_t)gridDim.x * FILL_THREADS, blockIdx.x, gridDim.x, threadIdx.x, FILL_THREADS);
+    __shared__ int32_t starts[PLAN_THREADS + 1];
+    const int64_t at = (int64_t)blockIdx.x * FILL_THREADS + threadIdx.x, step = (int64_t)gridDim.x * FILL_THREADS;
+    const int first = a.table ? a.head->first : 0, avail = a.table ? a.head->avail : 0;
+    if (a.batch <= PLAN_THREADS) {
+        for (int i = threadIdx.x; i <= a.batch; i += FILL_THREADS) starts[i] = a.tok_start[i];
+        __syncthreads();
+        plan_fill(a, starts, a.seq, a.lens, first, avail, at, step, blockIdx.x, gridDim.x, threadIdx.x, FILL_THREADS);
+    } else {
+        plan_fill(a, a.tok_start, a.seq, a.lens, first, avail, at, step, blockIdx.x, gridDim.x, threadIdx.x, FILL_THREADS);
+    }
 }
 
 // ---------------------------------------------------------------- rows of a cache
@@ -438,7 +505,7 @@ __device__ __forceinline__ float other_half_max(float v) {
 // 16 bytes a lane from memory to LDS at `lds` + 16 * lane, past the registers.  Not the builtin: for that, the compiler lets every later
 // LDS read wait for all such loads, which leaves one tile under way at most.  Whoever uses the bytes waits for them (wait_tiles) and, where
 // another wave asked for them, meets it at a barrier.
-// With the streaming hint: the caches need not keep what is read once (a copy of 128 MB to LDS by 256 workgroups: 24.4 us, so 19.7).
+// m0 is a reserved register: the compiler keeps nothing in it.  With the streaming hint: the caches need not keep what is read once (a copy of 128 MB to LDS by 256 workgroups: 24.4 us, so 19.7).
 __device__ __forceinline__ void load_to_lds(const uint16_t* from, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(lds), "v"(from) : "memory");
 }
@@ -1117,7 +1184,7 @@ __global__ __launch_bounds__(64 * REDUCE_WAVES) void tree_reduce_kernel(TreeArgs
 
 // ---------------------------------------------------------------- commit
 
-constexpr int COMMIT_LAYERS = 32;          // layers of a launch: their descriptors travel as arguments
+constexpr int COMMIT_LAYERS = 40;          // layers of a launch: their descriptors travel as arguments (4 KB at most)
 constexpr int COMMIT_THREADS = 256;
 
 struct CommitArgs {
@@ -1126,6 +1193,7 @@ struct CommitArgs {
     int32_t max_path;
     CacheArgs layer[COMMIT_LAYERS];
 };
+static_assert(sizeof(CommitArgs) <= 4096, "a launch's arguments");
 
 // One workgroup for a (layer, sequence, KV head): 16 rows at a time are read, then written.  path ascends, so a row that is still to be read lies
 // behind every row written so far.
