@@ -432,11 +432,11 @@ __device__ __forceinline__ int tiles_of(int tokens) { return (tokens + TREE_TILE
 // the first is exact for sequences of one length, the second close for any.  R: one to eight workgroups for each CU; more are better balanced, but
 // each costs about TREE_PIECE_COST tiles besides its own (its start, and partial sums written and read).
 template <bool SPARSE>
-__device__ __forceinline__ int tree_piece(const TreeArgs& a) {                 // tiles; 0: no sequence is cut
+__device__ __forceinline__ int tree_piece(const TreeArgs& a, const TreeSpan& own) {   // tiles; 0: no sequence is cut
     if (a.n_splits == 1) return 0;
     int total = 0, pairs = 0, most = 0, piece = 0;
-    for (int i = threadIdx.x & 63; i < a.batch; i += 64) {
-        const TreeSpan o = tree_span<SPARSE>(a, i);
+    for (int i = threadIdx.x & 63; i < a.batch || (a.batch == 1 && i < 64); i += 64) {   // (of one sequence every lane has the numbers already)
+        const TreeSpan o = a.batch == 1 ? own : tree_span<SPARSE>(a, i);
         const int wgs = a.cache.kv.G * (((o.n << a.g_shift) + TREE_ROWS - 1) / TREE_ROWS), t = tiles_of(o.all);
         total += t * wgs;
         pairs += wgs;
@@ -474,8 +474,9 @@ __device__ __forceinline__ int tree_piece(const TreeArgs& a) {                 /
     return piece > 0 ? piece : most;                              // (0: more sequences than pieces would balance, which stay whole)
 }
 template <bool SPARSE>
-__device__ __forceinline__ TreeSpan tree_work(const TreeArgs& a, int b, int piece) {
+__device__ __forceinline__ TreeSpan tree_work(const TreeArgs& a, int b) {
     TreeSpan s = tree_span<SPARSE>(a, b);
+    int piece = tree_piece<SPARSE>(a, s);
     if (a.n_splits == 1) {
         piece = tiles_of(s.all);
     } else {
@@ -767,20 +768,29 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
     int good = end;                                               // tokens before this one are all there
     if (LIST) {
         const int entries = SPARSE ? steps * TT * TEAMS : (end - begin + PAGE - 1) / PAGE;
-        for (int e = tid; e < entries; e += TREE_THREADS) {
-            int at = -1;
-            if (SPARSE) {
-                const int i = begin + e;
-                if (i < end) {
-                    const int pos = i < s.pre ? a.idx[(int64_t)b * a.budget + i] : s.before + (i - s.pre);
-                    if (i >= s.pre || (uint32_t)pos < (uint32_t)s.before) at = cache_row<PAGED>(a.cache, b, kvh, pos);
-                    if (at < 0) atomicMin(&lds.first_bad, e);
-                }
-            } else {
-                at = cache_row<PAGED>(a.cache, b, kvh, begin + e * PAGE);
-                if (at < 0) atomicMin(&lds.first_bad, e);
+        constexpr int RUN = 4;                                    // entries of a thread under way at once
+        for (int e0 = tid; e0 < entries; e0 += RUN * TREE_THREADS) {
+            int pos[RUN], at[RUN];
+#pragma unroll
+            for (int j = 0; j < RUN; ++j) {
+                const int e = e0 + j * TREE_THREADS, i = SPARSE ? begin + e : begin + e * PAGE;
+                pos[j] = SPARSE ? s.before + (i - s.pre) : i;
+                if (e >= entries || i >= end) pos[j] = -1;
+                else if (SPARSE && i < s.pre) pos[j] = a.idx[(int64_t)b * a.budget + i];
             }
-            lds.list[e] = at;
+#pragma unroll
+            for (int j = 0; j < RUN; ++j) {
+                const int i = begin + e0 + j * TREE_THREADS;
+                at[j] = -1;
+                if (pos[j] >= 0 && (!SPARSE || i >= s.pre || pos[j] < s.before)) at[j] = cache_row<PAGED>(a.cache, b, kvh, pos[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < RUN; ++j) {
+                const int e = e0 + j * TREE_THREADS;
+                if (e >= entries) continue;
+                if (at[j] < 0 && (SPARSE ? begin + e : begin + e * PAGE) < end) atomicMin(&lds.first_bad, e);
+                lds.list[e] = at[j];
+            }
         }
         __syncthreads();
         const int bad = __builtin_amdgcn_readfirstlane(lds.first_bad);
@@ -991,7 +1001,7 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
         if (!idle) any_step();
         it = 1;
         {
-            // Whole blocks, unrolled: the buffers' places are constants of the instructions then, and two steps' registers change places.
+            // Blocks, unrolled: the buffers' places are constants of the instructions then, and two steps' registers change places.
             static_assert(BLOCK == 2 || BLOCK == 4, "the loop's steps");
             uint32_t key[8], value[4];
 #pragma unroll
@@ -1024,12 +1034,25 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
                 ++it;
             };
             const int until = min(plain, steps - 1);              // (a step makes the next tile's scores)
+            auto swap = [&]() {                                   // after an odd number of steps
+                x = y;
+                p = p2;
+            };
 #pragma unroll 1
-            while (it + BLOCK <= until) {
+            while (it < until) {
                 step(std::integral_constant<int, 0>());
+                if (it >= until) {
+                    swap();
+                    break;
+                }
                 step(std::integral_constant<int, 1>());
                 if constexpr (BLOCK == 4) {
+                    if (it >= until) break;
                     step(std::integral_constant<int, 2>());
+                    if (it >= until) {
+                        swap();
+                        break;
+                    }
                     step(std::integral_constant<int, 3>());
                 }
             }
@@ -1069,44 +1092,63 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
     bool any_odd = false;
 #pragma unroll
     for (int i = 0; i < TREE_MAX_NODES / 32; ++i) any_odd |= lds.odd[i] != 0;
-    for (int item = tid; item < ROWS * 32; item += TREE_THREADS) {
-        const int r = item >> 5, c = item & 31, row = row0 + r;
-        if (row >= rows) break;
-        float top = lds.m[r];
+    // (four items of a thread at a time: their reads are under way together)
+    constexpr int ITEMS = ROWS * 32 / TREE_THREADS, RUN = ITEMS < 4 ? ITEMS : 4;
+    static_assert(ITEMS % RUN == 0, "whole runs");
+    const int c = tid & 31;
+#pragma unroll 1
+    for (int i0 = 0; i0 < ITEMS; i0 += RUN) {
+        if (row0 + i0 * (TREE_THREADS / 32) >= rows) break;
+        float top[RUN], sum[RUN];
+        f32x4 v[RUN];
 #pragma unroll
-        for (int w = 1; w < TEAMS; ++w) top = fmaxf(top, lds.m[w * ROWS + r]);
-        float sum = 0.0f;
-        f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = 0; i < RUN; ++i) {
+            const int r = (i0 + i) * (TREE_THREADS / 32) + (tid >> 5);
+            top[i] = lds.m[r];
+            sum[i] = lds.l[r];
+            v[i] = *reinterpret_cast<const f32x4*>(lds.ring + r * (D * 4) + ((c ^ (r & 31)) << 4));
+            if constexpr (TEAMS > 1) {
+                const float own = top[i];
 #pragma unroll
-        for (int w = 0; w < TEAMS; ++w) {
-            sum += lds.l[w * ROWS + r] * exp2f(lds.m[w * ROWS + r] - top);
-            v += *reinterpret_cast<const f32x4*>(lds.ring + (w * ROWS + r) * (D * 4) + ((c ^ (r & 31)) << 4));
-        }
-        if (any_odd) {
-            // Nodes with values that are not finite: the rows that attend to them get those values (whatever the weight: it is not 0).
-            const uint64_t* mask = a.masks + (int64_t)(s.start + (row >> a.g_shift)) * a.words;
-            for (int i = 0; i < s.n; ++i) {
-                if (!(lds.odd[i >> 5] >> (i & 31) & 1) || !(mask[i >> 6] >> (i & 63) & 1)) continue;
-                const int at = cache_row<PAGED>(a.cache, b, kvh, s.before + i);
-                const u32x2 w = *reinterpret_cast<const u32x2*>(a.cache.kv.v + cache_offset<PAGED>(a.cache, b, kvh, max(at, 0)) + c * 4);
+                for (int w = 1; w < TEAMS; ++w) top[i] = fmaxf(top[i], lds.m[w * ROWS + r]);
+                sum[i] *= exp2f(own - top[i]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t x = (j & 1) ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16;
-                    if ((x & 0x7f800000u) == 0x7f800000u) v[j] += __uint_as_float(x);
+                for (int w = 1; w < TEAMS; ++w) {
+                    sum[i] += lds.l[w * ROWS + r] * exp2f(lds.m[w * ROWS + r] - top[i]);
+                    v[i] += *reinterpret_cast<const f32x4*>(lds.ring + (w * ROWS + r) * (D * 4) + ((c ^ (r & 31)) << 4));
                 }
             }
         }
-        const int head = (kvh << a.g_shift) + (row & (g - 1));
-        if (whole) {
-            const int64_t to = (int64_t)(s.start + (row >> a.g_shift)) * a.H + head;
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-            const u32x2 w = {(uint32_t)f32_to_bf16_rne(v[0] * inv) | (uint32_t)f32_to_bf16_rne(v[1] * inv) << 16,
-                             (uint32_t)f32_to_bf16_rne(v[2] * inv) | (uint32_t)f32_to_bf16_rne(v[3] * inv) << 16};
-            *reinterpret_cast<u32x2*>(a.out + to * D + c * 4) = w;
-        } else {
-            const int64_t piece = ((int64_t)(s.part + (row >> a.g_shift)) * a.H + head) * a.n_splits + split;
-            *reinterpret_cast<f32x4*>(a.part_acc + piece * D + c * 4) = v;
-            if (c == 0) *reinterpret_cast<f32x2*>(a.part_ml + piece * 2) = f32x2{top, sum};
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+            const int row = row0 + (i0 + i) * (TREE_THREADS / 32) + (tid >> 5);
+            if (row >= rows) break;
+            if (any_odd) {
+                // Nodes with values that are not finite: the rows that attend to them get those values (whatever the weight: it is not 0).
+                const uint64_t* mask = a.masks + (int64_t)(s.start + (row >> a.g_shift)) * a.words;
+                for (int n = 0; n < s.n; ++n) {
+                    if (!(lds.odd[n >> 5] >> (n & 31) & 1) || !(mask[n >> 6] >> (n & 63) & 1)) continue;
+                    const int at = cache_row<PAGED>(a.cache, b, kvh, s.before + n);
+                    const u32x2 w = *reinterpret_cast<const u32x2*>(a.cache.kv.v + cache_offset<PAGED>(a.cache, b, kvh, max(at, 0)) + c * 4);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t x = (j & 1) ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16;
+                        if ((x & 0x7f800000u) == 0x7f800000u) v[i][j] += __uint_as_float(x);
+                    }
+                }
+            }
+            const int head = (kvh << a.g_shift) + (row & (g - 1));
+            if (whole) {
+                const int64_t to = (int64_t)(s.start + (row >> a.g_shift)) * a.H + head;
+                const float inv = sum[i] == 0.0f ? 0.0f : 1.0f / sum[i];
+                const u32x2 w = {(uint32_t)f32_to_bf16_rne(v[i][0] * inv) | (uint32_t)f32_to_bf16_rne(v[i][1] * inv) << 16,
+                                 (uint32_t)f32_to_bf16_rne(v[i][2] * inv) | (uint32_t)f32_to_bf16_rne(v[i][3] * inv) << 16};
+                *reinterpret_cast<u32x2*>(a.out + to * D + c * 4) = w;
+            } else {
+                const int64_t piece = ((int64_t)(s.part + (row >> a.g_shift)) * a.H + head) * a.n_splits + split;
+                *reinterpret_cast<f32x4*>(a.part_acc + piece * D + c * 4) = v[i];
+                if (c == 0) *reinterpret_cast<f32x2*>(a.part_ml + piece * 2) = f32x2{top[i], sum[i]};
+            }
         }
     }
 }
@@ -1121,7 +1163,7 @@ __global__ __launch_bounds__(TREE_THREADS, 2) void tree_attn_kernel(TreeArgs a) 
     const uint32_t G = a.cache.kv.G, pairs = G * (uint32_t)a.batch, pair = unit % pairs;
     const int split = unit / pairs, b = pair / G, kvh = pair - b * G, row0 = m_tile * TREE_ROWS;
     if (split >= a.n_splits) return;
-    const TreeSpan s = tree_work<SPARSE>(a, b, tree_piece<SPARSE>(a));
+    const TreeSpan s = tree_work<SPARSE>(a, b);
     const int left = (s.n << a.g_shift) - row0, begin = split * s.chunk;
     if (left <= 0 || begin >= s.all) return;
     // (a piece has no more tokens or pages than the list has room for: plan_tree)
