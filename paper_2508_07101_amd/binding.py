@@ -350,10 +350,28 @@ def _need(ok: bool, what: str):
 
 
 def _need_int(what: str, n: int, dtype, *tensors):
-    """Every tensor holds n contiguous numbers of this type at least.  (A step makes these calls once a layer: the message is made when it is needed.)"""
+    """Every tensor holds n contiguous numbers of this type at least, on the GPU.  (A step makes these calls once a layer: the message is made when it is needed.)"""
     for t in tensors:
-        if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
-            raise ValueError(f"{what}: a tensor of {n} or more {dtype}, contiguous, was expected, not {tuple(t.shape)} {t.dtype}")
+        if t.dtype is not dtype or t.numel() < n or not t.is_contiguous() or not t.is_cuda:
+            raise ValueError(f"{what}: a tensor of {n} or more {dtype}, contiguous, on the GPU was expected, not {tuple(t.shape)} {t.dtype} on {t.device}")
+
+
+def _cache_desc(what: str, params: CusaParams, kv: KvCache) -> CusaKv:
+    """The cache's descriptor, as KvCache.desc makes it, if it has the rows that the parameters speak of: kernels write there.  (Each of a step's calls makes
+    one a layer: a tensor is asked once for each thing.)"""
+    k, v, table, lens = kv.k, kv.v, kv.block_table, kv.seq_lens
+    shape, batch, bf16 = k.shape, params.batch, torch.bfloat16
+    if (len(shape) == 4 and v.shape == shape and shape[1] == params.n_kv_heads and shape[3] == params.head_dim and k.dtype is bf16 and v.dtype is bf16
+            and k.is_cuda and v.is_cuda and lens.dtype is torch.int32 and lens.numel() >= batch and lens.is_cuda and lens.is_contiguous()):
+        if table is None:
+            strides = k.stride()
+            if shape[0] >= batch and strides[3] == 1 and strides == v.stride():
+                return CusaKv(k.data_ptr(), v.data_ptr(), KV_CONTIGUOUS, strides[0], strides[1], strides[2], None, 0, 0, 0, lens.data_ptr(), kv.max_seq_len)
+        elif (k.is_contiguous() and v.is_contiguous() and table.dim() == 2 and table.shape[0] >= batch and table.dtype is torch.int32 and table.is_cuda
+                and table.is_contiguous()):
+            return CusaKv(k.data_ptr(), v.data_ptr(), KV_PAGED, 0, 0, 0, table.data_ptr(), table.shape[1], shape[2], shape[0], lens.data_ptr(), kv.max_seq_len)
+    raise ValueError(f"{what}: K and V are bf16 [batch or pages, {params.n_kv_heads}, tokens, {params.head_dim}] of equal strides (pages contiguous), lengths and tables int32 of "
+                     f"{batch} or more sequences, contiguous, all on the GPU; K is {tuple(shape)} {k.dtype} on {k.device}")
 
 
 def kv_plan_workspace_bytes(batch: int) -> int:
@@ -376,9 +394,11 @@ def kv_plan(held, keep, add, lens, tok_start, slots, ws, pool: Optional[PagePool
         d = CusaPool(KV_CONTIGUOUS, n, capacity, None, 0, 0, 0, None, None, None)
     else:
         _need(pool.block_table.shape[0] == n, "kv_plan: a row of the block table for each sequence")
+        _need_int("kv_plan", 2, torch.int32, pool.state, pool.state if state_out is None else state_out)
+        _need_int("kv_plan", 1, torch.int32, pool.block_table, pool.ring)
         d = pool.desc(state_out)
-    _check(load().cusa_kv_plan(ctypes.byref(d), _ptr(held), _ptr(keep), _ptr(add), slots.numel(), _ptr(lens), _ptr(tok_start),
-                               _ptr(slots), _ptr(ws), ws.numel(), _stream()), "cusa_kv_plan")
+    _check(load().cusa_kv_plan(ctypes.byref(d), held.data_ptr(), keep.data_ptr(), add.data_ptr(), slots.numel(), lens.data_ptr(), tok_start.data_ptr(),
+                               slots.data_ptr(), ws.data_ptr(), ws.numel(), _stream()), "cusa_kv_plan")
 
 
 def kv_append(params: CusaParams, kv: KvCache, slots, k_new, v_new):
@@ -386,11 +406,13 @@ def kv_append(params: CusaParams, kv: KvCache, slots, k_new, v_new):
     n, heads, d = k_new.shape
     _need(k_new.dtype in DTYPES and v_new.dtype == k_new.dtype and v_new.shape == k_new.shape and d == params.head_dim and
           heads == params.n_kv_heads, "kv_append: new rows are [n, n_kv_heads, 128] in bf16, fp16 or fp32")
-    _need(k_new.stride(2) == 1 and k_new.stride() == v_new.stride(), "kv_append: K and V rows have the same strides, elements side by side")
+    strides = k_new.stride()
+    _need(strides[2] == 1 and strides == v_new.stride(), "kv_append: K and V rows have the same strides, elements side by side")
+    _need(k_new.is_cuda and v_new.is_cuda, "kv_append: new rows are on the GPU")
     _need_int("kv_append", n, torch.int64, slots)
-    c = kv.desc()
-    r = CusaRows(_ptr(k_new), _ptr(v_new), DTYPES[k_new.dtype], n, k_new.stride(0), k_new.stride(1))
-    _check(load().cusa_kv_append(ctypes.byref(params), ctypes.byref(c), _ptr(slots), ctypes.byref(r), _stream()), "cusa_kv_append")
+    c = _cache_desc("kv_append", params, kv)
+    r = CusaRows(k_new.data_ptr(), v_new.data_ptr(), DTYPES[k_new.dtype], n, strides[0], strides[1])
+    _check(load().cusa_kv_append(ctypes.byref(params), ctypes.byref(c), slots.data_ptr(), ctypes.byref(r), _stream()), "cusa_kv_append")
 
 
 def mask_words(max_nodes: int) -> int:
@@ -406,7 +428,7 @@ def tree_masks(base, tok_start, parents, masks, positions, max_nodes: int):
     _need_int("tree_masks", 2, torch.int32, tok_start)
     _need_int("tree_masks", n, torch.int32, parents, parents if positions is None else positions)
     _need_int("tree_masks", n * mask_words(max_nodes), torch.int64, masks)
-    _check(load().cusa_tree_masks(batch, _ptr(base), _ptr(tok_start), _ptr(parents), n, max_nodes, _ptr(masks),
+    _check(load().cusa_tree_masks(batch, base.data_ptr(), tok_start.data_ptr(), parents.data_ptr(), n, max_nodes, masks.data_ptr(),
                                   _ptr(positions), _stream()), "cusa_tree_masks")
 
 
@@ -432,8 +454,10 @@ def tree_attn(params: CusaParams, q, kv: KvCache, tree: Tree, out, ws, idx=None,
     """Attention of the trees' nodes, q [tokens, H, 128] (a view of a fused projection's rows, or contiguous), over the whole prefix or
     over idx/cnt of it, and over the nodes that the masks name."""
     n, heads, d = q.shape
-    _need(q.dtype == torch.bfloat16 and heads == params.n_q_heads and d == params.head_dim and q.stride(2) == 1 and q.stride(1) == d,
+    strides = q.stride()
+    _need(q.dtype is torch.bfloat16 and heads == params.n_q_heads and d == params.head_dim and strides[2] == 1 and strides[1] == d,
           "tree_attn: q is bf16 [tokens, n_q_heads, 128], heads side by side")
+    _need(q.is_cuda and out.is_cuda, "tree_attn: q and out are on the GPU")
     _need(out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() >= n * heads * d, "tree_attn: out is bf16 [tokens, n_q_heads, 128], contiguous")
     _need_int("tree_attn", params.batch + 1, torch.int32, tree.tok_start)
     _need_int("tree_attn", n * mask_words(tree.max_nodes), torch.int64, tree.masks)
@@ -441,9 +465,9 @@ def tree_attn(params: CusaParams, q, kv: KvCache, tree: Tree, out, ws, idx=None,
         _need_int("tree_attn", params.batch * params.budget, torch.int32, idx)
         _need(cnt is not None, "tree_attn: idx comes with cnt")
         _need_int("tree_attn", params.batch, torch.int32, cnt)
-    c = kv.desc()
-    t = CusaTree(_ptr(tree.tok_start), _ptr(tree.masks), n, tree.max_nodes, q.stride(0))
-    _check(load().cusa_tree_attn(ctypes.byref(params), _ptr(q), ctypes.byref(c), ctypes.byref(t), _ptr(idx), _ptr(cnt), _ptr(out), _ptr(ws),
+    c = _cache_desc("tree_attn", params, kv)
+    t = CusaTree(tree.tok_start.data_ptr(), tree.masks.data_ptr(), n, tree.max_nodes, strides[0])
+    _check(load().cusa_tree_attn(ctypes.byref(params), q.data_ptr(), ctypes.byref(c), ctypes.byref(t), _ptr(idx), _ptr(cnt), out.data_ptr(), ws.data_ptr(),
                                  ws.numel(), _stream()), "cusa_tree_attn")
 
 
@@ -453,14 +477,14 @@ class KvCommit:
     def __init__(self, params: CusaParams, kv_layers: Sequence[KvCache]):
         self.params, self.n = params, len(kv_layers)
         self._keep = list(kv_layers)
-        self.kvs = (CusaKv * self.n)(*[kv.desc() for kv in kv_layers])
+        self.kvs = (CusaKv * self.n)(*[_cache_desc("kv_commit", params, kv) for kv in kv_layers])
 
     def run(self, base, path, n_path, keep=None):
         """Positions base[b] + path[b][i] -> base[b] + i for i < n_path[b]; keep (not base): base + n_path."""
         b = self.params.batch
         _need(path.dim() == 2 and path.shape[0] == b, "kv_commit: path is [batch, nodes]")
         _need_int("kv_commit", b, torch.int32, base, path, n_path, n_path if keep is None else keep)
-        _check(load().cusa_kv_commit(ctypes.byref(self.params), self.n, self.kvs, _ptr(base), _ptr(path), path.shape[1], _ptr(n_path),
+        _check(load().cusa_kv_commit(ctypes.byref(self.params), self.n, self.kvs, base.data_ptr(), path.data_ptr(), path.shape[1], n_path.data_ptr(),
                                      _ptr(keep), _stream()), "cusa_kv_commit")
 
 

@@ -164,3 +164,25 @@ def test_reference_plan_by_hand():
     assert t[0].tolist() == [5, 7, 0, -1] and t[2].tolist() == [1, 3, 4, -1]
     assert slots[:3] == [7 * 16 + 2, 7 * 16 + 3, 7 * 16 + 4] and slots[14] == 0 and slots[15] == 16 and slots[47] == 4 * 16 and slots[48:] == [-1] * 12
     assert s == [6, 2] and r[6] == 6 and r[7] == 2
+
+
+def test_binding_refuses_caches_of_other_shapes_and_host_memory():
+    i32, p = torch.zeros(4, dtype=torch.int32), cb.make_params(2, 8, 8, 1, 0)
+    rows, slots = torch.zeros((2, 8, 128), dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int64)
+
+    def cache(shape, dtype=torch.bfloat16, table=None):
+        return cb.KvCache(torch.zeros(shape, dtype=dtype), torch.zeros(shape, dtype=dtype), i32, 16, table)
+
+    for kv in (cache((2, 4, 16, 128)), cache((1, 8, 16, 128)), cache((2, 8, 16, 64)), cache((2, 8, 16, 128), torch.float16),
+               cache((2, 8, 16, 128)), cache((9, 8, 16, 128), table=torch.zeros((1, 4), dtype=torch.int32))):
+        with pytest.raises(ValueError):
+            cb.KvCommit(p, [kv])
+        with pytest.raises(ValueError):
+            cb.kv_append(p, kv, slots, rows, rows)
+        with pytest.raises(ValueError):
+            cb.tree_attn(p, rows, kv, cb.Tree(i32, torch.zeros((2, 1), dtype=torch.int64), 2), rows, i32)
+    pool = cb.PagePool.empty(2, 3, 5, "cpu")
+    with pytest.raises(ValueError, match="on the GPU"):
+        cb.kv_plan(i32[:2], i32[:2], i32[2:], i32[:2], i32[:3], slots, i32, pool)
+    with pytest.raises(ValueError, match="on the GPU"):
+        cb.tree_masks(i32, i32[:2], i32, torch.zeros((4, 1), dtype=torch.int64), None, 4)
