@@ -21,6 +21,11 @@ enum TreeKind { TREE_FULL, TREE_CHOSEN };
 inline int tree_piece_most(TreeKind kind) { return kind == TREE_CHOSEN ? TREE_LIST : TREE_LIST * 16; }
 inline bool tree_len_served(TreeKind kind, int64_t len) { return len <= (int64_t)tree_piece_most(kind) * TREE_MAX_SPLITS; }
 
+// Tokens up to which sequences stay whole: what a workgroup of up to 64 rows takes in three steps (its teams take 256 or 128 tokens a step), which is less than the
+// merge's launch costs (1 sequence, 4 rows, 300 tokens: whole 11.2 us, in two pieces 13.2; 520: 12.9 and 13.2; 1020, four steps: 16.3 and 14.2; 8 sequences, 64 rows,
+// 300 tokens: 13.9 and 16.1), and for more rows one piece.
+inline int tree_whole(int rows) { return rows <= 32 ? 768 : rows <= 64 ? 384 : TREE_MIN_PIECE; }
+
 struct TreePlan {
     int m_tiles;     // workgroups that share a KV head's tokens
     int n_splits;    // pieces of a sequence's tokens at most; the kernel makes fewer of a short one
@@ -34,7 +39,7 @@ inline TreePlan plan_tree(TreeKind kind, int max_len, int batch, int G, int g, i
     // pieces of the longest alone 1437 us, see tree_work).
     const int64_t wgs = pairs * p.m_tiles, want = batch == 1 ? TREE_CUS / wgs : wgs >= 8 * TREE_CUS ? 1 : std::max<int64_t>(4, 2 * TREE_CUS / wgs);
     const int64_t by_len = ((int64_t)max_len + TREE_MIN_PIECE - 1) / TREE_MIN_PIECE, by_list = ((int64_t)max_len + tree_piece_most(kind) - 1) / tree_piece_most(kind);
-    p.n_splits = (int)std::max<int64_t>({1, by_list, std::min<int64_t>({want, by_len, (int64_t)TREE_MAX_SPLITS})});
+    p.n_splits = (int)std::max<int64_t>({1, by_list, max_len <= tree_whole(max_nodes * g) ? 1 : std::min<int64_t>({want, by_len, (int64_t)TREE_MAX_SPLITS})});
     return p;
 }
 
