@@ -23,8 +23,9 @@ inline bool tree_len_served(TreeKind kind, int64_t len) { return len <= (int64_t
 
 // Tokens up to which sequences stay whole: what a workgroup of up to 64 rows takes in three steps (its teams take 256 or 128 tokens a step), which is less than the
 // merge's launch costs (1 sequence, 4 rows, 300 tokens: whole 11.2 us, in two pieces 13.2; 520: 12.9 and 13.2; 1020, four steps: 16.3 and 14.2; 8 sequences, 64 rows,
-// 300 tokens: 13.9 and 16.1), and for more rows one piece.
-inline int tree_whole(int rows) { return rows <= 32 ? 768 : rows <= 64 ? 384 : TREE_MIN_PIECE; }
+// 300 tokens: 13.9 and 16.1), and for more rows one piece.  Where half of the CUs have a workgroup anyway, up to 1536 tokens (25 sequences of 1064 tokens, 256 rows:
+// 58.9 us cut, 53.5 whole; of 2000: 18 sequences lose, 57 and 64).
+inline int tree_whole(int rows, int64_t wgs) { return std::max(rows <= 32 ? 768 : rows <= 64 ? 384 : TREE_MIN_PIECE, wgs >= TREE_CUS / 2 ? 1536 : 0); }
 
 struct TreePlan {
     int m_tiles;     // workgroups that share a KV head's tokens
@@ -38,8 +39,12 @@ inline TreePlan plan_tree(TreeKind kind, int max_len, int batch, int G, int g, i
     // One sequence: a piece for each CU.  Several: room for as many as make up for their lengths' differences (64 of 8192 to 32768 tokens, 8 KV heads:
     // pieces of the longest alone 1437 us, see tree_work).
     const int64_t wgs = pairs * p.m_tiles, want = batch == 1 ? TREE_CUS / wgs : wgs >= 8 * TREE_CUS ? 1 : std::max<int64_t>(4, 2 * TREE_CUS / wgs);
-    const int64_t by_len = ((int64_t)max_len + TREE_MIN_PIECE - 1) / TREE_MIN_PIECE, by_list = ((int64_t)max_len + tree_piece_most(kind) - 1) / tree_piece_most(kind);
-    p.n_splits = (int)std::max<int64_t>({1, by_list, max_len <= tree_whole(max_nodes * g) ? 1 : std::min<int64_t>({want, by_len, (int64_t)TREE_MAX_SPLITS})});
+    // Where every CU has a workgroup already, pieces only make up for lengths, and room for them costs what starting workgroups without work does: 40 sequences of
+    // 1000 tokens, 256 rows, 130 us with room for pieces of 256, 104 without; of 250 to 4000 tokens 200 and 158.  (Without any up to 8192 another 3 to 6 % at 10000
+    // tokens, but then a single long sequence among short ones holds up the rest.)
+    const int64_t least = wgs >= TREE_CUS ? 4096 : TREE_MIN_PIECE;
+    const int64_t by_len = ((int64_t)max_len + least - 1) / least, by_list = ((int64_t)max_len + tree_piece_most(kind) - 1) / tree_piece_most(kind);
+    p.n_splits = (int)std::max<int64_t>({1, by_list, max_len <= tree_whole(max_nodes * g, wgs) ? 1 : std::min<int64_t>({want, by_len, (int64_t)TREE_MAX_SPLITS})});
     return p;
 }
 

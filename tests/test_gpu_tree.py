@@ -351,6 +351,14 @@ def test_long_prefixes_and_bounds_far_above_the_lengths(budget):
         c.check()
 
 
+@pytest.mark.parametrize("batch,nodes,whole", [(1, 4, 768), (1, 14, 384), (2, 33, 256), (16, 36, 1536), (33, 3, 4096)])
+def test_sequences_about_as_long_as_stay_whole(batch, nodes, whole):
+    """The last length that is one piece, and the first that may be cut: the same bound, and a batch of which one sequence alone is that long."""
+    for length in (whole, whole + 1):
+        _Case("paged", 32, 8, [length - nodes] * batch, [nodes] * batch, 4).check()
+        _Case("head_major", 32, 8, [length - nodes] + [40] * (batch - 1), [nodes] * batch, 4).check()
+
+
 def test_many_sequences():
     rng = np.random.default_rng(8)
     _Case("paged", 32, 8, rng.integers(0, 600, 70), rng.integers(0, 20, 70), 3).check()
