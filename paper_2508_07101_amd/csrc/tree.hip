@@ -216,6 +216,7 @@ cusa_status cusa_tree_attn(const cusa_params* params, const void* q, const cusa_
     a.budget = params->budget;
     a.H = params->n_q_heads;
     a.g_shift = g == 1 ? 0 : g == 2 ? 1 : g == 4 ? 2 : 3;
+    a.tile_rows = pl.rows;
     a.m_tiles = pl.m_tiles;
     a.n_splits = pl.n_splits;
     a.batch = params->batch;

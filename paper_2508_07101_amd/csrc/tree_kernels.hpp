@@ -403,7 +403,7 @@ struct TreeArgs {
     float *part_acc, *part_ml;
     int32_t* pieces;       // of each sequence's tokens, for the merge
     float scale_log2e;
-    int32_t batch, max_tokens, max_nodes, words, budget, H, g_shift, m_tiles, n_splits;
+    int32_t batch, max_tokens, max_nodes, words, budget, H, g_shift, tile_rows /* 128 or 256 */, m_tiles, n_splits;
 };
 
 constexpr int TREE_WAVES = 8, TREE_THREADS = 64 * TREE_WAVES;
@@ -441,7 +441,7 @@ __device__ __forceinline__ int tree_piece(const TreeArgs& a, const TreeSpan& own
     int total = 0, pairs = 0, most = 0, piece = 0;
     for (int i = threadIdx.x & 63; i < a.batch || (a.batch == 1 && i < 64); i += 64) {   // (of one sequence every lane has the numbers already)
         const TreeSpan o = a.batch == 1 ? own : tree_span<SPARSE>(a, i);
-        const int wgs = a.cache.kv.G * (((o.n << a.g_shift) + TREE_ROWS - 1) / TREE_ROWS), t = tiles_of(o.all);
+        const int wgs = a.cache.kv.G * (((o.n << a.g_shift) + a.tile_rows - 1) >> __builtin_ctz(a.tile_rows)), t = tiles_of(o.all);
         total += t * wgs;
         pairs += wgs;
         most = max(most, t);
@@ -1162,8 +1162,7 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
     }
 }
 
-// Which form a workgroup takes goes by the rows that its own tree has, not by the bound: trees of a batch differ.  Workgroups of 128 rows at most make fewer
-// pieces and half the partial sums of few sequences (one of 32768 tokens under 60 nodes 55.5 -> 53.8 us), but read the tiles twice: 64 sequences 1337 -> 1481 us.
+// Which form a workgroup takes goes by the rows that its own tree has, not by the bound: trees of a batch differ.
 template <bool PAGED, bool SPARSE>
 __global__ __launch_bounds__(TREE_THREADS, 2) void tree_attn_kernel(TreeArgs a) {
     __shared__ TreeLds lds;
@@ -1171,10 +1170,10 @@ __global__ __launch_bounds__(TREE_THREADS, 2) void tree_attn_kernel(TreeArgs a) 
     // those that short sequences do not have.
     const uint32_t turn = blockIdx.x >> 3, m_tile = turn % (uint32_t)a.m_tiles, unit = turn / (uint32_t)a.m_tiles * 8 + (blockIdx.x & 7);
     const uint32_t G = a.cache.kv.G, pairs = G * (uint32_t)a.batch, pair = unit % pairs;
-    const int split = unit / pairs, b = pair / G, kvh = pair - b * G, row0 = m_tile * TREE_ROWS;
+    const int split = unit / pairs, b = pair / G, kvh = pair - b * G, row0 = m_tile * a.tile_rows;
     if (split >= a.n_splits) return;
     const TreeSpan s = tree_work<SPARSE>(a, b);
-    const int left = (s.n << a.g_shift) - row0, begin = split * s.chunk;
+    const int left = min((s.n << a.g_shift) - row0, a.tile_rows), begin = split * s.chunk;
     if (left <= 0 || begin >= s.all) return;
     // (a piece has no more tokens or pages than the list has room for: plan_tree)
     const int end = min(begin + s.chunk, s.all);

@@ -13,7 +13,7 @@ constexpr int TREE_MIN_PIECE = 256;     // tokens
 constexpr int TREE_CUS = 256;           // with a workgroup each at a time
 constexpr int TREE_PIECE_COST = 16;     // tiles of 32 tokens that a piece costs besides its own
 
-constexpr int TREE_ROWS = 256;          // rows (node, query head) of one KV head that a workgroup holds at most
+constexpr int TREE_ROWS = 256;          // rows (node, query head) of one KV head that a workgroup has registers for
 
 // Entries of a workgroup's list of cache rows: tokens of a chosen prefix, pages of 16 of a whole one.
 constexpr int TREE_LIST = 5120;
@@ -27,7 +27,27 @@ inline bool tree_len_served(TreeKind kind, int64_t len) { return len <= (int64_t
 // 58.9 us cut, 53.5 whole; of 2000: 18 sequences lose, 57 and 64).
 inline int tree_whole(int rows, int64_t wgs) { return std::max(rows <= 32 ? 768 : rows <= 64 ? 384 : TREE_MIN_PIECE, wgs >= TREE_CUS / 2 ? 1536 : 0); }
 
+// Where every CU has a workgroup already, pieces only make up for lengths, and room for them costs what starting workgroups without work does: 40 sequences of
+// 1000 tokens, 256 rows, 130 us with room for pieces of 256, 104 without; of 250 to 4000 tokens 200 and 158.  (Without any up to 8192 another 3 to 6 % at 10000
+// tokens, but then a single long sequence among short ones holds up the rest.)
+inline int tree_pieces(int rows, int64_t wgs, int max_len) {
+    const int least = wgs >= TREE_CUS ? 4096 : TREE_MIN_PIECE;
+    return max_len <= tree_whole(rows, wgs) ? 1 : (int)(((int64_t)max_len + least - 1) / least);
+}
+
+// Rows of a workgroup.  Half as many of twice as many workgroups where these and all their pieces run at once and sequences are not long: half as many steps
+// for the same tokens (a workgroup's two teams share them) and half the partial sums, but the tiles come twice from L2.  (60 nodes, 4 heads each: 1 sequence of 520
+// tokens 23.2 us, so 18.9; 8000: 34.5 and 28.7; 30000: 57.6 either way; 16 of 2000: 77 and 60; 256 nodes, 4 of 520: 53 and 36.  In more than a round the ones without work,
+// of trees and sequences that differ, leave the last ones waiting: 3 of 2000 under 27 to 62 nodes 32 and 44; 8 of 520 under 256 nodes 61 and 72.)  Where the last
+// workgroup's rows are few, waves that idle in the large form are the cheaper ones from 2048 tokens on (36 nodes: 1 of 2000 24.7 and 20.7, of 30000 47 and 56).
+inline int tree_tile_rows(int rows, int64_t pairs, int batch, int max_len) {
+    const int tiles = (rows + 127) / 128;
+    const int64_t wgs = pairs * tiles, at_once = batch == 1 ? wgs : wgs * tree_pieces(rows, wgs, max_len);   // (one sequence is cut for the CUs that there are)
+    return rows > 128 && at_once <= TREE_CUS && max_len <= (rows > 96 * tiles ? 8192 : 2048) ? 128 : TREE_ROWS;
+}
+
 struct TreePlan {
+    int rows;        // that a workgroup holds at most
     int m_tiles;     // workgroups that share a KV head's tokens
     int n_splits;    // pieces of a sequence's tokens at most; the kernel makes fewer of a short one
 };
@@ -35,16 +55,13 @@ struct TreePlan {
 inline TreePlan plan_tree(TreeKind kind, int max_len, int batch, int G, int g, int max_nodes) {
     const int64_t pairs = (int64_t)batch * G;
     TreePlan p;
-    p.m_tiles = (max_nodes * g + TREE_ROWS - 1) / TREE_ROWS;
+    p.rows = tree_tile_rows(max_nodes * g, pairs, batch, max_len);
+    p.m_tiles = (max_nodes * g + p.rows - 1) / p.rows;
     // One sequence: a piece for each CU.  Several: room for as many as make up for their lengths' differences (64 of 8192 to 32768 tokens, 8 KV heads:
     // pieces of the longest alone 1437 us, see tree_work).
     const int64_t wgs = pairs * p.m_tiles, want = batch == 1 ? TREE_CUS / wgs : wgs >= 8 * TREE_CUS ? 1 : std::max<int64_t>(4, 2 * TREE_CUS / wgs);
-    // Where every CU has a workgroup already, pieces only make up for lengths, and room for them costs what starting workgroups without work does: 40 sequences of
-    // 1000 tokens, 256 rows, 130 us with room for pieces of 256, 104 without; of 250 to 4000 tokens 200 and 158.  (Without any up to 8192 another 3 to 6 % at 10000
-    // tokens, but then a single long sequence among short ones holds up the rest.)
-    const int64_t least = wgs >= TREE_CUS ? 4096 : TREE_MIN_PIECE;
-    const int64_t by_len = ((int64_t)max_len + least - 1) / least, by_list = ((int64_t)max_len + tree_piece_most(kind) - 1) / tree_piece_most(kind);
-    p.n_splits = (int)std::max<int64_t>({1, by_list, max_len <= tree_whole(max_nodes * g, wgs) ? 1 : std::min<int64_t>({want, by_len, (int64_t)TREE_MAX_SPLITS})});
+    const int64_t by_list = ((int64_t)max_len + tree_piece_most(kind) - 1) / tree_piece_most(kind);
+    p.n_splits = (int)std::max<int64_t>({1, by_list, std::min<int64_t>({want, tree_pieces(max_nodes * g, wgs, max_len), TREE_MAX_SPLITS})});
     return p;
 }
 
@@ -56,8 +73,8 @@ struct TreeWs {
 inline TreeWs tree_workspace(TreeKind kind, int max_len, int batch, int H, int G, int max_tokens, int max_nodes) {
     const int g = H / G;
     size_t worst = 0;
-    for (int tiles = 1;; ++tiles) {
-        const int nodes = std::min(max_nodes, tiles * TREE_ROWS / g);
+    for (int rows = 32;; rows += 32) {               // (all that a plan asks of the rows changes behind multiples of 32)
+        const int nodes = std::min(max_nodes, rows / g);
         const TreePlan p = plan_tree(kind, max_len, batch, G, g, nodes);
         const size_t tokens = (size_t)std::min<int64_t>(max_tokens, (int64_t)batch * nodes);
         if (p.n_splits > 1) worst = std::max(worst, tokens * H * p.n_splits);
