@@ -593,28 +593,66 @@ __device__ __forceinline__ void read_values(TreeValues& vf, uint32_t vt, int lan
         for (int d = 0; d < 4; ++d) vf.f[k][d] = read_value(vt + 4096 * k + value_at(lane, d));
 }
 // O^T += V^T P^T: the weights are the product's operand in the order in which the lanes hold them.
+// Up to 64 rows, where memory bounds the time, a weight is two bf16 numbers, f + rest, and takes two products: it is off by 2^-15 of itself at most.  (From
+// 16384 cached tokens on, 64 sequences, this costs 1 % for up to 32 rows and 5 % for 64.)  Above, where the products bound the time, it is one, off by 2^-8 at
+// most, and the row's sum adds up the rounded weights: a token that outweighs the others is rounded alike in both.
 struct TreeWeights {
     bf16x8 f[2];
 };
-template <int K>
-__device__ __forceinline__ void add_values(TreeRow& r, const TreeValues& vf, const TreeWeights& p) {
-#pragma unroll
-    for (int d = 0; d < 4; ++d) r.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf.f[K][d]), p.f[K], r.o[d], 0, 0, 0);
+struct TreeFineWeights {
+    bf16x8 f[2], rest[2];
+};
+__device__ __forceinline__ void add_product(f32x16& o, s16x8 v, const TreeWeights& p, int k) {
+    o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), p.f[k], o, 0, 0, 0);
 }
-__device__ __forceinline__ void add_values(TreeRow& r, const TreeValues& vf, const TreeWeights& p) {
+__device__ __forceinline__ void add_product(f32x16& o, s16x8 v, const TreeFineWeights& p, int k) {
+    o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), p.rest[k], o, 0, 0, 0);
+    o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), p.f[k], o, 0, 0, 0);
+}
+template <int K, typename W>
+__device__ __forceinline__ void add_values(TreeRow& r, const TreeValues& vf, const W& p) {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) add_product(r.o[d], vf.f[K][d], p, K);
+}
+template <typename W>
+__device__ __forceinline__ void add_values(TreeRow& r, const TreeValues& vf, const W& p) {
     add_values<0>(r, vf, p);
     add_values<1>(r, vf, p);
 }
-// The weights 2^(scale x - m), rounded to bf16 for the product (2^-8 of each at most), and their sum in 32 bits.  (The sum by two-element dot products
-// halves its instructions, but these wait for the matrix pipe: a product with two of them takes 53 cycles instead of 32.)
+// A weight 2^(scale x - m).
+__device__ __forceinline__ float weight(float m, float x, float scale_log2e) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, scale_log2e, -m)); }
+// The weights and their sum, in 32 bits.  (Two-element dot products of the rounded weights: one wait for the matrix pipe each, 1 to 2 % of the time for 128 to
+// 512 rows; taking the weights apart again and adding them one by one 5 to 6 %.)
 template <int FROM = 0, int TO = 16>
 __device__ __forceinline__ float weigh(float m, const f32x16& x, float scale_log2e, TreeWeights& p) {
+    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
     float sum = 0.0f;
 #pragma unroll
-    for (int i = FROM; i < TO; ++i) {
-        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], scale_log2e, -m));
-        p.f[i >> 3][i & 7] = (__bf16)w;
-        sum += w;
+    for (int i = FROM; i < TO; i += 2) {
+        const bf16x2 w = {(__bf16)weight(m, x[i], scale_log2e), (__bf16)weight(m, x[i + 1], scale_log2e)};
+        p.f[i >> 3][i & 7] = w[0];
+        p.f[i >> 3][(i & 7) + 1] = w[1];
+        sum = __builtin_amdgcn_fdot2_f32_bf16(w, ones, sum, false);
+    }
+    return sum;
+}
+// f: the weight cut to bf16, less one step; rest: what is missing, a step to two, rounded.  Neither is negative or, from 2^-132 on, 0, so that a value that is
+// infinite stays so in both products.
+__device__ __forceinline__ float weigh(float m, const f32x16& x, float scale_log2e, TreeFineWeights& p) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+        const float w0 = weight(m, x[i], scale_log2e), w1 = weight(m, x[i + 1], scale_log2e);
+        const uint32_t cut = __builtin_amdgcn_perm(__float_as_uint(w1), __float_as_uint(w0), 0x07060302);
+        const uint32_t less = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, cut), u16x2{1, 1}));
+        const bf16x2 f = __builtin_bit_cast(bf16x2, less);
+        p.f[i >> 3][i & 7] = f[0];
+        p.f[i >> 3][(i & 7) + 1] = f[1];
+        p.rest[i >> 3][i & 7] = (__bf16)(w0 - __uint_as_float(less << 16));
+        p.rest[i >> 3][(i & 7) + 1] = (__bf16)(w1 - __uint_as_float(less & 0xffff0000u));
+        sum += w0;
+        sum += w1;
     }
     return sum;
 }
@@ -622,7 +660,8 @@ __device__ __forceinline__ float weigh(float m, const f32x16& x, float scale_log
 // themselves, so that nothing is lost up to there): the weights' sum, which is needed anyway, tells, and no maximum is taken otherwise.
 // From LOWEST, any score does.  NaN scores come here at every step.
 constexpr float TREE_RAISE = 256.0f;
-__device__ __forceinline__ void raise_and_weigh(TreeRow& r, const f32x16& x, float scale_log2e, TreeWeights& p, float sum) {
+template <typename W>
+__device__ __forceinline__ void raise_and_weigh(TreeRow& r, const f32x16& x, float scale_log2e, W& p, float sum) {
     if (__any(!(sum <= TREE_RAISE))) {
         float mx = x[0];
 #pragma unroll
@@ -690,7 +729,8 @@ __device__ __forceinline__ void mask_scores(f32x16& x, uint32_t allowed, int hal
 }
 // Its share of the output.  Values that are not finite must not meet the weight 0 of a row that does not attend to them: those of the tokens in `wash`,
 // which not every row attends to, are left out, and the lane's tokens with such values returned.
-__device__ __forceinline__ uint32_t add_washed(TreeRow& r, const TreeWeights& p, uint32_t vt, uint32_t wash, int lane) {
+template <typename W>
+__device__ __forceinline__ uint32_t add_washed(TreeRow& r, const W& p, uint32_t vt, uint32_t wash, int lane) {
     const int half = lane >> 5;
     uint32_t odd = 0;
     wash >>= 4 * half;
@@ -712,7 +752,7 @@ __device__ __forceinline__ uint32_t add_washed(TreeRow& r, const TreeWeights& p,
                 }
             }
             asm volatile("" ::: "memory");                        // one operand at a time: no registers for more
-            r.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), p.f[k], r.o[d], 0, 0, 0);
+            add_product(r.o[d], __builtin_bit_cast(s16x8, v), p, k);
         }
     return odd << (4 * half);
 }
@@ -877,7 +917,7 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
             if (!idle) {
                 TreeKeys kf;
                 TreeValues vf;
-                TreeWeights p;
+                TreeFineWeights p;
                 read_keys(kf, ring + k_at(it), lane);
                 f32x16 x = score(row, kf);
                 read_values(vf, ring + v_at(it), lane);
@@ -894,7 +934,7 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
             const uint32_t allowed = attended(it, there, common);
             if (!idle && there != 0) {
                 TreeKeys kf;
-                TreeWeights p;
+                TreeFineWeights p;
                 read_keys(kf, ring + k_at(it), lane);
                 f32x16 x = score(row, kf);
                 mask_scores(x, allowed, half);
