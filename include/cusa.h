@@ -320,8 +320,8 @@ cusa_status cusa_tree_masks(int32_t batch, const int32_t* base, const int32_t* t
  * from P on, which the masks speak for, are left out); idx device int32 [batch][budget], cnt[b] in [0, budget].
  * A node that attends to nothing gives zeros.  NaN and infinities in rows that a node does not attend to do not reach its output.
  * Scores and sums are binary32.  A weight is off by 2^-15 of itself at most where a workgroup has up to 64 rows (nodes times query heads of a KV head: a tree
- * of up to 64, the end of a larger one), and rounded to bf16 where it has more, in the product with V as in the sum of weights; weights count as 0 below 2^-126
- * of the row's reference, which is at most 2^8 times smaller than the largest weight.
+ * of up to 64, the end of a larger one), and rounded to bf16 where it has more, in the product with V as in the sum of weights.  Weights
+ * count down to 2^-132 of the row's largest.
  * q: device bf16, row r head h at q + r * q_stride + h * 128; out: device bf16 [max_tokens][n_q_heads][128]; rows of no
  * sequence are not written.  ws: cusa_tree_workspace_bytes, 256-byte aligned, content not preserved.
  * Errors as cusa_full_attn, and UNSUPPORTED for max_nodes > 256, pools of 2^31 or more rows, max_seq_len above 5242880 and, with idx, budget + max_nodes

@@ -76,3 +76,17 @@ def test_few_rows_have_weights_of_fifteen_bits(nodes):
     want, mass = ref.attention(q, k[0].double(), v[0].double(), n - nodes, nodes, ref.allowed(bits, nodes), 128 ** -0.5)
     err, tol = (out.double() - want).abs(), 2.0 ** -12 * mass + 2.0 ** -8 * want.abs()
     assert (err <= tol).all(), f"{int((err > tol).sum())} of {err.numel()}, worst {float((err / tol).max()):.3g} of the bound"
+
+
+@pytest.mark.parametrize("below", [126, 127, 130, 132])
+@pytest.mark.parametrize("B,H,G,nodes", FORMS)
+def test_weights_below_the_normal_range_count(B, H, G, nodes, below):
+    """One token has all the weight and the value 0, another a weight of 2^-below beside it and the value 2^120: the whole output.  In the first one's
+    tile, in a later one of the same team, in another team's, and (1100 tokens) in another piece."""
+    for n, heavy, light in ((40 + nodes, 3, 30), (300 + nodes, 3, 270), (300 + nodes, 3, 40), (300 + nodes, 270, 3), (1100 + nodes, 3, 1090), (1100 + nodes, 900, 3)):
+        c = torch.full((n,), -200.0)
+        c[heavy], c[light] = 0.0, -float(below)
+        v = torch.zeros((n, 128))
+        v[light] = 2.0 ** 120
+        out = _tokens(B, H, G, nodes, torch.ones((B * nodes, H)), c, v)
+        assert (out.float() == 2.0 ** (120 - below)).all(), (n, heavy, light, out.float().amin().item(), out.float().amax().item())
