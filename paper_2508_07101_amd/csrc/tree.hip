@@ -117,7 +117,9 @@ cusa_status cusa_kv_plan(const cusa_pool* pool, const int32_t* held, const int32
     }
     launch(KID_KV_PLAN, kv_plan_kernel<false>, 1, PLAN_THREADS, 0, s, a);
     if (launch_status() != CUSA_OK) return CUSA_ERR_LAUNCH;
-    const int64_t wgs = std::min<int64_t>(((int64_t)max_tokens + FILL_THREADS * FILL_RUN - 1) / (FILL_THREADS * FILL_RUN), 2048);
+    // enough for the tokens, and a workgroup a sequence for the pages that go back, also where no token comes
+    const int64_t by_tokens = ((int64_t)max_tokens + FILL_THREADS * FILL_RUN - 1) / (FILL_THREADS * FILL_RUN);
+    const int64_t wgs = std::min<int64_t>(std::max<int64_t>({by_tokens, paged ? pool->batch : 1, 1}), 2048);
     launch(KID_KV_FILL, kv_fill_kernel, dim3((unsigned)wgs), FILL_THREADS, 0, s, a);
     return launch_status();
 }
