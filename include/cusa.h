@@ -302,7 +302,7 @@ typedef struct {
     const int32_t*  tok_start;      /* device [batch + 1]; rows per sequence at most max_nodes                */
     const uint64_t* masks;          /* device [max_tokens][ceil(max_nodes / 64)]: bit i of row r: this node attends to node i of
                                      * its sequence.  Any bits: a node need not attend to itself                */
-    int32_t         max_tokens;     /* rows of the packed arrays                                              */
+    int32_t         max_tokens;     /* rows of the packed arrays, 1 or more                                   */
     int32_t         max_nodes;      /* 1 .. 256                                                               */
     int64_t         q_stride;       /* elements between two rows of q, a multiple of 8 and >= n_q_heads * 128  */
 } cusa_tree;

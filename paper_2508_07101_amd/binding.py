@@ -428,6 +428,8 @@ def tree_masks(base, tok_start, parents, masks, positions, max_nodes: int):
     _need_int("tree_masks", 2, torch.int32, tok_start)
     _need_int("tree_masks", n, torch.int32, parents, parents if positions is None else positions)
     _need_int("tree_masks", n * mask_words(max_nodes), torch.int64, masks)
+    if n == 0:                                               # a step in which nothing was drafted
+        return
     _check(load().cusa_tree_masks(batch, base.data_ptr(), tok_start.data_ptr(), parents.data_ptr(), n, max_nodes, masks.data_ptr(),
                                   _ptr(positions), _stream()), "cusa_tree_masks")
 
@@ -466,6 +468,8 @@ def tree_attn(params: CusaParams, q, kv: KvCache, tree: Tree, out, ws, idx=None,
         _need(cnt is not None, "tree_attn: idx comes with cnt")
         _need_int("tree_attn", params.batch, torch.int32, cnt)
     c = _cache_desc("tree_attn", params, kv)
+    if n == 0:
+        return
     t = CusaTree(tree.tok_start.data_ptr(), tree.masks.data_ptr(), n, tree.max_nodes, strides[0])
     _check(load().cusa_tree_attn(ctypes.byref(params), q.data_ptr(), ctypes.byref(c), ctypes.byref(t), _ptr(idx), _ptr(cnt), out.data_ptr(), ws.data_ptr(),
                                  ws.numel(), _stream()), "cusa_tree_attn")

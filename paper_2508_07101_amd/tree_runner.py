@@ -66,6 +66,8 @@ class TreeRunner:
         """The nodes' rows into the layer's cache, and their attention: over the whole prefix, or in a sparse layer over what the last selection
         layer chose for the trees' first nodes."""
         kv, kind = self.kvs[layer], self.schedule[layer]
+        if q.shape[0] == 0:
+            return
         cb.kv_append(self.params, kv, self.slots[: q.shape[0]], k_new, v_new)
         if kind == cb.LAYER_SELECT:
             rows = self.tok_start[:-1].clamp(max=q.shape[0] - 1)
