@@ -15,9 +15,9 @@ from . import binding as cb
 class TreeRunner:
     """A paged cache of several layers and the speculative steps on it.
 
-    A step is ``draft``, then ``layer`` for each layer in order, then ``accept``.  Prompts come in by ``admit`` (and ``append`` for each
-    layer).  Everything is enqueued on the current stream; nothing here waits for the GPU.  A sequence whose new tokens find no room has no rows
-    (``tok_start`` tells), so a caller whose pool may run out looks at it before it packs rows.
+    A step is ``draft`` (or ``room`` and ``trees``), then ``layer`` for each layer in order, then ``accept``.  Prompts come in by ``admit`` (and ``append`` for each
+    layer).  Everything is enqueued on the current stream; nothing here waits for the GPU.  A sequence whose new tokens find no room has no rows:
+    ``tok_start`` tells, and a caller whose pool may run out looks at it after ``draft`` (or ``admit``), before it packs the rows of q, K and V.
     """
 
     def __init__(self, params: cb.CusaParams, schedule: Sequence[int], n_pages: int, max_pages: int, max_tokens: int, max_nodes: int, device="cuda"):
@@ -33,6 +33,7 @@ class TreeRunner:
         self.slots = torch.full((max_tokens,), -1, dtype=torch.int64, device=device)
         self.masks = torch.zeros((max_tokens, cb.mask_words(max_nodes)), dtype=torch.int64, device=device)
         self.positions = ints(max_tokens)
+        self.rows = torch.arange(max_tokens, dtype=torch.int32, device=device)
         self.idx, self.cnt = ints(b, params.budget), ints(b)
         shape, self.max_len = (n_pages, g, 16, params.head_dim), 16 * max_pages
         # zeros, not whatever memory holds: rows of a page behind a sequence's end are read as parts of tiles
@@ -53,14 +54,35 @@ class TreeRunner:
     def append(self, layer: int, slots: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor):
         cb.kv_append(self.params, self.kvs[layer], slots, k_new, v_new)
 
-    def draft(self, nodes: torch.Tensor, parents: torch.Tensor) -> torch.Tensor:
-        """nodes[b] drafted tokens for sequence b, their parents packed; what the step before did not accept goes back.  Returns the positions."""
-        n = parents.numel()
+    def room(self, nodes: torch.Tensor, n: int) -> torch.Tensor:
+        """Room for nodes[b] drafted tokens of sequence b, n of all at most; what the step before did not accept goes back.  Returns tok_start: a sequence
+        without room has no rows."""
+        if n > self.slots.numel():
+            raise ValueError(f"{n} drafted tokens, room for {self.slots.numel()}")
         cb.kv_plan(self.lens, self.keep, nodes, self.lens, self.tok_start, self.slots[:n], self.plan_ws, self.pool)
-        cb.tree_masks(self.keep, self.tok_start, parents, self.masks[:n], self.positions[:n], self.max_nodes)
         torch.minimum(self.keep + 1, self.lens, out=self.first)
+        return self.tok_start
+
+    def trees(self, parents: torch.Tensor) -> torch.Tensor:
+        """The trees of the sequences that have room, by their nodes' parents, packed as tok_start says.  Returns the positions."""
+        n = parents.numel()
+        cb.tree_masks(self.keep, self.tok_start, parents, self.masks[:n], self.positions[:n], self.max_nodes)
         self.tree = cb.Tree(self.tok_start, self.masks[:n], self.max_nodes)
         return self.positions[:n]
+
+    def draft(self, nodes: torch.Tensor, parents: torch.Tensor) -> torch.Tensor:
+        """room and trees in one, without a look at what was granted: the parents are packed as they were asked for, nodes[b] of sequence b, and those of
+        sequences without room are left out (by torch, some 30 to 60 us of a step in which the GPU waits for the host; where nothing can be refused, room and
+        trees do without).  Returns the positions, packed as tok_start says (what is behind the last row is not defined)."""
+        n = parents.numel()
+        start = self.room(nodes, n)
+        if n > 0:
+            asked = nodes.clamp(min=0)
+            ahead = asked.cumsum(0, dtype=torch.int32) - asked - start[:-1]       # rows of sequences without room before each one's own
+            rows = self.rows[:n]
+            own = torch.searchsorted(start[1:], rows, right=True, out_int32=True).clamp(max=len(ahead) - 1)
+            parents = parents[(rows + ahead[own]).clamp(max=n - 1)]
+        return self.trees(parents)
 
     def layer(self, layer: int, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, out: torch.Tensor):
         """The nodes' rows into the layer's cache, and their attention: over the whole prefix, or in a sparse layer over what the last selection
@@ -113,7 +135,8 @@ def demo(batch: int = 4, prompt: int = 4000, nodes: int = 32, steps: int = 8, de
     for step in range(steps):
         if step == 1:                                                            # (the first one loads the kernels)
             start.record()
-        r.draft(most, parents)
+        r.room(most, len(parents))                                               # (there are pages for all steps: nothing is refused)
+        r.trees(parents)
         for i in range(len(schedule)):
             r.layer(i, q, k, v, out)
         r.accept(path, taken)

@@ -50,3 +50,47 @@ def test_a_step_in_which_nothing_is_drafted():
     torch.cuda.synchronize()
     assert r.lens.tolist() == r.keep.tolist() == [41, 17] and r.tok_start.tolist() == [0, 0, 0]
     assert r.pool.state.tolist()[1] == 12 - 3 - 2
+
+
+@pytest.mark.parametrize("split", [False, True])
+def test_trees_of_the_others_where_one_finds_no_room(split):
+    """Sequences of 16, 17, 0 and 33 tokens ask for 64, 3, 0 and 15 nodes with two free pages: the first is refused, the others need none.  The parents
+    are packed as they were asked for (draft), or as they were granted (room, then trees)."""
+    H, G, schedule = 8, 2, [cb.LAYER_FULL, cb.LAYER_SELECT, cb.LAYER_SPARSE]
+    prompts, asked = [16, 17, 0, 33], [64, 3, 0, 15]
+    r, kept = _started(prompts, 1 + 2 + 3 + 2, 8, 100, 64, schedule)
+    rng = np.random.default_rng(2)
+    parents = [[int(rng.integers(-1, j)) if j else -1 for j in range(n)] for n in asked]
+    granted = [0, 3, 0, 15]
+    if split:
+        assert r.room(_i32(asked), sum(asked)).tolist() == [0, 0, 3, 3, 18]
+        positions = r.trees(_i32(parents[1] + parents[3]))
+    else:
+        positions = r.draft(_i32(asked), _i32(sum(parents, [])))
+    assert r.tok_start.tolist() == [0, 0, 3, 3, 18] and r.lens.tolist() == [16, 20, 0, 48]
+    bits, depth = zip(*[ref.masks(p, 1) for p in parents])
+    assert positions[:18].tolist() == [17 + d for d in depth[1]] + [33 + d for d in depth[3]]
+    assert r.masks[:18].cpu().numpy().view(np.uint64).tolist() == np.concatenate([bits[1], bits[3]]).tolist()
+    q, k, v = _rows(18, H, G, 7)
+    at = np.concatenate([[0], np.cumsum(prompts)])
+    for i, kind in enumerate(schedule):
+        out = torch.full((18, H, 128), 7.0, dtype=torch.bfloat16, device=DEV)
+        r.layer(i, q, k, v, out)
+        torch.cuda.synchronize()
+        for b, own in ((1, slice(0, 3)), (3, slice(3, 18))):
+            old = [x[at[b]: at[b + 1]] for x in kept[i]]
+            seen = torch.arange(prompts[b], device=DEV)
+            if kind == cb.LAYER_SPARSE:
+                seen = r.idx[b, : int(r.cnt[b])].long()
+                seen = seen[seen < prompts[b]]
+            kk, vv = (torch.cat([c[seen], x[own]]).transpose(0, 1).double() for c, x in zip(old, (k, v)))
+            want, mass = ref.attention(q[own], kk, vv, len(seen), granted[b], ref.allowed(bits[b], granted[b]), 128 ** -0.5)
+            ref.assert_attention(out[own], want, mass, f"layer {i} sequence {b}")
+
+
+def test_more_nodes_than_the_runner_has_rows_for_change_nothing():
+    r, _ = _started([16, 17], 8, 8, 10, 64, [cb.LAYER_FULL])
+    state = r.pool.state.tolist()
+    with pytest.raises(ValueError, match="room for 10"):
+        r.draft(_i32([6, 6]), _i32([-1] * 12))
+    assert r.pool.state.tolist() == state and r.lens.tolist() == [16, 17]
