@@ -98,8 +98,9 @@ class TreeRunner:
         cb.tree_attn(self.params, q, kv, self.tree, out, self.tree_ws, self.idx if sparse else None, self.cnt if sparse else None)
 
     def accept(self, path: torch.Tensor, n_path: torch.Tensor):
-        """The accepted nodes of each tree, ascending (path [batch, most], n_path of them): their rows move together in all layers."""
-        self.commit.run(self.keep, path, n_path, self.kept)
+        """The accepted nodes of each tree, ascending (path [batch, most], n_path of them): their rows move together in all layers.  A sequence that had no
+        room has no nodes to accept, whatever n_path says: behind its tokens, its table names pages that may be another one's by now."""
+        self.commit.run(self.keep, path, torch.minimum(n_path, self.lens - self.keep), self.kept)
         self.keep.copy_(self.kept)
 
 

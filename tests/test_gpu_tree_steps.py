@@ -94,3 +94,32 @@ def test_more_nodes_than_the_runner_has_rows_for_change_nothing():
     with pytest.raises(ValueError, match="room for 10"):
         r.draft(_i32([6, 6]), _i32([-1] * 12))
     assert r.pool.state.tolist() == state and r.lens.tolist() == [16, 17]
+
+
+def test_a_sequence_without_room_accepts_nothing():
+    """The second sequence gives its two pages back, the first one gets them, the second one is refused and accepts three nodes all the same: its table
+    still names the pages, and the first one's rows in them stay as they are."""
+    r, _ = _started([16, 16], 4, 8, 100, 64, [cb.LAYER_FULL, cb.LAYER_FULL])
+    chain = list(range(-1, 63))
+    r.draft(_i32([0, 20]), _i32(chain[:20]))
+    r.accept(_i32([[0], [0]]), _i32([0, 0]))
+    r.draft(_i32([0, 0]), torch.empty(0, dtype=torch.int32, device=DEV))
+    r.draft(_i32([20, 64]), _i32(chain[:20] + chain))
+    assert r.tok_start.tolist() == [0, 20, 20] and r.pool.block_table[0, 1:3].tolist() == r.pool.block_table[1, 1:3].tolist()
+    new = [_rows(20, 8, 2, 50 + i)[1:] for i in range(2)]
+    before = []
+    for i, (k, v) in enumerate(new):
+        r.append(i, r.slots[:20], k, v)
+        before.append((r.kvs[i].k.clone(), r.kvs[i].v.clone()))
+    r.accept(_i32([[1, 4, 0], [3, 4, 5]]), _i32([2, 3]))
+    torch.cuda.synchronize()
+    page = int(r.pool.block_table[0, 1])
+    for kv, new_rows, old in zip(r.kvs, new, before):
+        for x, rows, want in zip((kv.k, kv.v), new_rows, old):
+            want[page, :, 0], want[page, :, 1] = rows[1], rows[4]
+            assert torch.equal(x, want)
+    assert r.keep.tolist() == [18, 16]
+    # and the next steps start from there (the page that the first one gives back comes to the second one a call later)
+    assert r.draft(_i32([3, 2]), _i32([-1, 0, 1, -1, 0]))[:3].tolist() == [18, 19, 20] and r.tok_start.tolist() == [0, 3, 3]
+    r.accept(_i32([[0], [0]]), _i32([0, 1]))
+    assert r.draft(_i32([3, 2]), _i32([-1, 0, 1, -1, 0])).tolist() == [18, 19, 20, 16, 17]
