@@ -86,7 +86,7 @@ typedef struct {
  * paged:      pools are [n_pages][n_kv_heads][page_size][128]; logical token t of
  *             sequence b lives in pool page block_table[b*max_pages + t/page_size],
  *             slot t % page_size.
- * seq_lens[b] = L_b >= 1 counts the token appended in this step (Alg. 1 appends
+ * seq_lens[b] = L_b >= 1 (0 where a call says so) counts the token appended in this step (Alg. 1 appends
  * before attending); max_seq_len is a host-side bound L_b <= max_seq_len used
  * to size grids and workspace. */
 typedef struct {
@@ -136,7 +136,8 @@ cusa_status cusa_workspace_layout(const cusa_params* params, int32_t max_seq_len
 
 /* Token selection of a selection layer (Alg. 1, the lines that build rho;
  * Sec. 3.2 and 3.3).  For each sequence b with L = seq_lens[b]:
- *   L <= K : rho = {0 .. L-1}
+ *   L <= K : rho = {0 .. L-1}; L = 0, an empty place of the batch, is served here: cnt is 0
+ *            and nothing of the sequence is read
  *   else   : P = q.K^T (unscaled, binary32, summed left to right over d) for
  *            tokens [0, L-W); every head ranks its min(k, L-W-n_sink) best tokens
  *            of [n_sink, L-W) by (score descending, position ascending); the

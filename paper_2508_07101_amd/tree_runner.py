@@ -18,6 +18,7 @@ class TreeRunner:
     A step is ``draft`` (or ``room`` and ``trees``), then ``layer`` for each layer in order, then ``accept``.  Prompts come in by ``admit`` (and ``append`` for each
     layer).  Everything is enqueued on the current stream; nothing here waits for the GPU.  A sequence whose new tokens find no room has no rows:
     ``tok_start`` tells, and a caller whose pool may run out looks at it after ``draft`` (or ``admit``), before it packs the rows of q, K and V.
+    Places of the batch may be empty.  A sequence ends when its entry of ``keep`` is set to 0: the next plan takes its pages back.
     """
 
     def __init__(self, params: cb.CusaParams, schedule: Sequence[int], n_pages: int, max_pages: int, max_tokens: int, max_nodes: int, device="cuda"):

@@ -123,3 +123,73 @@ def test_a_sequence_without_room_accepts_nothing():
     assert r.draft(_i32([3, 2]), _i32([-1, 0, 1, -1, 0]))[:3].tolist() == [18, 19, 20] and r.tok_start.tolist() == [0, 3, 3]
     r.accept(_i32([[0], [0]]), _i32([0, 1]))
     assert r.draft(_i32([3, 2]), _i32([-1, 0, 1, -1, 0])).tolist() == [18, 19, 20, 16, 17]
+
+
+@pytest.mark.parametrize("mode", [cb.RANK_FIRST_OCCURRENCE, cb.RANK_VOTES, cb.RANK_MAX_SCORE])
+@pytest.mark.parametrize("bound", [64, 4096, 200000])
+def test_selection_over_empty_places(mode, bound):
+    """Sequences of no tokens, without pages, among others: an empty set, and the others' sets as on their own."""
+    B, H, G, lens = 5, 8, 2, [0, 300, 0, 20, 0] if bound > 64 else [0, 30, 0, 20, 0]
+    pages = [ref.pages(n) for n in lens]
+    table = np.full((B, ref.pages(bound)), -1)
+    for b, n in enumerate(pages):
+        table[b, :n] = sum(pages[:b]) + np.arange(n)
+    k, v = (torch.randn((sum(pages), G, 16, 128), device=DEV).to(torch.bfloat16) for _ in range(2))
+    q = torch.randn((B, H, 128), device=DEV).to(torch.bfloat16)
+    sets = []
+    for own in ([0, 1, 2, 3, 4], [1, 3]):
+        params = cb.make_params(len(own), H, G, 64, 16, rank_mode=mode)
+        idx, cnt = torch.full((len(own), 64), -7, dtype=torch.int32, device=DEV), torch.full((len(own),), -7, dtype=torch.int32, device=DEV)
+        kv = cb.KvCache(k, v, _i32([lens[b] for b in own]), bound, _i32(table[own]))
+        print("select", mode, bound, own, flush=True)
+        cb.select(params, q[own].contiguous(), kv, idx, cnt, cb.alloc_workspace(params, bound))
+        torch.cuda.synchronize()
+        sets.append((idx.tolist(), cnt.tolist()))
+    assert sets[0][1] == [0, min(lens[1], 64), 0, 20, 0] and sets[1][1] == [min(lens[1], 64), 20]
+    for i, b in enumerate((1, 3)):
+        assert sets[0][0][b][: sets[0][1][b]] == sets[1][0][i][: sets[1][1][i]]
+    assert all(t == -7 for b in (0, 2, 4) for t in sets[0][0][b])
+
+
+def test_a_sequence_ends_and_another_takes_its_place():
+    """Empty places before, beside and after: through all kinds of layers, and every page comes back."""
+    schedule = [cb.LAYER_FULL, cb.LAYER_SELECT, cb.LAYER_SPARSE]
+    r, kept = _started([0, 50, 40], 12, 6, 40, 20, schedule)
+    for step, (asked, held) in enumerate([([0, 4, 3], [0, 50, 40]), ([0, 0, 3], [0, 0, 40]), ([0, 0, 0], [0, 0, 0]), ([2, 0, 0], [30, 0, 0])]):
+        if step == 1:
+            r.keep[1] = 0
+        if step == 2:
+            r.keep[2] = 0
+        if step == 3:
+            slots = torch.empty(30, dtype=torch.int64, device=DEV)
+            r.admit(_i32([30, 0, 0]), slots)
+            kept = []
+            for i in range(3):
+                _, k, v = _rows(30, 8, 2, 70 + i)
+                r.append(i, slots, k, v)
+                kept.append((k, v))
+        n = sum(asked)
+        positions = r.draft(_i32(asked), _i32(sum([list(range(-1, a - 1)) for a in asked], [])))
+        assert positions.tolist() == [h + j for h, a in zip(held, asked) for j in range(a)]
+        q, k, v = _rows(n, 8, 2, step)
+        for i, kind in enumerate(schedule):
+            out = torch.full((n, 8, 128), float("nan"), dtype=torch.bfloat16, device=DEV)
+            r.layer(i, q, k, v, out)
+            torch.cuda.synchronize()
+            at = 0
+            for b, a in enumerate(asked):
+                if a == 0:
+                    continue
+                old = kept[i] if step == 3 else [x[:50] if b == 1 else x[50:] for x in kept[i]]
+                seen = torch.arange(held[b], device=DEV)
+                if kind == cb.LAYER_SPARSE:
+                    seen = r.idx[b, : int(r.cnt[b])].long()
+                    seen = seen[seen < held[b]]
+                kk, vv = (torch.cat([c[seen], x[at: at + a]]).transpose(0, 1).double() for c, x in zip(old, (k, v)))
+                want, mass = ref.attention(q[at: at + a], kk, vv, len(seen), a, np.tril(np.ones((a, a), dtype=bool)), 128 ** -0.5)
+                ref.assert_attention(out[at: at + a], want, mass, f"step {step} layer {i} sequence {b}")
+                at += a
+        r.accept(_i32([[0]] * 3), _i32([0, 0, 0]))
+    r.keep.zero_()
+    r.draft(_i32([0, 0, 0]), torch.empty(0, dtype=torch.int32, device=DEV))
+    assert r.pool.state.tolist()[1] == 12 and sorted(r.pool.ring.tolist()) == list(range(12))
