@@ -319,7 +319,9 @@ cusa_status cusa_tree_masks(int32_t batch, const int32_t* base, const int32_t* t
  * (cusa_kv_append comes first), P = L - n:  Eq. 1 restricted to the positions t < P and to P + i for the bits i of its mask.
  * idx, cnt (both or neither): of the prefix only idx[b][0 .. cnt[b]) (as cusa_select makes them for the tree's first node: entries
  * from P on, which the masks speak for, are left out); idx device int32 [batch][budget], cnt[b] in [0, budget].
- * A node that attends to nothing gives zeros.  NaN and infinities in rows that a node does not attend to do not reach its output.
+ * A node that attends to nothing gives zeros.  NaN and infinities in rows that a node does not attend to do not reach its output; an infinite value of
+ * a node that it attends to makes its output infinite whatever the weight, one of the prefix does if the weight is not below 2^-126 of the row's largest (else
+ * infinite or NaN).
  * Scores and sums are binary32.  A weight is off by 2^-15 of itself at most where a workgroup has up to 64 rows (nodes times query heads of a KV head: a tree
  * of up to 64, the end of a larger one), and rounded to bf16 where it has more, in the product with V as in the sum of weights.  Weights
  * count down to 2^-132 of the row's largest.

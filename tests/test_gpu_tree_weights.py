@@ -90,3 +90,18 @@ def test_weights_below_the_normal_range_count(B, H, G, nodes, below):
         v[light] = 2.0 ** 120
         out = _tokens(B, H, G, nodes, torch.ones((B * nodes, H)), c, v)
         assert (out.float() == 2.0 ** (120 - below)).all(), (n, heavy, light, out.float().amin().item(), out.float().amax().item())
+
+
+@pytest.mark.parametrize("before", [40, 300, 1100, 5000])
+@pytest.mark.parametrize("B,H,G,nodes", FORMS)
+def test_infinite_values_of_nodes_whatever_their_piece_weighs(B, H, G, nodes, before):
+    """A token of the prefix outweighs the nodes by 2^200, more than 32 bits hold: an infinite value of the last node is the output of the last node all the
+    same, in one piece (up to 300 tokens) as in several, and reaches no other node."""
+    c = torch.full((before + nodes,), -200.0)
+    c[3] = 0.0
+    v = torch.ones((len(c), 128))
+    v[-1, 5:90:3], v[-1, 6:90:3] = float("inf"), -float("inf")
+    out = _tokens(B, H, G, nodes, torch.ones((B * nodes, H)), c, v).float().view(B, nodes, H, 128)
+    want = torch.ones((nodes, 128), device=DEV)
+    want[-1] = torch.where(v[-1].isinf(), v[-1], torch.ones(128)).to(DEV)
+    assert torch.equal(out, want[None, :, None].expand_as(out))
