@@ -365,13 +365,14 @@ def _cache_desc(what: str, params: CusaParams, kv: KvCache) -> CusaKv:
             and k.is_cuda and v.is_cuda and lens.dtype is torch.int32 and lens.numel() >= batch and lens.is_cuda and lens.is_contiguous()):
         if table is None:
             strides = k.stride()
-            if shape[0] >= batch and strides[3] == 1 and strides == v.stride():
+            if shape[0] >= batch and strides[3] == 1 and strides == v.stride() and kv.max_seq_len <= shape[2]:
                 return CusaKv(k.data_ptr(), v.data_ptr(), KV_CONTIGUOUS, strides[0], strides[1], strides[2], None, 0, 0, 0, lens.data_ptr(), kv.max_seq_len)
         elif (k.is_contiguous() and v.is_contiguous() and table.dim() == 2 and table.shape[0] >= batch and table.dtype is torch.int32 and table.is_cuda
                 and table.is_contiguous()):
             return CusaKv(k.data_ptr(), v.data_ptr(), KV_PAGED, 0, 0, 0, table.data_ptr(), table.shape[1], shape[2], shape[0], lens.data_ptr(), kv.max_seq_len)
     raise ValueError(f"{what}: K and V are bf16 [batch or pages, {params.n_kv_heads}, tokens, {params.head_dim}] of equal strides (pages contiguous), lengths and tables int32 of "
-                     f"{batch} or more sequences, contiguous, all on the GPU; K is {tuple(shape)} {k.dtype} on {k.device}")
+                     f"{batch} or more sequences, contiguous, all on the GPU, max_seq_len at most the tokens of a contiguous cache; K is {tuple(shape)} {k.dtype} on {k.device}, "
+                     f"max_seq_len {kv.max_seq_len}")
 
 
 def kv_plan_workspace_bytes(batch: int) -> int:
