@@ -356,6 +356,11 @@ def _need_int(what: str, n: int, dtype, *tensors):
             raise ValueError(f"{what}: a tensor of {n} or more {dtype}, contiguous, on the GPU was expected, not {tuple(t.shape)} {t.dtype} on {t.device}")
 
 
+def _need_workspace(what: str, ws: torch.Tensor):
+    if ws.dtype is not torch.uint8 or not ws.is_contiguous() or not ws.is_cuda:
+        raise ValueError(f"{what}: a workspace of uint8, contiguous, on the GPU was expected, not {tuple(ws.shape)} {ws.dtype} on {ws.device}")
+
+
 def _cache_desc(what: str, params: CusaParams, kv: KvCache) -> CusaKv:
     """The cache's descriptor, as KvCache.desc makes it, if it has the rows that the parameters speak of: kernels write there.  (Each of a step's calls makes
     one a layer: a tensor is asked once for each thing.)"""
@@ -391,6 +396,7 @@ def kv_plan(held, keep, add, lens, tok_start, slots, ws, pool: Optional[PagePool
     _need_int("kv_plan", n, torch.int32, held, keep, add, lens)
     _need_int("kv_plan", n + 1, torch.int32, tok_start)
     _need_int("kv_plan", 0, torch.int64, slots)
+    _need_workspace("kv_plan", ws)
     if pool is None:
         d = CusaPool(KV_CONTIGUOUS, n, capacity, None, 0, 0, 0, None, None, None)
     else:
@@ -462,6 +468,7 @@ def tree_attn(params: CusaParams, q, kv: KvCache, tree: Tree, out, ws, idx=None,
           "tree_attn: q is bf16 [tokens, n_q_heads, 128], heads side by side")
     _need(q.is_cuda and out.is_cuda, "tree_attn: q and out are on the GPU")
     _need(out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() >= n * heads * d, "tree_attn: out is bf16 [tokens, n_q_heads, 128], contiguous")
+    _need_workspace("tree_attn", ws)
     _need_int("tree_attn", params.batch + 1, torch.int32, tree.tok_start)
     _need_int("tree_attn", n * mask_words(tree.max_nodes), torch.int64, tree.masks)
     if idx is not None:

@@ -54,3 +54,15 @@ def _attn(kv=None, tree=None, idx=None, cnt=None, ws=None):
 def test_bounds_beyond_a_contiguous_cache(call, layout):
     with pytest.raises(ValueError, match="33"):
         call(_cache(32, 33, layout=layout))
+
+
+def _plan(ws):
+    cb.kv_plan(_i32(2), _i32(2), _i32(2), _i32(2), _i32(3), _gpu((8,), torch.int64), ws, capacity=10)
+
+
+@pytest.mark.parametrize("call", [_plan, lambda ws: _attn(ws=ws)])
+@pytest.mark.parametrize("ws", [torch.zeros(1 << 20, dtype=torch.uint8), _gpu((1 << 20,), torch.int32), _gpu((1 << 20,), torch.uint8, (2,))],
+                         ids=["host memory", "int32", "every second byte"])
+def test_workspaces_that_are_no_bytes_on_the_gpu(call, ws):
+    with pytest.raises(ValueError, match="workspace"):
+        call(ws)
