@@ -356,6 +356,12 @@ def _need_int(what: str, n: int, dtype, *tensors):
             raise ValueError(f"{what}: a tensor of {n} or more {dtype}, contiguous, on the GPU was expected, not {tuple(t.shape)} {t.dtype} on {t.device}")
 
 
+def _need_rows(what: str, name: str, rows: torch.Tensor, width: int):
+    """Rows of this many numbers each, or a flat tensor of them."""
+    if rows.dim() > 1 and rows.shape[-1] != width:
+        raise ValueError(f"{what}: {name} has rows of {width}, not {tuple(rows.shape)}")
+
+
 def _need_workspace(what: str, ws: torch.Tensor):
     if ws.dtype is not torch.uint8 or not ws.is_contiguous() or not ws.is_cuda:
         raise ValueError(f"{what}: a workspace of uint8, contiguous, on the GPU was expected, not {tuple(ws.shape)} {ws.dtype} on {ws.device}")
@@ -435,6 +441,7 @@ def tree_masks(base, tok_start, parents, masks, positions, max_nodes: int):
     _need_int("tree_masks", 2, torch.int32, tok_start)
     _need_int("tree_masks", n, torch.int32, parents, parents if positions is None else positions)
     _need_int("tree_masks", n * mask_words(max_nodes), torch.int64, masks)
+    _need_rows("tree_masks", "masks", masks, mask_words(max_nodes))
     if n == 0:                                               # a step in which nothing was drafted
         return
     _check(load().cusa_tree_masks(batch, base.data_ptr(), tok_start.data_ptr(), parents.data_ptr(), n, max_nodes, masks.data_ptr(),
@@ -471,8 +478,10 @@ def tree_attn(params: CusaParams, q, kv: KvCache, tree: Tree, out, ws, idx=None,
     _need_workspace("tree_attn", ws)
     _need_int("tree_attn", params.batch + 1, torch.int32, tree.tok_start)
     _need_int("tree_attn", n * mask_words(tree.max_nodes), torch.int64, tree.masks)
+    _need_rows("tree_attn", "masks", tree.masks, mask_words(tree.max_nodes))
     if idx is not None:
         _need_int("tree_attn", params.batch * params.budget, torch.int32, idx)
+        _need_rows("tree_attn", "idx", idx, params.budget)
         _need(cnt is not None, "tree_attn: idx comes with cnt")
         _need_int("tree_attn", params.batch, torch.int32, cnt)
     c = _cache_desc("tree_attn", params, kv)

@@ -66,3 +66,31 @@ def _plan(ws):
 def test_workspaces_that_are_no_bytes_on_the_gpu(call, ws):
     with pytest.raises(ValueError, match="workspace"):
         call(ws)
+
+
+def _masks(masks, nodes):
+    cb.tree_masks(_i32(2), _i32(3), _i32(5), masks, None, nodes)
+
+
+@pytest.mark.parametrize("shape", [(5, 2), (5, 3), (5, 1, 2)])
+def test_mask_rows_of_another_width(shape):
+    """Trees of up to 64 nodes have rows of one word: wider rows would be read and written a word apart.  (Flat ones have no width of their own.)"""
+    masks = _gpu(shape, torch.int64)
+    with pytest.raises(ValueError, match="masks"):
+        _masks(masks, 64)
+    with pytest.raises(ValueError, match="masks"):
+        _attn(tree=cb.Tree(_i32(3), masks, 64))
+    for right in ((7, 1), (5,)):
+        with pytest.raises(AssertionError, match="cusa_tree_masks was reached"):
+            _masks(_gpu(right, torch.int64), 64)
+        with pytest.raises(AssertionError, match="cusa_tree_attn was reached"):
+            _attn(tree=cb.Tree(_i32(3), _gpu(right, torch.int64), 64))
+
+
+@pytest.mark.parametrize("shape", [(2, 17), (2, 32), (4, 8)])
+def test_lists_of_another_width(shape):
+    with pytest.raises(ValueError, match="idx"):
+        _attn(idx=_i32(*shape), cnt=_i32(2))
+    for right in ((3, 16), (32,)):
+        with pytest.raises(AssertionError, match="cusa_tree_attn was reached"):
+            _attn(idx=_i32(*right), cnt=_i32(2))
