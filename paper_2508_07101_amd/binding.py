@@ -367,6 +367,12 @@ def _need_workspace(what: str, ws: torch.Tensor):
         raise ValueError(f"{what}: a workspace of uint8, contiguous, on the GPU was expected, not {tuple(ws.shape)} {ws.dtype} on {ws.device}")
 
 
+def _strides(t: torch.Tensor, alone):
+    """A tensor's strides; those of dimensions of one entry mean nothing (torch may have anything there) and are what `alone` has."""
+    strides, shape = t.stride(), t.shape
+    return tuple(a if n == 1 else s for n, s, a in zip(shape, strides, alone)) if 1 in shape else strides
+
+
 def _cache_desc(what: str, params: CusaParams, kv: KvCache) -> CusaKv:
     """The cache's descriptor, as KvCache.desc makes it, if it has the rows that the parameters speak of: kernels write there.  (Each of a step's calls makes
     one a layer: a tensor is asked once for each thing.)"""
@@ -375,8 +381,9 @@ def _cache_desc(what: str, params: CusaParams, kv: KvCache) -> CusaKv:
     if (len(shape) == 4 and v.shape == shape and shape[1] == params.n_kv_heads and shape[3] == params.head_dim and k.dtype is bf16 and v.dtype is bf16
             and k.is_cuda and v.is_cuda and lens.dtype is torch.int32 and lens.numel() >= batch and lens.is_cuda and lens.is_contiguous()):
         if table is None:
-            strides = k.stride()
-            if shape[0] >= batch and strides[3] == 1 and strides == v.stride() and kv.max_seq_len <= shape[2]:
+            alone = (0, 0, params.head_dim, 1)
+            strides = _strides(k, alone)
+            if shape[0] >= batch and strides[3] == 1 and strides == _strides(v, alone) and kv.max_seq_len <= shape[2]:
                 return CusaKv(k.data_ptr(), v.data_ptr(), KV_CONTIGUOUS, strides[0], strides[1], strides[2], None, 0, 0, 0, lens.data_ptr(), kv.max_seq_len)
         elif (k.is_contiguous() and v.is_contiguous() and table.dim() == 2 and table.shape[0] >= batch and table.dtype is torch.int32 and table.is_cuda
                 and table.is_contiguous()):
@@ -419,8 +426,8 @@ def kv_append(params: CusaParams, kv: KvCache, slots, k_new, v_new):
     n, heads, d = k_new.shape
     _need(k_new.dtype in DTYPES and v_new.dtype == k_new.dtype and v_new.shape == k_new.shape and d == params.head_dim and
           heads == params.n_kv_heads, "kv_append: new rows are [n, n_kv_heads, 128] in bf16, fp16 or fp32")
-    strides = k_new.stride()
-    _need(strides[2] == 1 and strides == v_new.stride(), "kv_append: K and V rows have the same strides, elements side by side")
+    strides = _strides(k_new, (0, 0, 1))
+    _need(strides[2] == 1 and strides == _strides(v_new, (0, 0, 1)), "kv_append: K and V rows have the same strides, elements side by side")
     _need(k_new.is_cuda and v_new.is_cuda, "kv_append: new rows are on the GPU")
     _need_int("kv_append", n, torch.int64, slots)
     c = _cache_desc("kv_append", params, kv)
@@ -470,7 +477,7 @@ def tree_attn(params: CusaParams, q, kv: KvCache, tree: Tree, out, ws, idx=None,
     """Attention of the trees' nodes, q [tokens, H, 128] (a view of a fused projection's rows, or contiguous), over the whole prefix or
     over idx/cnt of it, and over the nodes that the masks name."""
     n, heads, d = q.shape
-    strides = q.stride()
+    strides = _strides(q, (heads * d, d, 1))
     _need(q.dtype is torch.bfloat16 and heads == params.n_q_heads and d == params.head_dim and strides[2] == 1 and strides[1] == d,
           "tree_attn: q is bf16 [tokens, n_q_heads, 128], heads side by side")
     _need(q.is_cuda and out.is_cuda, "tree_attn: q and out are on the GPU")

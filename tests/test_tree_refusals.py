@@ -94,3 +94,46 @@ def test_lists_of_another_width(shape):
     for right in ((3, 16), (32,)):
         with pytest.raises(AssertionError, match="cusa_tree_attn was reached"):
             _attn(idx=_i32(*right), cnt=_i32(2))
+
+
+def _calls(monkeypatch):
+    """What reaches the library: the descriptors of a call by its name."""
+    seen = {}
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: seen.setdefault(name, [getattr(a, "_obj", a) for a in args]) and 0
+    monkeypatch.setattr(cb, "load", lambda: Library())
+    monkeypatch.setattr(cb, "_stream", lambda: None)
+    return seen
+
+
+def test_strides_of_one_entry_mean_nothing(monkeypatch):
+    """One token, one head, one sequence: torch may give such a dimension any stride, and calls the tensor contiguous."""
+    seen = _calls(monkeypatch)
+    one = cb.make_params(1, 1, 1, 16, 0)
+    k, v = _gpu((1, 1, 32, 128), torch.bfloat16, (8, 24, 128, 1)), _gpu((1, 1, 32, 128), torch.bfloat16, (9, 5, 128, 1))
+    kv = cb.KvCache(k, v, _i32(1), 32)
+    rows, more = _gpu((1, 1, 128), torch.bfloat16, (7, 3, 1)), _gpu((1, 1, 128), torch.bfloat16, (128, 1, 1))
+    cb.kv_append(one, kv, _gpu((1,), torch.int64), rows, more)
+    desc, r = seen["cusa_kv_append"][1], seen["cusa_kv_append"][3]
+    assert (desc.stride_batch % 8, desc.stride_head % 8, desc.stride_token) == (0, 0, 128) and (r.stride_token % 8, r.stride_head % 8) == (0, 0)
+    cb.tree_attn(one, rows, kv, cb.Tree(_i32(2), _gpu((1, 1), torch.int64), 4), _gpu((1, 1, 128), torch.bfloat16), _gpu((256,), torch.uint8))
+    assert seen.pop("cusa_tree_attn")[3].q_stride == 128
+    # the single token of a decode step, as a transposed projection leaves it: [H, 1, 128] seen as [1, H, 128]
+    cb.tree_attn(cb.make_params(1, 8, 1, 16, 0), _gpu((1, 8, 128), torch.bfloat16, (128, 128, 1)), kv, cb.Tree(_i32(2), _gpu((1, 1), torch.int64), 4),
+                 _gpu((1, 8, 128), torch.bfloat16), _gpu((256,), torch.uint8))
+    assert seen["cusa_tree_attn"][3].q_stride == 8 * 128
+    # one position: its stride is a row's
+    single = cb.KvCache(_gpu((2, 4, 1, 128), torch.bfloat16, (512, 128, 1, 1)), _gpu((2, 4, 1, 128), torch.bfloat16, (512, 128, 64, 1)), _i32(2), 1)
+    cb.KvCommit(P, [single])
+    rows = _gpu((3, 4, 128), torch.bfloat16)
+    seen.clear()
+    cb.kv_append(P, single, _gpu((3,), torch.int64), rows, rows)
+    desc = seen["cusa_kv_append"][1]
+    assert (desc.stride_batch, desc.stride_head, desc.stride_token) == (512, 128, 128)
+    with pytest.raises(ValueError):
+        cb.kv_append(P, _cache(32, 32), _gpu((3,), torch.int64), rows, _gpu((3, 4, 128), torch.bfloat16, (1024, 128, 1)))
+    with pytest.raises(ValueError):
+        cb.kv_append(P, cb.KvCache(_gpu((2, 4, 32, 128), torch.bfloat16), _gpu((2, 4, 32, 128), torch.bfloat16, (16384, 128, 512, 1)), _i32(2), 32),
+                     _gpu((3,), torch.int64), rows, rows)
