@@ -295,7 +295,7 @@ typedef struct {
 } cusa_rows;
 
 /* Row r goes to slots[r] (as cusa_kv_plan makes them) of one layer's cache, all KV heads; slots outside the pool, or at positions
- * from max_seq_len on, are left out.  Two rows with the same slot leave either.  kv's seq_lens and block_table are not read. */
+ * from max_seq_len on, are left out.  Two rows with the same slot leave a mix of them, 16 bytes of either.  kv's seq_lens and block_table are not read. */
 cusa_status cusa_kv_append(const cusa_params* params, const cusa_kv* kv, const int64_t* slots, const cusa_rows* rows, void* stream);
 
 /* A batch of trees, host memory. */

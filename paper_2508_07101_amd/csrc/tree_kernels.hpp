@@ -620,12 +620,12 @@ __device__ __forceinline__ void add_values(TreeRow& r, const TreeValues& vf, con
     add_values<1>(r, vf, p);
 }
 // A weight 2^(scale x - m).  The instruction makes 0 of results below 2^-126, which beside a value of 2^120 are not nothing: it makes the weight's 2^64-fold.
-// (Of 128 to 512 rows this costs 1.5 to 2 %.)
+// (Of 128 to 512 rows this costs 1 to 2 %.)
 __device__ __forceinline__ float weight(float m, float x, float scale_log2e) {
     return __builtin_amdgcn_exp2f(__builtin_fmaf(x, scale_log2e, 64.0f - m)) * 0x1p-64f;
 }
 // The weights and their sum, in 32 bits.  (Two-element dot products of the rounded weights: one wait for the matrix pipe each, 1 to 2 % of the time for 128 to
-// 512 rows; taking the weights apart again and adding them one by one 5 to 6 %.)
+// 512 rows; taking the weights apart again and adding them one by one 4 to 6 %.)
 template <int FROM = 0, int TO = 16>
 __device__ __forceinline__ float weigh(float m, const f32x16& x, float scale_log2e, TreeWeights& p) {
     const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};

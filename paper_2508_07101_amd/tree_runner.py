@@ -56,7 +56,7 @@ class TreeRunner:
         cb.kv_append(self.params, self.kvs[layer], slots, k_new, v_new)
 
     def room(self, nodes: torch.Tensor, n: int) -> torch.Tensor:
-        """Room for nodes[b] drafted tokens of sequence b, n of all at most; what the step before did not accept goes back.  Returns tok_start: a sequence
+        """Room for nodes[b] drafted tokens of sequence b (max_nodes at most), n of all at most; what the step before did not accept goes back.  Returns tok_start: a sequence
         without room has no rows."""
         if n > self.slots.numel():
             raise ValueError(f"{n} drafted tokens, room for {self.slots.numel()}")
@@ -73,8 +73,8 @@ class TreeRunner:
 
     def draft(self, nodes: torch.Tensor, parents: torch.Tensor) -> torch.Tensor:
         """room and trees in one, without a look at what was granted: the parents are packed as they were asked for, nodes[b] of sequence b, and those of
-        sequences without room are left out (by torch, some 30 to 60 us of a step in which the GPU waits for the host; where nothing can be refused, room and
-        trees do without).  Returns the positions, packed as tok_start says (what is behind the last row is not defined)."""
+        sequences without room are left out (by torch, some 30 to 60 us of a step in which the GPU waits for the host; where nothing can be refused, and in
+        a captured step, room and trees do without).  Returns the positions, packed as tok_start says (what is behind the last row is not defined)."""
         n = parents.numel()
         start = self.room(nodes, n)
         if n > 0:
