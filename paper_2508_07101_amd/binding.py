@@ -356,10 +356,11 @@ def _need_int(what: str, n: int, dtype, *tensors):
             raise ValueError(f"{what}: a tensor of {n} or more {dtype}, contiguous, on the GPU was expected, not {tuple(t.shape)} {t.dtype} on {t.device}")
 
 
-def _need_rows(what: str, name: str, rows: torch.Tensor, width: int):
-    """Rows of this many numbers each, or a flat tensor of them."""
-    if rows.dim() > 1 and rows.shape[-1] != width:
-        raise ValueError(f"{what}: {name} has rows of {width}, not {tuple(rows.shape)}")
+def _need_rows(what: str, name: str, rows: torch.Tensor, n: int, width: int, dtype):
+    """n rows of this many numbers at least (or a flat tensor of them), contiguous, on the GPU."""
+    shape = rows.shape
+    if rows.dtype is not dtype or rows.numel() < n * width or (len(shape) > 1 and shape[-1] != width) or not rows.is_contiguous() or not rows.is_cuda:
+        raise ValueError(f"{what}: {name} of {n} or more rows of {width} {dtype}, contiguous, on the GPU was expected, not {tuple(shape)} {rows.dtype} on {rows.device}")
 
 
 def _need_workspace(what: str, ws: torch.Tensor):
@@ -369,8 +370,7 @@ def _need_workspace(what: str, ws: torch.Tensor):
 
 def _strides(t: torch.Tensor, alone):
     """A tensor's strides; those of dimensions of one entry mean nothing (torch may have anything there) and are what `alone` has."""
-    strides, shape = t.stride(), t.shape
-    return tuple(a if n == 1 else s for n, s, a in zip(shape, strides, alone)) if 1 in shape else strides
+    return tuple(a if n == 1 else s for n, s, a in zip(t.shape, t.stride(), alone))
 
 
 def _cache_desc(what: str, params: CusaParams, kv: KvCache) -> CusaKv:
@@ -381,9 +381,11 @@ def _cache_desc(what: str, params: CusaParams, kv: KvCache) -> CusaKv:
     if (len(shape) == 4 and v.shape == shape and shape[1] == params.n_kv_heads and shape[3] == params.head_dim and k.dtype is bf16 and v.dtype is bf16
             and k.is_cuda and v.is_cuda and lens.dtype is torch.int32 and lens.numel() >= batch and lens.is_cuda and lens.is_contiguous()):
         if table is None:
-            alone = (0, 0, params.head_dim, 1)
-            strides = _strides(k, alone)
-            if shape[0] >= batch and strides[3] == 1 and strides == _strides(v, alone) and kv.max_seq_len <= shape[2]:
+            strides, of_v = k.stride(), v.stride()
+            if 1 in shape and (strides != of_v or (strides[0] | strides[1] | strides[2]) & 7 or strides[2] < params.head_dim):   # (mostly they do as they are)
+                alone = (0, 0, params.head_dim, 1)
+                strides, of_v = _strides(k, alone), _strides(v, alone)
+            if shape[0] >= batch and strides[3] == 1 and strides == of_v and kv.max_seq_len <= shape[2]:
                 return CusaKv(k.data_ptr(), v.data_ptr(), KV_CONTIGUOUS, strides[0], strides[1], strides[2], None, 0, 0, 0, lens.data_ptr(), kv.max_seq_len)
         elif (k.is_contiguous() and v.is_contiguous() and table.dim() == 2 and table.shape[0] >= batch and table.dtype is torch.int32 and table.is_cuda
                 and table.is_contiguous()):
@@ -426,8 +428,10 @@ def kv_append(params: CusaParams, kv: KvCache, slots, k_new, v_new):
     n, heads, d = k_new.shape
     _need(k_new.dtype in DTYPES and v_new.dtype == k_new.dtype and v_new.shape == k_new.shape and d == params.head_dim and
           heads == params.n_kv_heads, "kv_append: new rows are [n, n_kv_heads, 128] in bf16, fp16 or fp32")
-    strides = _strides(k_new, (0, 0, 1))
-    _need(strides[2] == 1 and strides == _strides(v_new, (0, 0, 1)), "kv_append: K and V rows have the same strides, elements side by side")
+    strides, of_v = k_new.stride(), v_new.stride()
+    if n == 1 or heads == 1:
+        strides, of_v = _strides(k_new, (0, 0, 1)), _strides(v_new, (0, 0, 1))
+    _need(strides[2] == 1 and strides == of_v, "kv_append: K and V rows have the same strides, elements side by side")
     _need(k_new.is_cuda and v_new.is_cuda, "kv_append: new rows are on the GPU")
     _need_int("kv_append", n, torch.int64, slots)
     c = _cache_desc("kv_append", params, kv)
@@ -447,8 +451,7 @@ def tree_masks(base, tok_start, parents, masks, positions, max_nodes: int):
     _need_int("tree_masks", batch, torch.int32, base)
     _need_int("tree_masks", 2, torch.int32, tok_start)
     _need_int("tree_masks", n, torch.int32, parents, parents if positions is None else positions)
-    _need_int("tree_masks", n * mask_words(max_nodes), torch.int64, masks)
-    _need_rows("tree_masks", "masks", masks, mask_words(max_nodes))
+    _need_rows("tree_masks", "masks", masks, n, mask_words(max_nodes), torch.int64)
     if n == 0:                                               # a step in which nothing was drafted
         return
     _check(load().cusa_tree_masks(batch, base.data_ptr(), tok_start.data_ptr(), parents.data_ptr(), n, max_nodes, masks.data_ptr(),
@@ -477,18 +480,16 @@ def tree_attn(params: CusaParams, q, kv: KvCache, tree: Tree, out, ws, idx=None,
     """Attention of the trees' nodes, q [tokens, H, 128] (a view of a fused projection's rows, or contiguous), over the whole prefix or
     over idx/cnt of it, and over the nodes that the masks name."""
     n, heads, d = q.shape
-    strides = _strides(q, (heads * d, d, 1))
+    strides = _strides(q, (heads * d, d, 1)) if n == 1 or heads == 1 else q.stride()
     _need(q.dtype is torch.bfloat16 and heads == params.n_q_heads and d == params.head_dim and strides[2] == 1 and strides[1] == d,
           "tree_attn: q is bf16 [tokens, n_q_heads, 128], heads side by side")
     _need(q.is_cuda and out.is_cuda, "tree_attn: q and out are on the GPU")
     _need(out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() >= n * heads * d, "tree_attn: out is bf16 [tokens, n_q_heads, 128], contiguous")
     _need_workspace("tree_attn", ws)
     _need_int("tree_attn", params.batch + 1, torch.int32, tree.tok_start)
-    _need_int("tree_attn", n * mask_words(tree.max_nodes), torch.int64, tree.masks)
-    _need_rows("tree_attn", "masks", tree.masks, mask_words(tree.max_nodes))
+    _need_rows("tree_attn", "masks", tree.masks, n, mask_words(tree.max_nodes), torch.int64)
     if idx is not None:
-        _need_int("tree_attn", params.batch * params.budget, torch.int32, idx)
-        _need_rows("tree_attn", "idx", idx, params.budget)
+        _need_rows("tree_attn", "idx", idx, params.batch, params.budget, torch.int32)
         _need(cnt is not None, "tree_attn: idx comes with cnt")
         _need_int("tree_attn", params.batch, torch.int32, cnt)
     c = _cache_desc("tree_attn", params, kv)
