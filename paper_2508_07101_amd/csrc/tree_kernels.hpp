@@ -593,8 +593,8 @@ __device__ __forceinline__ void read_values(TreeValues& vf, uint32_t vt, int lan
         for (int d = 0; d < 4; ++d) vf.f[k][d] = read_value(vt + 4096 * k + value_at(lane, d));
 }
 // O^T += V^T P^T: the weights are the product's operand in the order in which the lanes hold them.
-// Up to 64 rows, where memory bounds the time, a weight is two bf16 numbers, f + rest, and takes two products: it is off by 2^-15 of itself at most.  (From
-// 16384 cached tokens on, 64 sequences, this costs 1 % for up to 32 rows and 5 % for 64.)  Above, where the products bound the time, it is one, off by 2^-8 at
+// Up to 64 rows, where memory bounds the time, a weight is two bf16 numbers, f + rest, and takes two products: it is off by 2^-15 of itself at most.  (Over
+// 64 sequences of 20480 tokens this costs 1 % for up to 32 rows and 2 to 5 % for 64.)  Above, where the products bound the time, it is one, off by 2^-8 at
 // most, and the row's sum adds up the rounded weights: a token that outweighs the others is rounded alike in both.
 struct TreeWeights {
     bf16x8 f[2];
@@ -764,9 +764,9 @@ __device__ __forceinline__ uint32_t add_washed(TreeRow& r, const W& p, uint32_t 
 // LDS at the end.  Two waves to a SIMD.  Tiles come by loads from memory straight to LDS, several of them under way.
 // One pass: S^T = K Q^T, weights 2^(scale S - m) against a reference m that the row keeps, O^T += V^T P^T, divided by the weights' sum at the end.
 // What bounds it goes by the rows that share a KV head's tokens (64 sequences of 20480 tokens, 32 heads over 8, paged): memory up to 128 rows (nodes times
-// query heads of a KV head): 4 rows 6.6 TB/s, 32 rows 6.3, 64 rows 6.1, 128 rows 5.4 TB/s and 691 TFLOP/s; above that the matrix cores and the softmax beside them: 256
-// rows 887 TFLOP/s, 512 rows 963 (a library product of 8192^3 reaches 1222).  192 rows cost as much as 256 do on half of the SIMDs: 744.  One
-// sequence of 32768 tokens, 240 rows: 49 us, of which 29 are the tiles' arrival, 6 the way to the first tile, 5 the partial sums' way out.
+// query heads of a KV head): 4 rows 6.5 TB/s, 32 rows 6.2, 64 rows 5.6 to 5.9, 128 rows 5.1 to 5.4 TB/s and 650 to 690 TFLOP/s; above that the matrix cores and the softmax
+// beside them: 256 rows 850 TFLOP/s, 512 rows 924 (a library product of 8192^3 reaches 1210).  192 rows cost as much as 256 do on half of the SIMDs: 712.  One
+// sequence of 32768 tokens, 240 rows: 50 us, of which about 29 are the tiles' arrival, 6 the way to the first tile, 5 the partial sums' way out.
 template <int RG, bool PAGED, bool SPARSE>
 __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, TreeLds& lds, int b, int kvh, int row0, int split, int begin, int end) {
     constexpr int TEAMS = TREE_WAVES / RG;
