@@ -334,7 +334,8 @@ cusa_status cusa_tree_attn(const cusa_params* params, const void* q, const cusa_
                            const int32_t* cnt, void* out, void* ws, size_t ws_bytes, void* stream);
 
 /* The accepted branches' rows moved together, in all layers: position base[b] + path[b][i] -> base[b] + i for i < n_path[b], K and V,
- * all KV heads; path[b] ascending, and positions at or beyond max_seq_len are left out.  keep[b] = base[b] + n_path[b] (NULL: not
+ * all KV heads; path[b] ascending, and positions at or beyond max_seq_len are left out.  Nothing here knows how many nodes a sequence has: n_path is at
+ * most that, 0 for one that cusa_kv_plan gave no room (behind its tokens, a table may name pages that went to others since).  keep[b] = base[b] + n_path[b] (NULL: not
  * wanted; neither base nor n_path), what the next cusa_kv_plan keeps.  path: device int32 [batch][max_path]; base, n_path, keep: device int32 [batch]. */
 cusa_status cusa_kv_commit(const cusa_params* params, int32_t n_layers, const cusa_kv* kv_layers, const int32_t* base,
                            const int32_t* path, int32_t max_path, const int32_t* n_path, int32_t* keep, void* stream);

@@ -98,3 +98,11 @@ def test_list_entries_outside_the_prefix_are_left_out(layout, name):
         c.idx[b, : len(entries)] = _i32(entries)
         c.sets[b] = np.delete(entries, out)
     c.check(f"{layout} {name}")
+
+
+def test_the_single_token_of_a_transposed_projection():
+    """[H, 1, 128] seen as [1, H, 128]: the stride of the one token means nothing."""
+    c = _Case("head_major", 8, 2, [300], [1], 26)
+    want = c.out()
+    c.q = c.q.reshape(8, 1, 128).transpose(0, 1)
+    assert c.q.stride(0) == 128 and torch.equal(c.out(), want)
