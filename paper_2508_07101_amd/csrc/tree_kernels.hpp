@@ -620,24 +620,28 @@ __device__ __forceinline__ void add_values(TreeRow& r, const TreeValues& vf, con
     add_values<1>(r, vf, p);
 }
 // A weight 2^(scale x - m).  The instruction makes 0 of results below 2^-126, which beside a value of 2^120 are not nothing: it makes the weight's 2^64-fold.
-// (Of 128 to 512 rows this costs 1 to 2 %.)
+// (With the sums below 1 to 2 % for 128 to 512 rows.)
 __device__ __forceinline__ float weight(float m, float x, float scale_log2e) {
     return __builtin_amdgcn_exp2f(__builtin_fmaf(x, scale_log2e, 64.0f - m)) * 0x1p-64f;
 }
-// The weights and their sum, in 32 bits.  (Two-element dot products of the rounded weights: one wait for the matrix pipe each, 1 to 2 % of the time for 128 to
-// 512 rows; taking the weights apart again and adding them one by one 4 to 6 %.)
-template <int FROM = 0, int TO = 16>
-__device__ __forceinline__ float weigh(float m, const f32x16& x, float scale_log2e, TreeWeights& p) {
+// The weights' sum, in 32 bits, is of the rounded ones: two-element dot products.  These wait for the matrix pipe, so they stand where this wave has no products to
+// issue beside them.  (64 sequences of 20480 tokens under 64 nodes, 256 rows: weights below 2^-126 left out and sums unrounded 1508 us; both in, dot products among the
+// products 1559, behind them 1520.  Taking the weights apart again and adding them one by one: 4 to 6 % for 128 to 512 rows.)
+template <int FROM, int TO>
+__device__ __forceinline__ void weigh(float m, const f32x16& x, float scale_log2e, TreeWeights& p) {
+#pragma unroll
+    for (int i = FROM; i < TO; ++i) p.f[i >> 3][i & 7] = (__bf16)weight(m, x[i], scale_log2e);
+}
+__device__ __forceinline__ float add_up(const TreeWeights& p) {
     const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
     float sum = 0.0f;
 #pragma unroll
-    for (int i = FROM; i < TO; i += 2) {
-        const bf16x2 w = {(__bf16)weight(m, x[i], scale_log2e), (__bf16)weight(m, x[i + 1], scale_log2e)};
-        p.f[i >> 3][i & 7] = w[0];
-        p.f[i >> 3][(i & 7) + 1] = w[1];
-        sum = __builtin_amdgcn_fdot2_f32_bf16(w, ones, sum, false);
-    }
+    for (int i = 0; i < 16; i += 2) sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{p.f[i >> 3][i & 7], p.f[i >> 3][(i & 7) + 1]}, ones, sum, false);
     return sum;
+}
+__device__ __forceinline__ float weigh(float m, const f32x16& x, float scale_log2e, TreeWeights& p) {
+    weigh<0, 16>(m, x, scale_log2e, p);
+    return add_up(p);
 }
 // f: the weight cut to bf16, less one step; rest: what is missing, a step to two, rounded.  Neither is negative or, from 2^-132 on, 0, so that a value that is
 // infinite stays so in both products.
@@ -698,31 +702,31 @@ __device__ __forceinline__ void tree_step(TreeRow& r, const f32x16& x, f32x16& y
 #pragma unroll
     for (int k = 0; k < 4; ++k) kf.f[k] = read_key(key[k] + NEXT_K);
     __builtin_amdgcn_sched_barrier(0);
-    float sum = weigh<0, 8>(r.m, x, scale_log2e, p);              // (while the operands are on their way)
+    weigh<0, 8>(r.m, x, scale_log2e, p);                          // (while the operands are on their way)
     __builtin_amdgcn_sched_barrier(0);
     // products and softmax in turn: in this order they issue, and neither pipe waits for the other
     add_values<0>(r, vf, p_last);
-    sum += weigh<8, 12>(r.m, x, scale_log2e, p);
+    weigh<8, 12>(r.m, x, scale_log2e, p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, 3, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int k = 4; k < 8; ++k) kf.f[k] = read_key(key[k] + NEXT_K);   // (in the first values' registers)
     __builtin_amdgcn_sched_barrier(0);
     add_values<1>(r, vf, p_last);
-    sum += weigh<12, 16>(r.m, x, scale_log2e, p);
+    weigh<12, 16>(r.m, x, scale_log2e, p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, 3, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
     y = score(r, kf);
     __builtin_amdgcn_sched_barrier(0);
-    raise_and_weigh(r, x, scale_log2e, p, sum);
+    raise_and_weigh(r, x, scale_log2e, p, add_up(p));
 }
 // A tile that not every row attends to as a whole: scores of the tokens outside `allowed` (a bit each) weigh nothing.
 __device__ __forceinline__ void mask_scores(f32x16& x, uint32_t allowed, int half) {
