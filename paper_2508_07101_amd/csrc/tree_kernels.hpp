@@ -306,7 +306,7 @@ __device__ __forceinline__ u32x4 load_as_bf16(const void* base, int64_t at) {
 }
 
 // A group of 16 lanes for a row of 128 elements.  Rows are numbered (token, K heads then V heads).  Bound by memory: 131 072 fp32 rows of 8 KV heads (1.6 GB read
-// and written) take 304 us, 5.3 TB/s, as much as a plain copy's rate; 2388 bf16 rows from a fused projection (20 MB) 5.5 us, mostly latency.
+// and written) take 304 us, 5.3 TB/s, as much as a plain copy's rate; 2388 bf16 rows from a fused projection (20 MB) 5.9 us, mostly latency.
 template <int DTYPE, bool PAGED>
 __global__ __launch_bounds__(APPEND_THREADS) void kv_append_kernel(AppendArgs a) {
     constexpr int PER_WG = APPEND_THREADS / 16 * APPEND_ROWS;
@@ -361,7 +361,7 @@ __device__ __forceinline__ int tree_span(const int32_t* tok_start, int b, int ma
 
 // One workgroup for a tree, a thread for a node.  Who stands above a node is known after as many rounds as the depth has bits: each
 // round a node takes over what the node it points to knows, and points where that one points.  Latency is all: 60 nodes 3.3 us (a launch that does
-// nothing takes about 3), 64 trees of up to 256 nodes 5.4.
+// nothing takes about 3), 64 trees of up to 256 nodes 5.5.
 __global__ __launch_bounds__(TREE_MAX_NODES) void tree_masks_kernel(MasksArgs a) {
     __shared__ uint64_t rows[TREE_MAX_NODES / 64][TREE_MAX_NODES];
     __shared__ int up[TREE_MAX_NODES], deep[TREE_MAX_NODES];
@@ -768,8 +768,8 @@ __device__ __forceinline__ uint32_t add_washed(TreeRow& r, const W& p, uint32_t 
 // LDS at the end.  Two waves to a SIMD.  Tiles come by loads from memory straight to LDS, several of them under way.
 // One pass: S^T = K Q^T, weights 2^(scale S - m) against a reference m that the row keeps, O^T += V^T P^T, divided by the weights' sum at the end.
 // What bounds it goes by the rows that share a KV head's tokens (64 sequences of 20480 tokens, 32 heads over 8, paged): memory up to 128 rows (nodes times
-// query heads of a KV head): 4 rows 6.5 TB/s, 32 rows 6.2, 64 rows 5.6 to 5.9, 128 rows 5.1 to 5.4 TB/s and 650 to 690 TFLOP/s; above that the matrix cores and the softmax
-// beside them: 256 rows 850 TFLOP/s, 512 rows 924 (a library product of 8192^3 reaches 1210).  192 rows cost as much as 256 do on half of the SIMDs: 712.  One
+// query heads of a KV head): 4 rows 6.5 TB/s, 32 rows 6.2, 64 rows 5.6 to 5.9, 128 rows 5.2 to 5.4 TB/s and 660 to 690 TFLOP/s; above that the matrix cores and the softmax
+// beside them: 256 rows 856 to 873 TFLOP/s, 512 rows 933 (a library product of 8192^3 reaches 1210).  192 rows cost as much as 256 do on half of the SIMDs: 717.  One
 // sequence of 32768 tokens, 240 rows: 50 us, of which about 29 are the tiles' arrival, 6 the way to the first tile, 5 the partial sums' way out.
 template <int RG, bool PAGED, bool SPARSE>
 __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, TreeLds& lds, int b, int kvh, int row0, int split, int begin, int end) {

@@ -22,14 +22,14 @@ inline int tree_piece_most(TreeKind kind) { return kind == TREE_CHOSEN ? TREE_LI
 inline bool tree_len_served(TreeKind kind, int64_t len) { return len <= (int64_t)tree_piece_most(kind) * TREE_MAX_SPLITS; }
 
 // Tokens up to which sequences stay whole: what a workgroup of up to 64 rows takes in three steps (its teams take 256 or 128 tokens a step), which is less than the
-// merge's launch costs (1 sequence, 4 rows, 300 tokens: whole 9.7 us, in pieces 12.5; 520: 11.7 and 12.7; 1020, four steps: 15.0 and 13.7; 8 sequences, 64 rows,
-// 300 tokens: 14.7 and 16.8; 1020: 28.1 and 22.4), and for more rows one piece.  Where half of the CUs have a workgroup anyway, up to 1536 tokens (256 rows, 16 sequences
-// of 1064 tokens: whole 38.2 us, cut 57.3; 25: 54.1 and 58.9).  Of 2000 equal tokens 18 still gain, 83 and 99, but of 100 to 2000 they lose, 74 and 65.
+// merge's launch costs (1 sequence, 4 rows, 300 tokens: whole 9.8 us, in pieces 12.5; 520: 11.7 and 12.8; 1020, four steps: 14.9 and 13.7; 8 sequences, 64 rows,
+// 300 tokens: 14.8 and 16.8; 1020: 28.0 and 22.5), and for more rows one piece.  Where half of the CUs have a workgroup anyway, up to 1536 tokens (256 rows, 16 sequences
+// of 1064 tokens: whole 38 us, cut 59; 25: 55 and 61).  Of 2000 equal tokens 18 still gain, 81 and 100, but of 100 to 2000 they lose, 72 and 64.
 inline int tree_whole(int rows, int64_t wgs) { return std::max(rows <= 32 ? 768 : rows <= 64 ? 384 : TREE_MIN_PIECE, wgs >= TREE_CUS / 2 ? 1536 : 0); }
 
 // Where every CU has a workgroup already, pieces only make up for lengths, and room for them costs what starting workgroups without work does: 40 sequences of
-// 2000 tokens, 256 rows, 183 us with room for pieces of 256, 168 without; of 250 to 4000 tokens 208 and 166.  From 4096 on there is room: 40 of 10000 tokens 571,
-// without 656, 33 of 8192 under 3 nodes 226 and 264.  (Ragged batches of many would do without, 40 of 600 to 10000 tokens 361 and 341, but then a single long sequence
+// 2000 tokens, 256 rows, 183 us with room for pieces of 256, 167 without; of 250 to 4000 tokens 206 and 163.  From 4096 on there is room: 40 of 10000 tokens 567,
+// without 647, 33 of 8192 under 3 nodes 226 and 263.  (Ragged batches of many would do without, 40 of 600 to 10000 tokens 357 and 336, but then a single long sequence
 // among short ones holds up the rest.)
 inline int tree_pieces(int rows, int64_t wgs, int max_len) {
     const int least = wgs >= TREE_CUS ? 4096 : TREE_MIN_PIECE;
@@ -38,10 +38,11 @@ inline int tree_pieces(int rows, int64_t wgs, int max_len) {
 
 // Rows of a workgroup.  Half as many of twice as many workgroups where these and all their pieces run at once and sequences are not long: half as many steps
 // for the same tokens (a workgroup's two teams share them) and half the partial sums, but the tiles come twice from L2.  (60 nodes, 4 heads each: 1 sequence of 520
-// tokens 22.4 us, so 18.8; 8000: 30.5 and 26.7; 16 of 2000: 71 and 56; 256 nodes, 4 of 520: 53 and 36.)  In more than a round the ones without work, of trees and
-// sequences that differ, leave the last ones waiting: 8 of 520 under 256 nodes 57 and 67, 8 of 500 to 8000 under 20 to 60 nodes 79 and 88, though 3 of up to 2000
-// 28 and 23.  Beyond 8192 tokens a single sequence would gain up to 30000 (30000: 53.7 and 52.6; 131072: 168.5 and 174.6), several lose (8 of 30000: 304 and 319).  Where the
-// last workgroup's rows are few, waves that idle in the large form are the cheaper ones from 2048 tokens on (36 nodes: 1 of 2000 24.0 and 19.7, of 30000 45 and 52).
+// tokens 22.3 us, so 18.6; 8000: 31.0 and 27.1; 16 of 2000: 72 and 55; 256 nodes, 4 of 520: 53 and 36.)  In more than a round the ones without work, of trees and
+// sequences that differ, leave the last ones waiting: 8 of 520 under 256 nodes 58 and 70, 8 of 500 to 8000 under 20 to 60 nodes 79 and 88, though 3 of up to 2000
+// 28 and 24.  Beyond 8192 tokens a single sequence would gain up to 30000 (10000: 35.4 and 30.4; 30000: 53.8 and 53.2; 131072: 166 and 176), several lose (8 of 30000: 302
+// and 319).  Where the last workgroup's rows are few, waves that idle in the large form are the cheaper ones from 2048 tokens on (36 nodes: 1 of 2000 23.5 and 19.5, of
+// 30000 46 and 52).
 inline int tree_tile_rows(int rows, int64_t pairs, int batch, int max_len) {
     const int tiles = (rows + 127) / 128;
     const int64_t wgs = pairs * tiles, at_once = batch == 1 ? wgs : wgs * tree_pieces(rows, wgs, max_len);   // (one sequence is cut for the CUs that there are)
