@@ -340,6 +340,96 @@ cusa_status cusa_tree_attn(const cusa_params* params, const void* q, const cusa_
 cusa_status cusa_kv_commit(const cusa_params* params, int32_t n_layers, const cusa_kv* kv_layers, const int32_t* base,
                            const int32_t* path, int32_t max_path, const int32_t* n_path, int32_t* keep, void* stream);
 
+/* ---- beam search over paged caches -----------------------------------------------------------
+ * A group: `width` (1 .. 32) consecutive rows of the batch that continue one prompt, the beams of a search or samples drawn side by side.  Rows of
+ * a group share the pages of what they have in common; rows of different groups share none.  Per step:
+ *   cusa_beam_select    the best continuations of every group, from the logits: parents, tokens, scores
+ *   cusa_kv_fork        block tables by parents, pages that nobody holds any more back, a slot for each row's token
+ *   cusa_kv_copy        the pages that two rows would both write to, in all layers
+ *   cusa_shared_pages   each page of a group once, with the rows that hold it
+ *   per layer: cusa_kv_append (the tokens' K and V rows into their slots), cusa_beam_attn; cusa_select and cusa_sparse_attn take the tables as they are
+ * A prompt gets its pages by cusa_kv_plan, in one row of its group (the others hold nothing), and cusa_kv_fork gives them to the other rows.  From then on the rows'
+ * pages come and go by cusa_kv_fork alone: cusa_kv_plan would give a shared page back while others hold it (it may run for other rows of the batch; held = keep and
+ * add = 0 leave a row as it is).  A page stands in the same column of every row that holds it, and once in a row.
+ * Lengths, parents, tables and lists are device memory and read when the kernels run; values out of range there are left out or cut to the bounds and
+ * never make a kernel read or write out of range. */
+
+/* Logits of a batch of groups, host memory. */
+typedef struct {
+    const void* logits;             /* device: row r's at logits + r * stride elements, aligned to an element                */
+    int32_t     dtype;              /* cusa_dtype                                                                            */
+    int64_t     stride;             /* >= vocab                                                                              */
+    int32_t     rows, width;        /* rows: a multiple of width, <= 65535                                                   */
+    int32_t     vocab;
+    int32_t     n;                  /* continuations of a group, 1 .. 64                                                     */
+    int32_t     end_token;          /* the token after which a beam has ended, -1: none                                      */
+} cusa_beams;
+
+/* The n best continuations of every group.  Row r with scores[r] = s and logits x proposes every token t with x_t above -infinity, worth
+ *   s + (x_t - max x) - ln(sum_u exp(x_u - max x)),
+ * and with ended[r] != 0 (ended NULL: no row has ended) only end_token, worth s.  A row whose score is not finite proposes nothing, and neither does one
+ * that has not ended with a logit that is NaN or +infinity, or with none above -infinity.  Of equal ones the lower row's comes first, then the lower token.
+ * out_scores, parents, tokens, out_ended: device [rows / width][n], best first: the value rounded to binary32, the row's number in its group, the token, and 1 if
+ * the row had ended or the token is end_token (NULL: not wanted).  Behind the last: -infinity, -1, -1, 0.  With n = width these are the next step's rows: out_scores may
+ * be scores and out_ended may be ended then.  The sum of a row: binary32 terms, off by 2^-21 of each other at most, and sums of 64 of them; the rest in
+ * binary64.  scores: device float [rows].  ws: cusa_beam_workspace_bytes, 256-byte aligned.  ended needs an end_token.
+ * Errors: INVALID_ARG, UNSUPPORTED (width > 32, n > 64, rows > 65535), WORKSPACE_TOO_SMALL, LAUNCH. */
+cusa_status cusa_beam_workspace_bytes(int32_t rows, int32_t vocab, int32_t n, size_t* bytes);
+cusa_status cusa_beam_select(const cusa_beams* beams, const float* scores, const int32_t* ended, float* out_scores, int32_t* parents, int32_t* tokens,
+                             int32_t* out_ended, void* ws, size_t ws_bytes, void* stream);
+
+/* Rows take over other rows' tokens.  Row b of a group takes those of row parents[b] of the group (in [0, width); anything else: none, the row ends up empty), of which
+ * there are held[.] (cut to [0, 16 * max_pages]), and, if grow != 0, it has a parent and ended[b] == 0 (ended NULL: none has), room for one more.
+ * A row that is to write into a page with tokens does so if no other row holds that page afterwards, or if all that do are to write and b is the lowest;
+ * else it gets a new page in its place and a copy to be made (cusa_kv_copy).  In order of the groups:
+ *   a group fits         if none of its rows gets beyond 16 * max_pages tokens
+ *   it is granted        if it fits and needs no new page, or the new pages of all groups that fit, up to and including it, are free; a group that is not granted
+ *                        stays as it is: lens = held, table_out = its rows of block_table, nothing else
+ *   lens[b]              tokens of the row with the new one
+ *   slots[b]             where the new token goes (page * 16 + position % 16); -1 where there is none, or the table names no page
+ *   copies[b]            from, to, tokens, 0: the first `tokens` tokens of page `from` belong into page `to`; -1, -1, 0, 0 where there is no copy
+ *   table_out            entries up to ceil(lens / 16); those behind are not written.  New pages come from the front of the queue in order of the rows
+ *   pages back           pages that rows of the group held and none holds any more go to the queue's end, in order of groups, columns and rows;
+ *                        they are not handed out by the same call
+ * Paged pools only.  table_out: device [batch][max_pages], may be the pool's block_table; lens may be held.  held, parents, ended, lens: device int32 [batch];
+ * slots: device int64 [batch]; copies: device int32 [batch][4], 16-byte aligned; granted (NULL: not wanted): device int32 [batch / width], 0 or 1.
+ * ws: cusa_kv_fork_workspace_bytes, 256-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED (contiguous caches among them), WORKSPACE_TOO_SMALL, LAUNCH. */
+size_t      cusa_kv_fork_workspace_bytes(int32_t batch, int32_t max_pages);
+cusa_status cusa_kv_fork(const cusa_pool* pool, int32_t width, const int32_t* held, const int32_t* parents, const int32_t* ended, int32_t grow, int32_t* table_out,
+                         int32_t* lens, int64_t* slots, int32_t* copies, int32_t* granted, void* ws, size_t ws_bytes, void* stream);
+
+/* Pages copied in all layers, K and V, all KV heads: of copy i the first copies[i][2] (cut to [0, 16]) tokens of page copies[i][0] into page copies[i][1]; copies whose
+ * pages are none of the pool's are left out.  No page is written by two copies or read by one and written by another.  copies: device int32 [n][4], 16-byte aligned.
+ * kv's seq_lens, max_seq_len and block_table are not read. */
+cusa_status cusa_kv_copy(const cusa_params* params, int32_t n_layers, const cusa_kv* kv_layers, const int32_t* copies, int32_t n, void* stream);
+
+/* The pages of groups, host memory.  entries: device int32 [batch / width][max_entries][4], 16-byte aligned: page, column, rows that hold it (bit b: row b of the
+ * group), 0.  count: device int32 [batch / width][2]: entries of the group, and how many at the front every row with tokens attends to as a whole. */
+typedef struct {
+    int32_t  width;
+    int32_t  max_entries;           /* of a group: min(width * ceil(max_seq_len / 16), n_pages) or more */
+    int32_t* entries;
+    int32_t* count;
+} cusa_shared;
+
+/* Each page of a group once: in order of the columns, then of the lowest row that holds it; entries of the table that name no page are left out, entries of the
+ * list behind the last are not written.  Of kv, block_table, max_pages, page_size, n_pages, seq_lens and max_seq_len are read.  Once a step: the layers share their tables.
+ * ws: cusa_shared_pages_workspace_bytes, 256-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL, LAUNCH. */
+size_t      cusa_shared_pages_workspace_bytes(int32_t batch, int32_t max_seq_len);
+cusa_status cusa_shared_pages(const cusa_kv* kv, int32_t batch, const cusa_shared* shared, void* ws, size_t ws_bytes, void* stream);
+
+/* FullAttention of every row's one query over its seq_lens[b] tokens (Eq. 1), as cusa_full_attn, but over the list that cusa_shared_pages made of the same tables and
+ * lengths: a page is read once for all rows that hold it.  A row without tokens gives zeros.  NaN and infinities in rows of the cache that a query does not attend to do not
+ * reach its output; an infinite value of a token that not all rows of the group attend to makes the outputs of those that do infinite whatever the weight, one that all
+ * attend to does if the weight is not below 2^-126 of the row's largest (else infinite or NaN).  Weights as in cusa_tree_attn: off by 2^-15 of themselves where width times the query
+ * heads of a KV head are up to 64, else rounded to bf16, in the product with V as in their sum.
+ * q: device bf16, row b head h at q + b * q_stride + h * 128 (q_stride a multiple of 8, >= n_q_heads * 128); out: device bf16 [batch][n_q_heads][128].  params->batch: rows, a multiple of
+ * width.  kv's block_table is not read.  ws: cusa_beam_attn_workspace_bytes, 256-byte aligned, content not preserved.
+ * Errors as cusa_full_attn, and UNSUPPORTED for contiguous caches, width > 32, pools of 2^31 or more rows, and max_entries above 147456 unless 147456 are enough. */
+cusa_status cusa_beam_attn_workspace_bytes(const cusa_params* params, int32_t max_seq_len, const cusa_shared* shared, size_t* bytes);
+cusa_status cusa_beam_attn(const cusa_params* params, const void* q, int64_t q_stride, const cusa_kv* kv, const cusa_shared* shared, void* out,
+                           void* ws, size_t ws_bytes, void* stream);
+
 const char* cusa_strerror(cusa_status status);
 
 /* Digest of the sources this binary was compiled from (16 hex digits); a loader compares it

@@ -28,6 +28,8 @@ EXPORTS = [
     "cusa_build_id", "cusa_probe_stream_read", "cusa_probe_traffic", "cusa_sparse_attn_noalloc", "cusa_noalloc_max_scratch_bytes",
     "cusa_kv_plan_workspace_bytes", "cusa_kv_plan", "cusa_kv_append", "cusa_tree_masks", "cusa_tree_workspace_bytes", "cusa_tree_attn",
     "cusa_kv_commit",
+    "cusa_beam_workspace_bytes", "cusa_beam_select", "cusa_kv_fork_workspace_bytes", "cusa_kv_fork", "cusa_kv_copy", "cusa_shared_pages_workspace_bytes",
+    "cusa_shared_pages", "cusa_beam_attn_workspace_bytes", "cusa_beam_attn",
 ]
 
 
@@ -66,6 +68,15 @@ class CusaRows(ctypes.Structure):
 class CusaTree(ctypes.Structure):
     _fields_ = [("tok_start", ctypes.c_void_p), ("masks", ctypes.c_void_p), ("max_tokens", ctypes.c_int32), ("max_nodes", ctypes.c_int32),
                 ("q_stride", ctypes.c_int64)]
+
+
+class CusaBeams(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("stride", ctypes.c_int64), ("rows", ctypes.c_int32), ("width", ctypes.c_int32),
+                ("vocab", ctypes.c_int32), ("n", ctypes.c_int32), ("end_token", ctypes.c_int32)]
+
+
+class CusaShared(ctypes.Structure):
+    _fields_ = [("width", ctypes.c_int32), ("max_entries", ctypes.c_int32), ("entries", ctypes.c_void_p), ("count", ctypes.c_void_p)]
 
 
 class CusaError(RuntimeError):
@@ -147,6 +158,19 @@ def load():
     lib.cusa_tree_attn.argtypes = [P(CusaParams), vp, P(CusaKv), P(CusaTree), vp, vp, vp, vp, sz, vp]
     lib.cusa_kv_commit.argtypes = [P(CusaParams), i32, P(CusaKv), vp, vp, i32, vp, vp, vp]
     for name in ("cusa_kv_plan", "cusa_kv_append", "cusa_tree_masks", "cusa_tree_workspace_bytes", "cusa_tree_attn", "cusa_kv_commit"):
+        getattr(lib, name).restype = ctypes.c_int
+    lib.cusa_beam_workspace_bytes.argtypes = [i32, i32, i32, P(sz)]
+    lib.cusa_beam_select.argtypes = [P(CusaBeams), vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.cusa_kv_fork_workspace_bytes.argtypes = [i32, i32]
+    lib.cusa_kv_fork_workspace_bytes.restype = sz
+    lib.cusa_kv_fork.argtypes = [P(CusaPool), i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.cusa_kv_copy.argtypes = [P(CusaParams), i32, P(CusaKv), vp, i32, vp]
+    lib.cusa_shared_pages_workspace_bytes.argtypes = [i32, i32]
+    lib.cusa_shared_pages_workspace_bytes.restype = sz
+    lib.cusa_shared_pages.argtypes = [P(CusaKv), i32, P(CusaShared), vp, sz, vp]
+    lib.cusa_beam_attn_workspace_bytes.argtypes = [P(CusaParams), i32, P(CusaShared), P(sz)]
+    lib.cusa_beam_attn.argtypes = [P(CusaParams), vp, ctypes.c_int64, P(CusaKv), P(CusaShared), vp, vp, sz, vp]
+    for name in ("cusa_beam_workspace_bytes", "cusa_beam_select", "cusa_kv_fork", "cusa_kv_copy", "cusa_shared_pages", "cusa_beam_attn_workspace_bytes", "cusa_beam_attn"):
         getattr(lib, name).restype = ctypes.c_int
     lib.cusa_probe_stream_read.argtypes = [vp, sz, vp, vp]
     lib.cusa_probe_stream_read.restype = ctypes.c_int
@@ -519,6 +543,162 @@ class KvCommit:
 
 def kv_commit(params, kv_layers, base, path, n_path, keep=None):
     KvCommit(params, kv_layers).run(base, path, n_path, keep)
+
+
+# ---- beam search over paged caches ---------------------------------------------
+
+def _need_group(what: str, rows: int, width: int):
+    _need(width >= 1 and rows >= 1 and rows % width == 0, f"{what}: groups of {width} rows in {rows}")
+
+
+def beam_workspace_bytes(rows: int, vocab: int, n: int) -> int:
+    b = ctypes.c_size_t(0)
+    _check(load().cusa_beam_workspace_bytes(rows, vocab, n, ctypes.byref(b)), "cusa_beam_workspace_bytes")
+    return int(b.value)
+
+
+def alloc_beam_workspace(rows: int, vocab: int, n: int, device="cuda") -> torch.Tensor:
+    return torch.empty(beam_workspace_bytes(rows, vocab, n), dtype=torch.uint8, device=device)
+
+
+def beam_select(logits, scores, width: int, out_scores, parents, tokens, ws, ended=None, out_ended=None, end_token: int = -1):
+    """The best continuations of every group of `width` rows: logits [rows, vocab] (bf16, fp16 or fp32; a view of wider rows, or contiguous), scores float32 [rows];
+    out_scores float32, parents, tokens and out_ended int32, [groups, n] each, best first.  ended int32 [rows]: rows that propose nothing but end_token."""
+    _need(logits.dim() == 2 and logits.dtype in DTYPES and logits.is_cuda, "beam_select: logits are [rows, vocab] in bf16, fp16 or fp32, on the GPU")
+    rows, vocab = logits.shape
+    _need_group("beam_select", rows, width)
+    strides = _strides(logits, (vocab, 1))
+    _need(strides[1] == 1 and strides[0] >= vocab, "beam_select: a row's logits stand side by side")
+    _need(out_scores.dim() == 2 and out_scores.shape[0] == rows // width, "beam_select: out_scores is [groups, n]")
+    n = out_scores.shape[1]
+    _need_int("beam_select", rows, torch.float32, scores)
+    _need_int("beam_select", rows, torch.int32, *(() if ended is None else (ended,)))
+    _need_rows("beam_select", "out_scores", out_scores, rows // width, n, torch.float32)
+    for name, t in (("parents", parents), ("tokens", tokens), ("out_ended", out_ended)):
+        if t is not None or name != "out_ended":
+            _need_rows("beam_select", name, t, rows // width, n, torch.int32)
+    _need_workspace("beam_select", ws)
+    d = CusaBeams(logits.data_ptr(), DTYPES[logits.dtype], strides[0], rows, width, vocab, n, end_token)
+    _check(load().cusa_beam_select(ctypes.byref(d), scores.data_ptr(), _ptr(ended), out_scores.data_ptr(), parents.data_ptr(), tokens.data_ptr(), _ptr(out_ended),
+                                   ws.data_ptr(), ws.numel(), _stream()), "cusa_beam_select")
+
+
+def fork_workspace_bytes(batch: int, max_pages: int) -> int:
+    return int(load().cusa_kv_fork_workspace_bytes(batch, max_pages))
+
+
+def alloc_fork_workspace(pool: PagePool) -> torch.Tensor:
+    return torch.empty(fork_workspace_bytes(*pool.block_table.shape), dtype=torch.uint8, device=pool.block_table.device)
+
+
+def kv_fork(pool: PagePool, width: int, held, parents, lens, slots, copies, ws, ended=None, grow: bool = True, table_out=None, state_out=None, granted=None):
+    """Rows of a group take over the tokens of the rows that they descend from (parents, int32, numbers within the group; -1: none), and with `grow` each that has a parent and has
+    not ended gets room for one token: lens int32 [B], slots int64 [B], copies int32 [B, 4] (from, to, tokens, 0: KvCopy makes them).
+    table_out, state_out: where the new table and the queue's state go instead of back into the pool."""
+    n, max_pages = pool.block_table.shape
+    _need_group("kv_fork", n, width)
+    _need_int("kv_fork", n, torch.int32, held, parents, lens, *(() if ended is None else (ended,)))
+    _need_int("kv_fork", n, torch.int64, slots)
+    _need_rows("kv_fork", "copies", copies, n, 4, torch.int32)
+    _need_rows("kv_fork", "table_out", pool.block_table if table_out is None else table_out, n, max_pages, torch.int32)
+    _need_int("kv_fork", 2, torch.int32, pool.state, pool.state if state_out is None else state_out)
+    _need_int("kv_fork", 1, torch.int32, pool.block_table, pool.ring)
+    _need_int("kv_fork", n // width, torch.int32, *(() if granted is None else (granted,)))
+    _need_workspace("kv_fork", ws)
+    d = pool.desc(state_out)
+    _check(load().cusa_kv_fork(ctypes.byref(d), width, held.data_ptr(), parents.data_ptr(), _ptr(ended), 1 if grow else 0,
+                               (pool.block_table if table_out is None else table_out).data_ptr(), lens.data_ptr(), slots.data_ptr(), copies.data_ptr(), _ptr(granted),
+                               ws.data_ptr(), ws.numel(), _stream()), "cusa_kv_fork")
+
+
+class KvCopy:
+    """Marshals the layers' caches once; run() copies pages in all of them."""
+
+    def __init__(self, params: CusaParams, kv_layers: Sequence[KvCache]):
+        self.params, self.n = params, len(kv_layers)
+        self._keep = list(kv_layers)
+        _need(all(kv.block_table is not None for kv in kv_layers), "kv_copy: paged caches")
+        self.kvs = (CusaKv * self.n)(*[_cache_desc("kv_copy", params, kv) for kv in kv_layers])
+
+    def run(self, copies):
+        """copies int32 [n, 4]: from, to, tokens, 0."""
+        n = copies.shape[0]
+        _need(copies.dim() == 2, "kv_copy: copies is [n, 4]")
+        _need_rows("kv_copy", "copies", copies, n, 4, torch.int32)
+        if n == 0:
+            return
+        _check(load().cusa_kv_copy(ctypes.byref(self.params), self.n, self.kvs, copies.data_ptr(), n, _stream()), "cusa_kv_copy")
+
+
+def kv_copy(params, kv_layers, copies):
+    KvCopy(params, kv_layers).run(copies)
+
+
+@dataclass
+class SharedPages:
+    """The pages of groups of `width` rows, each once, with the rows that hold it."""
+    width: int
+    entries: torch.Tensor       # int32 [groups, most, 4]: page, column, bits of the rows, 0
+    count: torch.Tensor         # int32 [groups, 2]: entries, and how many at the front all rows attend to as a whole
+
+    @staticmethod
+    def empty(batch: int, width: int, max_seq_len: int, n_pages: int, device="cuda") -> "SharedPages":
+        most = min(width * ((max_seq_len + 15) // 16), n_pages)
+        return SharedPages(width, torch.zeros((batch // width, most, 4), dtype=torch.int32, device=device), torch.zeros((batch // width, 2), dtype=torch.int32, device=device))
+
+    def desc(self, what: str, batch: int) -> CusaShared:
+        _need_group(what, batch, self.width)
+        e, groups = self.entries, batch // self.width
+        _need(e.dim() == 3 and e.shape[0] >= groups and e.shape[2] == 4, f"{what}: entries are [groups, most, 4]")
+        _need_int(what, groups * e.shape[1] * 4, torch.int32, e)
+        _need_rows(what, "count", self.count, groups, 2, torch.int32)
+        return CusaShared(self.width, e.shape[1], e.data_ptr(), self.count.data_ptr())
+
+
+def pages_workspace_bytes(batch: int, max_seq_len: int) -> int:
+    return int(load().cusa_shared_pages_workspace_bytes(batch, max_seq_len))
+
+
+def alloc_pages_workspace(batch: int, max_seq_len: int, device="cuda") -> torch.Tensor:
+    return torch.empty(pages_workspace_bytes(batch, max_seq_len), dtype=torch.uint8, device=device)
+
+
+def shared_pages(block_table, lens, max_seq_len: int, n_pages: int, shared: SharedPages, ws):
+    """Which pages the groups hold, from the rows' block table and lengths: once a step, for all its layers."""
+    _need(block_table.dim() == 2, "shared_pages: block_table is [rows, columns]")
+    n, columns = block_table.shape
+    _need_int("shared_pages", n, torch.int32, block_table, lens)
+    _need_workspace("shared_pages", ws)
+    d = shared.desc("shared_pages", n)
+    kv = CusaKv(None, None, KV_PAGED, 0, 0, 0, block_table.data_ptr(), columns, 16, n_pages, lens.data_ptr(), max_seq_len)
+    _check(load().cusa_shared_pages(ctypes.byref(kv), n, ctypes.byref(d), ws.data_ptr(), ws.numel(), _stream()), "cusa_shared_pages")
+
+
+def beam_attn_workspace_bytes(params: CusaParams, max_seq_len: int, shared: SharedPages) -> int:
+    n, d = ctypes.c_size_t(0), shared.desc("beam_attn", params.batch)
+    _check(load().cusa_beam_attn_workspace_bytes(ctypes.byref(params), max_seq_len, ctypes.byref(d), ctypes.byref(n)), "cusa_beam_attn_workspace_bytes")
+    return int(n.value)
+
+
+def alloc_beam_attn_workspace(params: CusaParams, max_seq_len: int, shared: SharedPages, device="cuda") -> torch.Tensor:
+    return torch.empty(beam_attn_workspace_bytes(params, max_seq_len, shared), dtype=torch.uint8, device=device)
+
+
+def beam_attn(params: CusaParams, q, kv: KvCache, shared: SharedPages, out, ws):
+    """Full attention of every row's token, q [B, H, 128] (a view of a fused projection's rows, or contiguous), over the pages of its group: each is read once
+    for all rows that hold it.  shared: of the same tables and lengths."""
+    n, heads, d = q.shape
+    strides = _strides(q, (heads * d, d, 1)) if n == 1 or heads == 1 else q.stride()
+    _need(q.dtype is torch.bfloat16 and n == params.batch and heads == params.n_q_heads and d == params.head_dim and strides[2] == 1 and strides[1] == d,
+          "beam_attn: q is bf16 [batch, n_q_heads, 128], heads side by side")
+    _need(q.is_cuda and out.is_cuda, "beam_attn: q and out are on the GPU")
+    _need(out.dtype is torch.bfloat16 and out.is_contiguous() and out.numel() >= n * heads * d, "beam_attn: out is bf16 [batch, n_q_heads, 128], contiguous")
+    _need_workspace("beam_attn", ws)
+    _need(kv.block_table is not None, "beam_attn: a paged cache")
+    s = shared.desc("beam_attn", n)
+    c = _cache_desc("beam_attn", params, kv)
+    _check(load().cusa_beam_attn(ctypes.byref(params), q.data_ptr(), strides[0], ctypes.byref(c), ctypes.byref(s), out.data_ptr(), ws.data_ptr(), ws.numel(), _stream()),
+           "cusa_beam_attn")
 
 
 def probe_stream_read(src: torch.Tensor, sink: torch.Tensor):

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <hip/hip_ext.h>
 
+#include <algorithm>
 #include <atomic>
 #include <mutex>
 #include <vector>
@@ -15,14 +16,16 @@ namespace cusa {
 
 // ------------------------------------------------------------------ profiling
 
-enum KernelId { KID_SCORE = 0, KID_TOPK, KID_UNION, KID_ATTN_FULL, KID_ATTN_SPARSE, KID_REDUCE, KID_ATTN_SELECT, KID_ATTN_PER_HEAD, KID_RHO_PER_HEAD, KID_RANK_AGG, KID_RECALL, KID_PROBE, KID_TOPK_SLICE, KID_TOPK_MERGE, KID_PROBE_GATHER, KID_PROBE_RW_SCATTER, KID_PROBE_RW_BURST, KID_SAMPLE_THRESHOLD, KID_TOPK_FILTERED, KID_PROBE_TILES, KID_TOPK_VALUES, KID_ATTN_FILTER, KID_KV_PLAN, KID_KV_FILL, KID_KV_APPEND, KID_TREE_MASKS, KID_TREE_ATTN, KID_TREE_REDUCE, KID_KV_COMMIT, KID_COUNT };
+enum KernelId { KID_SCORE = 0, KID_TOPK, KID_UNION, KID_ATTN_FULL, KID_ATTN_SPARSE, KID_REDUCE, KID_ATTN_SELECT, KID_ATTN_PER_HEAD, KID_RHO_PER_HEAD, KID_RANK_AGG, KID_RECALL, KID_PROBE, KID_TOPK_SLICE, KID_TOPK_MERGE, KID_PROBE_GATHER, KID_PROBE_RW_SCATTER, KID_PROBE_RW_BURST, KID_SAMPLE_THRESHOLD, KID_TOPK_FILTERED, KID_PROBE_TILES, KID_TOPK_VALUES, KID_ATTN_FILTER, KID_KV_PLAN, KID_KV_FILL, KID_KV_APPEND, KID_TREE_MASKS, KID_TREE_ATTN, KID_TREE_REDUCE, KID_KV_COMMIT, KID_BEAM_ROWS, KID_BEAM_MERGE, KID_KV_FORK, KID_FORK_TABLES, KID_FORK_PAGES, KID_KV_COPY, KID_SHARED_PAGES, KID_BEAM_ATTN, KID_BEAM_REDUCE, KID_COUNT };
 inline const char* const kKernelNames[KID_COUNT] = {"score_kernel", "topk_kernel", "union_kernel",
                                              "attn_kernel<full>", "attn_kernel<sparse>", "attn_reduce_kernel",
                                              "attn_kernel<full+score>", "attn_kernel<per-head>", "per_head_rho_kernel",
                                              "rank_aggregate_kernel", "recall_kernel", "probe_stream_read_kernel", "topk_kernel<slice>",
                                              "topk_kernel<merge>", "probe_traffic_kernel<gather>", "probe_traffic_kernel<scattered writes>",
                                              "probe_traffic_kernel<burst writes>", "sample_threshold_kernel", "topk_kernel<filtered>", "probe_traffic_kernel<stream>", "topk_values_kernel", "attn_kernel<full+filter>",
-                                             "kv_plan_kernel", "kv_fill_kernel", "kv_append_kernel", "tree_masks_kernel", "tree_attn_kernel", "tree_reduce_kernel", "kv_commit_kernel"};
+                                             "kv_plan_kernel", "kv_fill_kernel", "kv_append_kernel", "tree_masks_kernel", "tree_attn_kernel", "tree_reduce_kernel", "kv_commit_kernel",
+                                             "beam_rows_kernel", "beam_merge_kernel", "kv_fork_kernel", "fork_tables_kernel", "fork_pages_kernel", "kv_copy_kernel", "shared_pages_kernel",
+                                             "beam_attn_kernel", "beam_reduce_kernel"};
 
 // With the profiler on, every launch carries a start and a stop event that the runtime fills
 // from the dispatch's own begin and end timestamps (hipExtLaunchKernelGGL), which is what a
@@ -147,6 +150,47 @@ inline KvView make_view(const cusa_params* p, const cusa_kv* kv) {
     v.G = p->n_kv_heads;
     v.seq_lens = kv->seq_lens;
     return v;
+}
+
+constexpr int MAX_BATCH = 65535;           // a dimension of the grids
+constexpr int64_t MAX_STRIDE = 1 << 26;    // elements between two tokens: some rows' offset fits 32 bits of bytes
+
+inline cusa_status check_pool(const cusa_pool* p) {
+    if (!p || p->batch < 1) return CUSA_ERR_INVALID_ARG;
+    if (p->batch > MAX_BATCH) return CUSA_ERR_UNSUPPORTED;
+    if (p->layout == CUSA_KV_CONTIGUOUS) return p->capacity < 1 ? CUSA_ERR_INVALID_ARG : CUSA_OK;
+    if (p->layout != CUSA_KV_PAGED) return CUSA_ERR_INVALID_ARG;
+    if (p->page_size != PAGE) return CUSA_ERR_UNSUPPORTED;
+    if (!p->block_table || !p->ring || !p->state || !p->state_out || p->max_pages < 1 || p->n_pages < 1) return CUSA_ERR_INVALID_ARG;
+    if (p->n_pages > 0x7fffffff || (int64_t)p->batch * p->max_pages > 0x7fffffff) return CUSA_ERR_UNSUPPORTED;
+    return CUSA_OK;
+}
+
+// A cache that these kernels can address: check_kv's rules, row numbers and a token's stride that fit 31 bits.
+inline cusa_status check_cache(const cusa_params* p, const cusa_kv* kv, bool reads_tables) {
+    cusa_kv c;
+    if (!kv) return CUSA_ERR_INVALID_ARG;
+    c = *kv;
+    if (!reads_tables) {                   // seq_lens and block_table may be missing where they are not read
+        if (!c.seq_lens) c.seq_lens = reinterpret_cast<const int32_t*>(16);
+        if (c.layout == CUSA_KV_PAGED && !c.block_table) c.block_table = reinterpret_cast<const int32_t*>(16);
+        if (c.layout == CUSA_KV_PAGED) c.max_pages = 0x7fffffff / PAGE + 1;
+    }
+    const cusa_status st = check_kv(p, &c);
+    if (st != CUSA_OK) return st;
+    if (p->batch > MAX_BATCH || p->n_kv_heads > MAX_BATCH || kv->max_seq_len > (1 << 30)) return CUSA_ERR_UNSUPPORTED;
+    if (kv->layout == CUSA_KV_CONTIGUOUS && kv->stride_token > MAX_STRIDE) return CUSA_ERR_UNSUPPORTED;
+    if (kv->layout == CUSA_KV_PAGED && kv->n_pages > 0x7fffffff / PAGE / p->n_kv_heads) return CUSA_ERR_UNSUPPORTED;
+    return CUSA_OK;
+}
+
+inline CacheArgs cache_args(const cusa_params* p, const cusa_kv* kv) {
+    CacheArgs c;
+    c.kv = make_view(p, kv);
+    if (kv->layout != CUSA_KV_PAGED) c.kv.bt = nullptr;
+    c.n_pages = (int32_t)std::min<int64_t>(kv->n_pages, 0x7fffffff);
+    c.max_len = kv->max_seq_len;
+    return c;
 }
 
 // ------------------------------------------------------------------ helpers

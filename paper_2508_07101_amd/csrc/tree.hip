@@ -9,48 +9,7 @@ using namespace cusa;
 
 namespace {
 
-constexpr int MAX_BATCH = 65535;           // a dimension of the grids
-constexpr int64_t MAX_STRIDE = 1 << 26;    // elements between two tokens: some rows' offset fits 32 bits of bytes
-
 size_t plan_ws_bytes(int batch) { return 256 + align256((size_t)batch * sizeof(PlanSeq)); }
-
-cusa_status check_pool(const cusa_pool* p) {
-    if (!p || p->batch < 1) return CUSA_ERR_INVALID_ARG;
-    if (p->batch > MAX_BATCH) return CUSA_ERR_UNSUPPORTED;
-    if (p->layout == CUSA_KV_CONTIGUOUS) return p->capacity < 1 ? CUSA_ERR_INVALID_ARG : CUSA_OK;
-    if (p->layout != CUSA_KV_PAGED) return CUSA_ERR_INVALID_ARG;
-    if (p->page_size != PAGE) return CUSA_ERR_UNSUPPORTED;
-    if (!p->block_table || !p->ring || !p->state || !p->state_out || p->max_pages < 1 || p->n_pages < 1) return CUSA_ERR_INVALID_ARG;
-    if (p->n_pages > 0x7fffffff || (int64_t)p->batch * p->max_pages > 0x7fffffff) return CUSA_ERR_UNSUPPORTED;
-    return CUSA_OK;
-}
-
-// A cache that these kernels can address: check_kv's rules, row numbers and a token's stride that fit 31 bits.
-cusa_status check_cache(const cusa_params* p, const cusa_kv* kv, bool reads_tables) {
-    cusa_kv c;
-    if (!kv) return CUSA_ERR_INVALID_ARG;
-    c = *kv;
-    if (!reads_tables) {                   // seq_lens and block_table may be missing where they are not read
-        if (!c.seq_lens) c.seq_lens = reinterpret_cast<const int32_t*>(16);
-        if (c.layout == CUSA_KV_PAGED && !c.block_table) c.block_table = reinterpret_cast<const int32_t*>(16);
-        if (c.layout == CUSA_KV_PAGED) c.max_pages = 0x7fffffff / PAGE + 1;
-    }
-    const cusa_status st = check_kv(p, &c);
-    if (st != CUSA_OK) return st;
-    if (p->batch > MAX_BATCH || p->n_kv_heads > MAX_BATCH || kv->max_seq_len > (1 << 30)) return CUSA_ERR_UNSUPPORTED;
-    if (kv->layout == CUSA_KV_CONTIGUOUS && kv->stride_token > MAX_STRIDE) return CUSA_ERR_UNSUPPORTED;
-    if (kv->layout == CUSA_KV_PAGED && kv->n_pages > 0x7fffffff / PAGE / p->n_kv_heads) return CUSA_ERR_UNSUPPORTED;
-    return CUSA_OK;
-}
-
-CacheArgs cache_args(const cusa_params* p, const cusa_kv* kv) {
-    CacheArgs c;
-    c.kv = make_view(p, kv);
-    if (kv->layout != CUSA_KV_PAGED) c.kv.bt = nullptr;
-    c.n_pages = (int32_t)std::min<int64_t>(kv->n_pages, 0x7fffffff);
-    c.max_len = kv->max_seq_len;
-    return c;
-}
 
 template <int DTYPE>
 void launch_append(bool paged, dim3 grid, hipStream_t s, const AppendArgs& a) {
