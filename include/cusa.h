@@ -425,7 +425,8 @@ cusa_status cusa_shared_pages(const cusa_kv* kv, int32_t batch, const cusa_share
  * heads of a KV head are up to 64, else rounded to bf16, in the product with V as in their sum.
  * q: device bf16, row b head h at q + b * q_stride + h * 128 (q_stride a multiple of 8, >= n_q_heads * 128); out: device bf16 [batch][n_q_heads][128].  params->batch: rows, a multiple of
  * width.  kv's block_table is not read.  ws: cusa_beam_attn_workspace_bytes, 256-byte aligned, content not preserved.
- * Errors as cusa_full_attn, and UNSUPPORTED for contiguous caches, width > 32, pools of 2^31 or more rows, and max_entries above 147456 unless 147456 are enough. */
+ * Errors as cusa_full_attn, and UNSUPPORTED for contiguous caches, width > 32, pools of 2^31 or more rows, and more than 147456 pages
+ * in a group, min(max_entries, width * ceil(max_seq_len / 16)). */
 cusa_status cusa_beam_attn_workspace_bytes(const cusa_params* params, int32_t max_seq_len, const cusa_shared* shared, size_t* bytes);
 cusa_status cusa_beam_attn(const cusa_params* params, const void* q, int64_t q_stride, const cusa_kv* kv, const cusa_shared* shared, void* out,
                            void* ws, size_t ws_bytes, void* stream);

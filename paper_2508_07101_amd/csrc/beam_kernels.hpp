@@ -1,4 +1,4 @@
-// Device code for beam search over paged caches: groups of rows that share pages.
+// Device code for beam search over paged caches: groups of rows that share pages.  (Attention over a group's pages is a form of tree_attn_kernel.)
 //
 //   beam_rows_kernel     the best tokens of each row and the sum of its weights
 //   beam_merge_kernel    the best of a group's rows
@@ -7,7 +7,6 @@
 //   fork_pages_kernel    these to the queue's end
 //   kv_copy_kernel       pages copied in all layers
 //   shared_pages_kernel  each page of a group once, with the rows that hold it
-//   beam_attn_kernel     attention of the rows' queries over that list
 #pragma once
 #include "plan_scan.hpp"
 
@@ -16,7 +15,7 @@ namespace cusa {
 constexpr int BEAM_WIDTH = 32;             // rows of a group: a bit each
 constexpr int BEAM_MOST = 64;              // continuations of a group: a lane each
 
-typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+
 
 // ---------------------------------------------------------------- selection
 
@@ -428,103 +427,6 @@ __global__ __launch_bounds__(SHARED_COLS) void shared_pages_kernel(SharedArgs a)
         const int n = (int)min(found, (int64_t)a.max_entries);
         a.count[group * 2] = n;
         a.count[group * 2 + 1] = min(n, broken);
-    }
-}
-
-// ---------------------------------------------------------------- attention
-
-struct BeamAttnArgs {
-    CacheArgs cache;
-    const uint16_t* q;
-    int64_t q_stride;
-    const int32_t *entries, *count;
-    uint16_t* out;
-    float scale_log2e;
-    int32_t width, max_entries, H;
-};
-constexpr int BEAM_ATTN_WAVES = 4;
-
-// A workgroup for the g queries of a row and a KV head: every wave takes a page at a time, four lanes a token for the scores, two columns a lane for the values.
-template <int g>
-__global__ __launch_bounds__(64 * BEAM_ATTN_WAVES) void beam_attn_kernel(BeamAttnArgs a) {
-    __shared__ float q[g][D], acc_of[BEAM_ATTN_WAVES][g][D], m_of[BEAM_ATTN_WAVES][g], l_of[BEAM_ATTN_WAVES][g];
-    const int kvh = blockIdx.x, b = blockIdx.y, group = b / a.width, r = b % a.width, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int len = clampi(a.cache.kv.seq_lens[b], 0, a.cache.max_len), n = clampi(a.count[group * 2], 0, a.max_entries);
-    for (int i = threadIdx.x; i < g * D; i += 64 * BEAM_ATTN_WAVES)
-        q[i / D][i % D] = __uint_as_float((uint32_t)a.q[(int64_t)b * a.q_stride + (int64_t)(kvh * g + i / D) * D + i % D] << 16);
-    __syncthreads();
-    float m[g], l[g], acc[g][2];
-#pragma unroll
-    for (int h = 0; h < g; ++h) {
-        m[h] = LOWEST;
-        l[h] = acc[h][0] = acc[h][1] = 0.0f;
-    }
-    const i32x4* const list = reinterpret_cast<const i32x4*>(a.entries) + (int64_t)group * a.max_entries;
-    for (int e = wave; e < n; e += BEAM_ATTN_WAVES) {
-        const i32x4 entry = list[e];
-        const int64_t left = len - (int64_t)entry[1] * PAGE;
-        if (!((uint32_t)entry[2] >> r & 1) || (uint32_t)entry[0] >= (uint32_t)a.cache.n_pages || entry[1] < 0 || left <= 0) continue;
-        const int tokens = (int)min(left, (int64_t)PAGE), t = lane >> 2;
-        const int64_t at = ((int64_t)entry[0] * a.cache.kv.G + kvh) * PAGE * D;
-        const uint16_t* const k = a.cache.kv.k + at + t * D + (lane & 3) * 32;
-        const uint16_t* const v = a.cache.kv.v + at;
-        float x[g];
-#pragma unroll
-        for (int h = 0; h < g; ++h) x[h] = 0.0f;
-        for (int c = 0; c < 32; ++c) {
-            const float kc = __uint_as_float((uint32_t)k[c] << 16);
-#pragma unroll
-            for (int h = 0; h < g; ++h) x[h] += kc * q[h][(lane & 3) * 32 + c];
-        }
-#pragma unroll
-        for (int h = 0; h < g; ++h) {
-            x[h] += __shfl_xor(x[h], 1);
-            x[h] += __shfl_xor(x[h], 2);
-            x[h] = t < tokens ? x[h] * a.scale_log2e : -INFINITY;
-            float top = x[h];
-#pragma unroll
-            for (int o = 4; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-            top = fmaxf(top, m[h]);
-            const float f = exp2f(m[h] - top);
-            m[h] = top;
-            x[h] = exp2f(x[h] - top);
-            float sum = x[h];
-#pragma unroll
-            for (int o = 4; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-            l[h] = l[h] * f + sum;
-            acc[h][0] *= f;
-            acc[h][1] *= f;
-        }
-        for (int j = 0; j < tokens; ++j) {
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(v + j * D + lane * 2);
-#pragma unroll
-            for (int h = 0; h < g; ++h) {
-                const float p = __shfl(x[h], j * 4);
-                acc[h][0] += p * __uint_as_float(w << 16);
-                acc[h][1] += p * __uint_as_float(w & 0xffff0000u);
-            }
-        }
-    }
-#pragma unroll
-    for (int h = 0; h < g; ++h) {
-        acc_of[wave][h][lane * 2] = acc[h][0];
-        acc_of[wave][h][lane * 2 + 1] = acc[h][1];
-        if (lane == 0) {
-            m_of[wave][h] = m[h];
-            l_of[wave][h] = l[h];
-        }
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < g * D; i += 64 * BEAM_ATTN_WAVES) {
-        const int h = i / D;
-        float top = LOWEST, sum = 0.0f, o = 0.0f;
-        for (int w = 0; w < BEAM_ATTN_WAVES; ++w) top = fmaxf(top, m_of[w][h]);
-        for (int w = 0; w < BEAM_ATTN_WAVES; ++w) {
-            const float f = exp2f(m_of[w][h] - top);
-            sum += f * l_of[w][h];
-            o += f * acc_of[w][h][i % D];
-        }
-        a.out[((int64_t)b * a.H + kvh * g + h) * D + i % D] = f32_to_bf16_rne(sum == 0.0f ? 0.0f : o / sum);
     }
 }
 

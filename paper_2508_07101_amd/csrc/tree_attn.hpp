@@ -2,6 +2,9 @@
 //
 //   tree_attn_kernel    attention of a tree's nodes over the prefix (or the part of it that was chosen) and their branch
 //   tree_reduce_kernel  merges the pieces of a long prefix
+//
+// The second form of both, BEAM: instead of a tree's nodes the rows of a group, instead of a sequence's tokens the group's list of pages (cusa_shared), each with the rows that
+// hold it.  The pages that all rows attend to as a whole come first and are the prefix; behind them a row attends to the tokens of the pages that it holds, up to its length.
 #pragma once
 #include <type_traits>
 
@@ -34,6 +37,10 @@ struct TreeArgs {
     int32_t* pieces;       // of each sequence's tokens, for the merge
     float scale_log2e;
     int32_t batch, max_tokens, max_nodes, words, budget, H, g_shift, tile_rows /* 128 or 256 */, m_tiles, n_splits;
+    // groups: batch of them, of max_nodes rows each
+    const int32_t *entries, *count;
+    int32_t max_entries;   // of a group, looked at
+    int64_t entry_stride;
 };
 
 constexpr int TREE_WAVES = 8, TREE_THREADS = 64 * TREE_WAVES;
@@ -49,9 +56,18 @@ struct TreeSpan {
 // The workspace has rows for max_nodes nodes of a sequence.  A sequence that owns more rows of the packed arrays has only its first max_nodes looked at:
 // the next one's start there may lie behind the workspace's rows, and its partial results move up (to rows of their own: starts are apart by as much).
 __device__ __forceinline__ int part_row(const TreeArgs& a, int b, int start) { return min(start, b * a.max_nodes); }
-template <bool SPARSE>
+template <bool SPARSE, bool BEAM>
 __device__ __forceinline__ TreeSpan tree_span(const TreeArgs& a, int b) {
     TreeSpan s;
+    if constexpr (BEAM) {
+        const int n = clampi(a.count[b * 2], 0, a.max_entries);
+        s.n = a.max_nodes;
+        s.start = s.part = b * s.n;
+        s.before = 0;
+        s.pre = clampi(a.count[b * 2 + 1], 0, n) * PAGE;
+        s.all = n * PAGE;
+        return s;
+    }
     const int L = clampi(a.cache.kv.seq_lens[b], 0, a.cache.max_len);
     s.n = min(tree_span(a.tok_start, b, a.max_tokens, a.max_nodes, s.start), L);
     s.part = part_row(a, b, s.start);
@@ -65,12 +81,12 @@ __device__ __forceinline__ int tiles_of(int tokens) { return (tokens + TREE_TILE
 // and at most M tiles in one, pieces of ceil(M / floor(R / W)) tiles are R at most, and so are pieces of T / (R - W) tiles (a last piece each is shorter):
 // the first is exact for sequences of one length, the second close for any.  R: one to eight workgroups for each CU; more are better balanced, but
 // each costs about TREE_PIECE_COST tiles besides its own (its start, and partial sums written and read).
-template <bool SPARSE>
+template <bool SPARSE, bool BEAM>
 __device__ __forceinline__ int tree_piece(const TreeArgs& a, const TreeSpan& own) {   // tiles; 0: no sequence is cut
     if (a.n_splits == 1) return 0;
     int total = 0, pairs = 0, most = 0, piece = 0;
     for (int i = threadIdx.x & 63; i < a.batch || (a.batch == 1 && i < 64); i += 64) {   // (of one sequence every lane has the numbers already)
-        const TreeSpan o = a.batch == 1 ? own : tree_span<SPARSE>(a, i);
+        const TreeSpan o = a.batch == 1 ? own : tree_span<SPARSE, BEAM>(a, i);
         const int wgs = a.cache.kv.G * (((o.n << a.g_shift) + a.tile_rows - 1) >> __builtin_ctz(a.tile_rows)), t = tiles_of(o.all);
         total += t * wgs;
         pairs += wgs;
@@ -107,14 +123,14 @@ __device__ __forceinline__ int tree_piece(const TreeArgs& a, const TreeSpan& own
     piece = __builtin_amdgcn_readfirstlane(piece);
     return piece > 0 ? piece : most;                              // (0: more sequences than pieces would balance, which stay whole)
 }
-template <bool SPARSE>
+template <bool SPARSE, bool BEAM>
 __device__ __forceinline__ TreeSpan tree_work(const TreeArgs& a, int b) {
-    TreeSpan s = tree_span<SPARSE>(a, b);
-    int piece = tree_piece<SPARSE>(a, s);
+    TreeSpan s = tree_span<SPARSE, BEAM>(a, b);
+    int piece = tree_piece<SPARSE, BEAM>(a, s);
     if (a.n_splits == 1) {
         piece = tiles_of(s.all);
     } else {
-        piece = min(piece, (SPARSE ? TREE_LIST : TREE_LIST * PAGE) / TREE_TILE);   // what a workgroup's list has room for
+        piece = min(piece, (SPARSE ? TREE_LIST : (BEAM ? BEAM_LIST : TREE_LIST) * PAGE) / TREE_TILE);   // what a workgroup's list has room for
         piece = max(piece, (tiles_of(s.all) + a.n_splits - 1) / a.n_splits);       // what the launch has pieces for
     }
     s.chunk = piece * TREE_TILE;
@@ -164,12 +180,16 @@ __device__ __forceinline__ void wave_barrier() {
 }
 
 constexpr int TREE_RING = 128 * 1024;      // bytes of LDS for token tiles
+template <bool BEAM>
 struct TreeLds {
+    static constexpr int LIST = BEAM ? BEAM_LIST : TREE_LIST;
     __attribute__((aligned(16))) unsigned char ring[TREE_RING];
-    int32_t list[TREE_LIST];
+    int32_t list[LIST];
     float m[TREE_ROWS], l[TREE_ROWS];      // of every row, a set for each team
-    uint32_t odd[TREE_MAX_NODES / 32];     // nodes among this workgroup's tokens with a value that is not finite
-    int32_t first_bad;                     // entry of the list that names no row
+    uint32_t odd[(BEAM ? LIST : TREE_MAX_NODES) / 32];   // nodes (pages) among this workgroup's tokens with a value that is not finite
+    int32_t first_bad;                     // entry of the list that names no row (0: a page has such a value)
+    int32_t col[BEAM ? LIST : 1];          // of a group's page: its column, and the rows that hold it
+    uint32_t holders[BEAM ? LIST : 1];
 };
 
 typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -401,8 +421,8 @@ __device__ __forceinline__ uint32_t add_washed(TreeRow& r, const W& p, uint32_t 
 // query heads of a KV head): 4 rows 6.5 TB/s, 32 rows 6.2, 64 rows 5.6 to 5.9, 128 rows 5.2 to 5.4 TB/s and 660 to 690 TFLOP/s; above that the matrix cores and the softmax
 // beside them: 256 rows 856 to 873 TFLOP/s, 512 rows 933 (a library product of 8192^3 reaches 1210).  192 rows cost as much as 256 do on half of the SIMDs: 717.  One
 // sequence of 32768 tokens, 240 rows: 50 us, of which about 29 are the tiles' arrival, 6 the way to the first tile, 5 the partial sums' way out.
-template <int RG, bool PAGED, bool SPARSE>
-__device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, TreeLds& lds, int b, int kvh, int row0, int split, int begin, int end) {
+template <int RG, bool PAGED, bool SPARSE, bool BEAM>
+__device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, TreeLds<BEAM>& lds, int b, int kvh, int row0, int split, int begin, int end) {
     constexpr int TEAMS = TREE_WAVES / RG;
     constexpr int TT = TREE_TILE;                                 // tokens of a team's tile
     constexpr int ROWS = 32 * RG;
@@ -416,7 +436,7 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int team = wave / RG, mine = wave % RG, half = lane >> 5, col = lane & 31;
     const int g = 1 << a.g_shift, rows = s.n << a.g_shift;
-    if (tid < TREE_MAX_NODES / 32) lds.odd[tid] = 0;
+    if (tid < (BEAM ? BEAM_LIST : TREE_MAX_NODES) / 32) lds.odd[tid] = 0;
     if (tid == 0) lds.first_bad = 0x7fffffff;
     __syncthreads();
 
@@ -439,6 +459,7 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
     for (int d = 0; d < 4; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) row.o[d][i] = 0.0f;
+    const int row_len = BEAM ? clampi(a.cache.kv.seq_lens[s.start + node], 0, a.cache.max_len) : 0;
     const bool idle = row0 + mine * 32 >= rows;                   // a wave without rows loads its share and computes nothing
 
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds.ring;
@@ -452,7 +473,18 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
 
     const int steps = (end - begin + TT * TEAMS - 1) / (TT * TEAMS);
     int good = end;                                               // tokens before this one are all there
-    if (LIST) {
+    if constexpr (BEAM) {
+        const int entries = (end - begin) / PAGE;
+        const i32x4* const list = reinterpret_cast<const i32x4*>(a.entries) + b * a.entry_stride + begin / PAGE;
+        for (int e = tid; e < entries; e += TREE_THREADS) {
+            const i32x4 x = list[e];
+            const bool is = (uint32_t)x[0] < (uint32_t)a.cache.n_pages && x[1] >= 0;   // (all are, of a list that cusa_shared_pages made for this pool)
+            lds.list[e] = is ? (x[0] * a.cache.kv.G + kvh) * PAGE : 0;
+            lds.col[e] = x[1];
+            lds.holders[e] = is ? (uint32_t)x[2] : 0;
+        }
+        __syncthreads();
+    } else if (LIST) {
         const int entries = SPARSE ? steps * TT * TEAMS : (end - begin + PAGE - 1) / PAGE;
         constexpr int RUN = 4;                                    // entries of a thread under way at once
         for (int e0 = tid; e0 < entries; e0 += RUN * TREE_THREADS) {
@@ -509,6 +541,19 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
     auto attended = [&](int it, uint32_t& there, uint32_t& common) -> uint32_t {
         const int t = begin + (it * TEAMS + team) * TT;
         there = t + 32 <= end ? 0xffffffffu : t >= end ? 0u : (1u << (end - t)) - 1;
+        if constexpr (BEAM) {
+            const int in_front = s.pre - t;                       // tokens of pages that all rows attend to as a whole
+            common = in_front >= 32 ? 0xffffffffu : in_front >= 16 ? 0xffffu : 0u;
+            common &= there;
+            uint32_t own = 0;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int e = min((t - begin) / PAGE + j, BEAM_LIST - 1);
+                const int n = (int)max(min((int64_t)row_len - (int64_t)lds.col[e] * PAGE, (int64_t)PAGE), (int64_t)0);
+                if (lds.holders[e] >> (node & 31) & 1) own |= ((1u << n) - 1) << (16 * j);
+            }
+            return (common | own) & there;
+        }
         if (LIST && t + 32 > good) there = (uint32_t)__ballot(t + col < end && lds.list[SPARSE ? t - begin + col : (t - begin + col) >> 4] >= 0);
         const int from = s.pre - t;                               // tokens of the prefix in this step
         const uint32_t prefix = from >= 32 ? 0xffffffffu : from <= 0 ? 0u : (1u << from) - 1;
@@ -518,8 +563,9 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
     auto note_odd = [&](int it, uint32_t odd) {                   // nodes with values that were left out
         const int t = begin + (it * TEAMS + team) * TT;
         for (; odd; odd &= odd - 1) {
-            const int i = t + __builtin_ctz(odd) - s.pre;
+            const int i = BEAM ? (t - begin + __builtin_ctz(odd)) / PAGE : t + __builtin_ctz(odd) - s.pre;
             atomicOr(&lds.odd[i >> 5], 1u << (i & 31));
+            if (BEAM) lds.first_bad = 0;
         }
     };
     const int plain = max(0, min(s.pre, good) - begin) / (TT * TEAMS);   // tiles that every row attends to as a whole: the first ones
@@ -776,8 +822,12 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
     __syncthreads();
     const bool whole = s.chunk >= s.all;
     bool any_odd = false;
+    if constexpr (BEAM) {
+        any_odd = lds.first_bad == 0;
+    } else {
 #pragma unroll
-    for (int i = 0; i < TREE_MAX_NODES / 32; ++i) any_odd |= lds.odd[i] != 0;
+        for (int i = 0; i < TREE_MAX_NODES / 32; ++i) any_odd |= lds.odd[i] != 0;
+    }
     // (four items of a thread at a time: their reads are under way together)
     constexpr int ITEMS = ROWS * 32 / TREE_THREADS, RUN = ITEMS < 4 ? ITEMS : 4;
     static_assert(ITEMS % RUN == 0, "whole runs");
@@ -809,7 +859,28 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
         for (int i = 0; i < RUN; ++i) {
             const int row = row0 + (i0 + i) * (TREE_THREADS / 32) + (tid >> 5);
             if (row >= rows) break;
-            if (any_odd) {
+            if constexpr (BEAM) {
+                const int of = s.start + (row >> a.g_shift), len = a.cache.kv.seq_lens[of];
+                if (any_odd) {                                    // (as below, for the tokens of pages)
+                    for (int e = 0; e < (end - begin) / PAGE; ++e) {
+                        if (!(lds.odd[e >> 5] >> (e & 31) & 1) || !(lds.holders[e] >> (of - s.start) & 1)) continue;
+                        const int64_t left = (int64_t)min(len, a.cache.max_len) - (int64_t)lds.col[e] * PAGE;
+                        for (int j = 0; j < (int)min(left, (int64_t)PAGE); ++j) {
+                            const u32x2 w = *reinterpret_cast<const u32x2*>(a.cache.kv.v + (int64_t)(lds.list[e] + j) * D + c * 4);
+#pragma unroll
+                            for (int n = 0; n < 4; ++n) {
+                                const uint32_t x = (n & 1) ? w[n >> 1] & 0xffff0000u : w[n >> 1] << 16;
+                                if ((x & 0x7f800000u) == 0x7f800000u) v[i][n] += __uint_as_float(x);
+                            }
+                        }
+                    }
+                }
+                if (len <= 0) {                                   // a row without tokens
+                    top[i] = LOWEST;
+                    sum[i] = 0.0f;
+                    v[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                }
+            } else if (any_odd) {
                 // Nodes with values that are not finite: the rows that attend to them get those values (whatever the weight: it is not 0).
                 const uint64_t* mask = a.masks + (int64_t)(s.start + (row >> a.g_shift)) * a.words;
                 for (int n = 0; n < s.n; ++n) {
@@ -840,34 +911,48 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
 }
 
 // Which form a workgroup takes goes by the rows that its own tree has, not by the bound: trees of a batch differ.
-template <bool PAGED, bool SPARSE>
+template <bool PAGED, bool SPARSE, bool BEAM = false>
 __global__ __launch_bounds__(TREE_THREADS, 2) void tree_attn_kernel(TreeArgs a) {
-    __shared__ TreeLds lds;
+    __shared__ TreeLds<BEAM> lds;
     // Workgroups go to the 8 XCDs in turn: those that share a KV head's tokens come 8 apart, to the same L2.  First pieces first: behind them come
     // those that short sequences do not have.
     const uint32_t turn = blockIdx.x >> 3, m_tile = turn % (uint32_t)a.m_tiles, unit = turn / (uint32_t)a.m_tiles * 8 + (blockIdx.x & 7);
     const uint32_t G = a.cache.kv.G, pairs = G * (uint32_t)a.batch, pair = unit % pairs;
     const int split = unit / pairs, b = pair / G, kvh = pair - b * G, row0 = m_tile * a.tile_rows;
     if (split >= a.n_splits) return;
-    const TreeSpan s = tree_work<SPARSE>(a, b);
+    const TreeSpan s = tree_work<SPARSE, BEAM>(a, b);
     const int left = min((s.n << a.g_shift) - row0, a.tile_rows), begin = split * s.chunk;
+    if (BEAM && s.all == 0 && split == 0) {                       // a group without tokens
+        for (int i = threadIdx.x; i < (left << 5); i += TREE_THREADS) {
+            const int row = row0 + (i >> 5);
+            const int64_t to = (int64_t)(s.start + (row >> a.g_shift)) * a.H + (kvh << a.g_shift) + (row & ((1 << a.g_shift) - 1));
+            *reinterpret_cast<u32x2*>(a.out + to * D + (i & 31) * 4) = u32x2{0, 0};
+        }
+        if (a.n_splits > 1 && kvh == 0 && m_tile == 0 && threadIdx.x == 0) a.pieces[b] = 0;
+    }
     if (left <= 0 || begin >= s.all) return;
     // (a piece has no more tokens or pages than the list has room for: plan_tree)
     const int end = min(begin + s.chunk, s.all);
     if (a.n_splits > 1 && split == 0 && kvh == 0 && m_tile == 0 && threadIdx.x == 0) a.pieces[b] = (s.all + s.chunk - 1) / s.chunk;
-    if (left <= 32) tree_rows<1, PAGED, SPARSE>(a, s, lds, b, kvh, row0, split, begin, end);
-    else if (left <= 64) tree_rows<2, PAGED, SPARSE>(a, s, lds, b, kvh, row0, split, begin, end);
-    else if (left <= 128) tree_rows<4, PAGED, SPARSE>(a, s, lds, b, kvh, row0, split, begin, end);
-    else tree_rows<8, PAGED, SPARSE>(a, s, lds, b, kvh, row0, split, begin, end);
+    if (left <= 32) tree_rows<1, PAGED, SPARSE, BEAM>(a, s, lds, b, kvh, row0, split, begin, end);
+    else if (left <= 64) tree_rows<2, PAGED, SPARSE, BEAM>(a, s, lds, b, kvh, row0, split, begin, end);
+    else if (left <= 128) tree_rows<4, PAGED, SPARSE, BEAM>(a, s, lds, b, kvh, row0, split, begin, end);
+    else tree_rows<8, PAGED, SPARSE, BEAM>(a, s, lds, b, kvh, row0, split, begin, end);
 }
 
 // A wave for a row: a lane for each piece's weight, then two columns a lane.  Bound by the partial sums' way back from memory: 31 MB of one sequence (1920 rows in 32
 // pieces) take 6.0 us, 5.2 TB/s.
 constexpr int REDUCE_WAVES = 4;
+template <bool BEAM = false>
 __global__ __launch_bounds__(64 * REDUCE_WAVES) void tree_reduce_kernel(TreeArgs a) {
     const int lane = threadIdx.x & 63, b = blockIdx.y;
-    int start;
-    const int n = min(tree_span(a.tok_start, b, a.max_tokens, a.max_nodes, start), clampi(a.cache.kv.seq_lens[b], 0, a.cache.max_len));
+    int start, n;
+    if constexpr (BEAM) {
+        start = b * a.max_nodes;
+        n = a.max_nodes;
+    } else {
+        n = min(tree_span(a.tok_start, b, a.max_tokens, a.max_nodes, start), clampi(a.cache.kv.seq_lens[b], 0, a.cache.max_len));
+    }
     if (n == 0) return;                                           // (without a node, nobody has written how many pieces there are)
     const int pieces = a.pieces[b];
     if (pieces <= 1) return;

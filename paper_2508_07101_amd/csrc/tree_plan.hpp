@@ -17,8 +17,9 @@ constexpr int TREE_ROWS = 256;          // rows (node, query head) of one KV hea
 
 // Entries of a workgroup's list of cache rows: tokens of a chosen prefix, pages of 16 of a whole one.
 constexpr int TREE_LIST = 5120;
-enum TreeKind { TREE_FULL, TREE_CHOSEN };
-inline int tree_piece_most(TreeKind kind) { return kind == TREE_CHOSEN ? TREE_LIST : TREE_LIST * 16; }
+constexpr int BEAM_LIST = 2304;         // pages of a group, with their columns and the rows that hold them
+enum TreeKind { TREE_FULL, TREE_CHOSEN, TREE_GROUP /* tokens: those of a group's pages */ };
+inline int tree_piece_most(TreeKind kind) { return kind == TREE_CHOSEN ? TREE_LIST : (kind == TREE_GROUP ? BEAM_LIST : TREE_LIST) * 16; }
 inline bool tree_len_served(TreeKind kind, int64_t len) { return len <= (int64_t)tree_piece_most(kind) * TREE_MAX_SPLITS; }
 
 // Tokens up to which sequences stay whole: what a workgroup of up to 64 rows takes in three steps (its teams take 256 or 128 tokens a step), which is less than the
