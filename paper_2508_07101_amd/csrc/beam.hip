@@ -18,16 +18,35 @@ cusa_status check_workspace(const void* ws, size_t have, size_t need) {
     return have < need ? CUSA_ERR_WORKSPACE_TOO_SMALL : CUSA_OK;
 }
 
-struct BeamWs {
-    size_t ln_sum, top, best, total;
+// Parts of a row, a wave each: enough waves for the chip, but parts of 4 KB at least, and a lane each where they come together.
+constexpr int PART_LEAST = 256;            // loads of 16 bytes
+struct BeamParts {
+    int parts, len;                        // len: loads of 16 bytes
 };
-BeamWs beam_ws(int32_t rows, int32_t n) {
+BeamParts beam_parts(int32_t rows, int32_t vocab, int size) {
+    const int64_t loads = std::max<int64_t>(1, ((int64_t)vocab * size + 15) / 16);
+    const int64_t want = std::min<int64_t>({(loads + PART_LEAST - 1) / PART_LEAST, std::max(1, 4096 / rows), 64});
+    const int64_t len = ((loads + want - 1) / want + 63) / 64 * 64;
+    return {(int)((loads + len - 1) / len), (int)len};
+}
+
+struct BeamWs {
+    size_t sum, top, best, total;
+};
+BeamWs beam_ws(int32_t rows, int parts, int32_t n) {
     BeamWs w;
-    w.ln_sum = 0;
-    w.top = align256((size_t)rows * 8);
-    w.best = w.top + align256((size_t)rows * 4);
-    w.total = w.best + align256((size_t)rows * n * 8);
+    w.sum = 0;
+    w.top = align256((size_t)rows * parts * 8);
+    w.best = w.top + align256((size_t)rows * parts * 4);
+    w.total = w.best + align256((size_t)rows * parts * n * 8);
     return w;
+}
+
+template <int DTYPE>
+void launch_rows(hipStream_t s, const BeamArgs& a) {
+    const dim3 grid((unsigned)(((int64_t)a.rows * a.parts + BEAM_WAVES - 1) / BEAM_WAVES));
+    if (a.part_len <= PART_LEAST) launch(KID_BEAM_ROWS, beam_rows_kernel<DTYPE, 4>, grid, 64 * BEAM_WAVES, 0, s, a);
+    else launch(KID_BEAM_ROWS, beam_rows_kernel<DTYPE, 8>, grid, 64 * BEAM_WAVES, 0, s, a);
 }
 
 cusa_status check_beams(int32_t rows, int32_t vocab, int32_t n) {
@@ -69,7 +88,7 @@ cusa_status cusa_beam_workspace_bytes(int32_t rows, int32_t vocab, int32_t n, si
     const cusa_status st = check_beams(rows, vocab, n);
     if (st != CUSA_OK) return st;
     if (!bytes) return CUSA_ERR_INVALID_ARG;
-    *bytes = beam_ws(rows, n).total;
+    *bytes = beam_ws(rows, std::max(beam_parts(rows, vocab, 2).parts, beam_parts(rows, vocab, 4).parts), n).total;   // of any type
     return CUSA_OK;
 }
 
@@ -84,7 +103,8 @@ cusa_status cusa_beam_select(const cusa_beams* beams, const float* scores, const
     if ((uintptr_t)beams->logits & (beams->dtype == CUSA_F32 ? 3 : 1)) return CUSA_ERR_INVALID_ARG;
     if (beams->end_token < -1 || beams->end_token >= beams->vocab || (ended && beams->end_token < 0)) return CUSA_ERR_INVALID_ARG;
     if (beams->n != beams->width && (out_scores == scores || (out_ended && out_ended == ended))) return CUSA_ERR_INVALID_ARG;
-    const BeamWs w = beam_ws(beams->rows, beams->n);
+    const BeamParts parts = beam_parts(beams->rows, beams->vocab, beams->dtype == CUSA_F32 ? 4 : 2);
+    const BeamWs w = beam_ws(beams->rows, parts.parts, beams->n);
     if ((st = check_workspace(ws, ws_bytes, w.total)) != CUSA_OK) return st;
     BeamArgs a = {};
     a.logits = beams->logits;
@@ -95,7 +115,7 @@ cusa_status cusa_beam_select(const cusa_beams* beams, const float* scores, const
     a.parents = parents;
     a.tokens = tokens;
     a.out_ended = out_ended;
-    a.ln_sum = ws_ptr<double>(ws, w.ln_sum);
+    a.sum = ws_ptr<double>(ws, w.sum);
     a.top = ws_ptr<float>(ws, w.top);
     a.best = ws_ptr<uint64_t>(ws, w.best);
     a.rows = beams->rows;
@@ -103,15 +123,16 @@ cusa_status cusa_beam_select(const cusa_beams* beams, const float* scores, const
     a.vocab = beams->vocab;
     a.n = beams->n;
     a.end_token = beams->end_token;
+    a.parts = parts.parts;
+    a.part_len = parts.len;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const dim3 grid((unsigned)beams->rows);
     switch (beams->dtype) {
-        case CUSA_BF16: launch(KID_BEAM_ROWS, beam_rows_kernel<CUSA_BF16>, grid, BEAM_THREADS, 0, s, a); break;
-        case CUSA_F16: launch(KID_BEAM_ROWS, beam_rows_kernel<CUSA_F16>, grid, BEAM_THREADS, 0, s, a); break;
-        default: launch(KID_BEAM_ROWS, beam_rows_kernel<CUSA_F32>, grid, BEAM_THREADS, 0, s, a); break;
+        case CUSA_BF16: launch_rows<CUSA_BF16>(s, a); break;
+        case CUSA_F16: launch_rows<CUSA_F16>(s, a); break;
+        default: launch_rows<CUSA_F32>(s, a); break;
     }
     if (launch_status() != CUSA_OK) return CUSA_ERR_LAUNCH;
-    launch(KID_BEAM_MERGE, beam_merge_kernel, dim3((unsigned)(beams->rows / beams->width)), BEAM_THREADS, 0, s, a);
+    launch(KID_BEAM_MERGE, beam_merge_kernel, dim3((unsigned)(beams->rows / beams->width)), 64 * MERGE_WAVES, 0, s, a);
     return launch_status();
 }
 

@@ -26,10 +26,10 @@ struct BeamArgs {
     const int32_t* ended;
     float* out_scores;
     int32_t *parents, *tokens, *out_ended;
-    double* ln_sum;                        // [rows]: logarithm of the sum of weights; NaN: the row proposes nothing
-    float* top;                            // [rows]: the largest logit
-    uint64_t* best;                        // [rows][n]: keys, best first; 0: none
-    int32_t rows, width, vocab, n, end_token;
+    float* top;                            // [rows][parts]: the largest logit
+    double* sum;                           // [rows][parts]: weights relative to it
+    uint64_t* best;                        // [rows][parts][n]: keys, best first; 0: none
+    int32_t rows, width, vocab, n, end_token, parts, part_len /* in 16 bytes */;
 };
 
 // Larger is better: the logit's order above, of equal ones the lower token.  0 is no token's key.
@@ -43,103 +43,273 @@ __device__ __forceinline__ float key_logit(uint64_t key) {
 }
 __device__ __forceinline__ uint32_t key_token(uint64_t key) { return 0xffffffffu - (uint32_t)key; }
 
-template <int DTYPE>                       // cusa_dtype
-__device__ __forceinline__ float load_logit(const void* p, int64_t at) {
-    if constexpr (DTYPE == 0) return __uint_as_float((uint32_t)static_cast<const uint16_t*>(p)[at] << 16);
-    else if constexpr (DTYPE == 1) return (float)static_cast<const _Float16*>(p)[at];
-    else return static_cast<const float*>(p)[at];
-}
-
-constexpr int BEAM_THREADS = 256;
-
-// A workgroup for a row: the largest logit, the sum of weights, then the best tokens one after the other, each in a pass of its own.
-template <int DTYPE>
-__global__ __launch_bounds__(BEAM_THREADS) void beam_rows_kernel(BeamArgs a) {
-    __shared__ uint64_t key[BEAM_THREADS / 64];
-    __shared__ double part[BEAM_THREADS / 64];
-    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t at = (int64_t)row * a.stride;
-    auto largest = [&](uint64_t k) {
+__device__ __forceinline__ uint64_t shuffle_key(uint64_t k, int mask) { return __shfl_xor((unsigned long long)k, mask); }
+// The wave's 64 values in falling order, over the lanes: a bitonic network.
+template <typename T, typename F>
+__device__ __forceinline__ T sort_lanes(T v, int lane, F other) {
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) k = max(k, (uint64_t)__shfl_xor((unsigned long long)k, o));
-        __syncthreads();
-        if (lane == 0) key[wave] = k;
-        __syncthreads();
-        return max(max(key[0], key[1]), max(key[2], key[3]));
-    };
-    uint64_t mine = 0;
-    for (int t = tid; t < a.vocab; t += BEAM_THREADS) {
-        const float x = load_logit<DTYPE>(a.logits, at + t);
-        if (x > -INFINITY) mine = max(mine, beam_key(x, t));
-    }
-    uint64_t next = largest(mine);
-    const float top = next ? key_logit(next) : -INFINITY;
-    double sum = 0.0;
-    for (int t = tid; t < a.vocab; t += BEAM_THREADS) sum += (double)exp2f((load_logit<DTYPE>(a.logits, at + t) - top) * 1.4426950408889634f);
+    for (int size = 2; size <= 64; size <<= 1)
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-    if (lane == 0) part[wave] = sum;
-    __syncthreads();
-    sum = part[0] + part[1] + part[2] + part[3];
-    if (tid == 0) {
-        a.top[row] = top;
-        a.ln_sum[row] = log(sum);                          // (NaN of a NaN, of an infinity less itself, of nothing)
-    }
-    for (int i = 0; i < a.n; ++i) {
-        if (tid == 0) a.best[(int64_t)row * a.n + i] = next;
-        mine = 0;
-        for (int t = tid; t < a.vocab; t += BEAM_THREADS) {
-            const float x = load_logit<DTYPE>(a.logits, at + t);
-            if (!(x > -INFINITY)) continue;
-            const uint64_t k = beam_key(x, t);
-            if (k < next) mine = max(mine, k);
+        for (int stride = size >> 1; stride > 0; stride >>= 1) {
+            const T o = other(v, stride);
+            v = (((lane & stride) == 0) == ((lane & size) == 0)) ? (v > o ? v : o) : (v > o ? o : v);
         }
-        next = largest(mine);
+    return v;
+}
+// The 64 largest of two such lists, in falling order.
+__device__ __forceinline__ uint64_t merge_lanes(uint64_t list, uint64_t batch, int lane) {
+    const uint64_t turned = shuffle_key(batch, 63);
+    uint64_t v = list > turned ? list : turned;
+#pragma unroll
+    for (int stride = 32; stride > 0; stride >>= 1) {
+        const uint64_t o = shuffle_key(v, stride);
+        v = (lane & stride) == 0 ? (v > o ? v : o) : (v > o ? o : v);
     }
+    return v;
+}
+__device__ __forceinline__ uint64_t lane_key(uint64_t k, int lane) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, lane);
 }
 
-// A workgroup for a group: a thread for every candidate of its rows at a time, and the best of all that are left, n times.
-__global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs a) {
-    __shared__ double value[BEAM_WIDTH * BEAM_MOST];
-    __shared__ int32_t token[BEAM_WIDTH * BEAM_MOST], over[BEAM_WIDTH];
-    const int group = blockIdx.x, row0 = group * a.width, all = a.width * a.n;
-    for (int i = threadIdx.x; i < all; i += BEAM_THREADS) {
-        const int r = row0 + i / a.n, j = i % a.n;
-        const float s = a.scores[r];
-        const bool ended = a.ended && a.ended[r] != 0;
-        double v = -INFINITY;
-        int t = -1;
-        if (__builtin_isfinite(s)) {
-            if (ended) {
-                if (j == 0) {
-                    v = s;
-                    t = a.end_token;
-                }
-            } else if (const uint64_t k = a.best[(int64_t)r * a.n + j]; k && !__builtin_isnan(a.ln_sum[r])) {
-                v = (double)s + (((double)key_logit(k) - a.top[r]) - a.ln_sum[r]);
-                t = key_token(k);
+template <int DTYPE>                       // cusa_dtype
+struct Logits {
+    static constexpr int SIZE = DTYPE == 2 ? 4 : 2, PER = 16 / SIZE;
+    static constexpr uint32_t NONE = DTYPE == 0 ? 0xff80ff80u : DTYPE == 1 ? 0xfc00fc00u : 0xff800000u;   // -infinity
+    static __device__ __forceinline__ float at(const u32x4& x, int k) {
+        if constexpr (DTYPE == 0) return __uint_as_float((k & 1) ? x[k >> 1] & 0xffff0000u : x[k >> 1] << 16);
+        else if constexpr (DTYPE == 1) return (float)__builtin_bit_cast(_Float16, (uint16_t)((k & 1) ? x[k >> 1] >> 16 : x[k >> 1] & 0xffffu));
+        else return __uint_as_float(x[k]);
+    }
+    static __device__ __forceinline__ float one(const void* p, int64_t i) {
+        if constexpr (DTYPE == 0) return __uint_as_float((uint32_t)static_cast<const uint16_t*>(p)[i] << 16);
+        else if constexpr (DTYPE == 1) return (float)static_cast<const _Float16*>(p)[i];
+        else return static_cast<const float*>(p)[i];
+    }
+};
+
+constexpr int BEAM_WAVES = 4;
+constexpr float LOG2E = 1.4426950408889634f;
+
+__device__ __forceinline__ void lds_of_wave() {            // what the wave's other lanes wrote to LDS is there
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// A wave for a part of a row.  One pass: the largest logit and the sum of weights relative to it, a pair in every lane; the best tokens, one in every lane,
+// in falling order.  R loads of 16 bytes a lane are looked at in a step.  Of the step's logits only those above the n-th best so far matter; where n lanes or more have such
+// ones, their maxima are sorted: the n-th largest of them bounds the step's n best from below, and leaves few.  Those few are gathered in LDS, sorted 64 at a time and merged.
+template <int DTYPE, int R>
+__global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) {
+    typedef Logits<DTYPE> X;
+    constexpr int PER = X::PER;
+    __shared__ uint64_t found_of[BEAM_WAVES][128];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint64_t* const found = found_of[wave];
+    const int unit = blockIdx.x * BEAM_WAVES + wave, row = unit / a.parts, part = unit - row * a.parts;
+    if (row >= a.rows) return;
+    if ((a.ended && a.ended[row] != 0) || !__builtin_isfinite(a.scores[row])) return;   // (nobody asks for its tokens)
+    const char* const base = static_cast<const char*>(a.logits) + (int64_t)row * a.stride * X::SIZE;
+    const int head = min((int)((16 - ((uintptr_t)base & 15)) & 15) / X::SIZE, a.vocab);   // logits before the first 16 bytes that are aligned
+    const int whole = (a.vocab - head) / PER, tail = a.vocab - head - whole * PER;
+    const u32x4* const body = reinterpret_cast<const u32x4*>(base + head * X::SIZE);
+    const int begin = min(part * a.part_len, whole), end = min(begin + a.part_len, whole);
+
+    uint64_t list = 0;
+    int found_n = 0;                                       // uniform
+    auto flush = [&]() {
+        lds_of_wave();
+        for (int i = 0; i < found_n; i += 64) list = merge_lanes(list, sort_lanes(i + lane < found_n ? found[i + lane] : 0, lane, shuffle_key), lane);
+        lds_of_wave();
+        found_n = 0;
+    };
+    float top = -INFINITY, sum = 0.0f;
+    auto weigh = [&](float to, float x) { return __builtin_amdgcn_exp2f((x - to) * LOG2E); };
+    auto raise = [&](float to) {
+        const float ref = to > -INFINITY ? to : 0.0f;
+        sum *= weigh(ref, top);
+        top = to;
+        return ref;
+    };
+#pragma unroll 1
+    for (int v0 = begin; v0 < end; v0 += 64 * R) {
+        u32x4 x[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            x[r] = u32x4{X::NONE, X::NONE, X::NONE, X::NONE};
+            const int v = v0 + r * 64 + lane;
+            if (v < end) x[r] = __builtin_nontemporal_load(body + v);
+        }
+        float most[R], largest = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            most[r] = X::at(x[r], 0);
+#pragma unroll
+            for (int k = 1; k < PER; ++k) most[r] = fmaxf(most[r], X::at(x[r], k));
+            largest = fmaxf(largest, most[r]);
+        }
+        const float ref = raise(fmaxf(top, largest));
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float w[PER];
+#pragma unroll
+            for (int k = 0; k < PER; ++k) w[k] = weigh(ref, X::at(x[r], k));
+#pragma unroll
+            for (int o = PER / 2; o > 0; o >>= 1)
+#pragma unroll
+                for (int k = 0; k < o; ++k) w[k] += w[k + o];
+            sum += w[0];
+        }
+        // The tokens that may be among the n best.  (Tokens of later steps are larger: of equal logits those that are there already come first.)
+        const uint64_t last = lane_key(list, a.n - 1);
+        float least = last ? key_logit(last) : -INFINITY;
+        const int lanes = __popcll(__ballot(largest > least));
+        if (lanes == 0) continue;
+        bool ties = false;
+        if (lanes >= a.n) {
+            const float sorted = sort_lanes(largest, lane, [](float v, int mask) { return __shfl_xor(v, mask); });
+            least = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sorted), a.n - 1));   // (above the old one: n lanes are)
+            ties = true;
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (!__any(most[r] > least)) continue;
+            const uint32_t token = head + (v0 + r * 64 + lane) * PER;
+#pragma unroll 1
+            for (int k = 0; k < PER; ++k) {
+                const float y = X::at(x[r], k);
+                const uint64_t who = __ballot(y > least);
+                if (!who) continue;
+                if (y > least) found[found_n + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = beam_key(y, token + k);
+                found_n += __popcll(who);
+                if (found_n > 64) flush();
             }
         }
-        value[i] = v;
-        token[i] = t;
-        if (j == 0) over[i / a.n] = ended;
+        if (ties) {                                        // as many as there may be places for, the first ones
+            int left = a.n;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (left <= 0 || !__any(most[r] >= least)) continue;
+                int at = 0, total = 0;
+#pragma unroll
+                for (int k = 0; k < PER; ++k) {
+                    const uint64_t who = __ballot(X::at(x[r], k) == least);
+                    at += __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+                    total += __popcll(who);
+                }
+                const uint32_t token = head + (v0 + r * 64 + lane) * PER;
+#pragma unroll
+                for (int k = 0; k < PER; ++k) {
+                    if (X::at(x[r], k) != least) continue;
+                    if (at < left) found[found_n + at] = beam_key(least, token + k);
+                    ++at;
+                }
+                found_n += min(total, left);
+                left -= total;
+                if (found_n > 64) flush();
+            }
+        }
+        if (found_n >= 32 || !last) flush();
+    }
+    if (part == 0 && head + tail > 0) {                    // what is not 16 aligned bytes: PER - 1 logits at either end at most
+        const int i = lane < head ? lane : lane >= 32 && lane - 32 < tail ? a.vocab - tail + lane - 32 : -1;
+        const float y = i >= 0 ? X::one(base, i) : -INFINITY;
+        const float ref = raise(fmaxf(top, y));
+        sum += weigh(ref, y);
+        const uint64_t who = __ballot(y > -INFINITY);
+        if (y > -INFINITY) found[found_n + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = beam_key(y, i);
+        found_n += __popcll(who);
+    }
+    if (found_n > 0) flush();
+    float all = top;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) all = fmaxf(all, __shfl_xor(all, o));
+    double total = (double)(sum * weigh(all > -INFINITY ? all : 0.0f, top));
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o);
+    if (lane < a.n) a.best[(int64_t)unit * a.n + lane] = list;
+    if (lane == 0) {
+        a.top[unit] = all;
+        a.sum[unit] = total;                               // (NaN with a NaN among the logits, or with +infinity)
+    }
+}
+
+// A workgroup for a group, a wave for each of its rows at a time: the parts' sums and lists together, the tokens' worth in 64 bits.  Then every candidate counts, row by row, who comes
+// before it.
+constexpr int MERGE_WAVES = 8;
+__global__ __launch_bounds__(64 * MERGE_WAVES) void beam_merge_kernel(BeamArgs a) {
+    __shared__ double value[BEAM_WIDTH][BEAM_MOST];
+    __shared__ int32_t token[BEAM_WIDTH][BEAM_MOST], over[BEAM_WIDTH], there[BEAM_WIDTH];
+    const int group = blockIdx.x, row0 = group * a.width, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int b = wave; b < a.width; b += MERGE_WAVES) {
+        const int row = row0 + b;
+        const float s = a.scores[row];
+        const bool ended = a.ended && a.ended[row] != 0, counts = __builtin_isfinite(s);
+        double v = -INFINITY;
+        int t = -1;
+        if (counts && ended) {
+            if (lane == 0) {
+                v = s;
+                t = a.end_token;
+            }
+        } else if (counts) {
+            const bool mine = lane < a.parts;
+            const int64_t unit = (int64_t)row * a.parts;
+            const float own = mine ? a.top[unit + lane] : -INFINITY;
+            float top = own;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+            double sum = mine && own > -INFINITY ? a.sum[unit + lane] * exp((double)own - (double)top) : 0.0;
+            if (mine && !(a.sum[unit + lane] >= 0.0)) sum = NAN;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+            const uint64_t* const keys = a.best + unit * a.n;
+            uint64_t list = 0;
+            for (int i = 0; i < a.parts * a.n; i += 64) {
+                const uint64_t k = i + lane < a.parts * a.n ? keys[i + lane] : 0;
+                if (__any(k > lane_key(list, a.n - 1))) list = merge_lanes(list, sort_lanes(k, lane, shuffle_key), lane);
+            }
+            if (top < INFINITY && sum > 0.0 && lane < a.n && list) {
+                v = (double)s + (((double)key_logit(list) - (double)top) - log(sum));
+                t = key_token(list);
+            }
+        }
+        if (lane < a.n) {
+            value[b][lane] = v;
+            token[b][lane] = t;
+        }
+        const int n = __popcll(__ballot(v > -INFINITY));
+        if (lane == 0) {
+            over[b] = ended;
+            there[b] = n;
+        }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < all; i += BEAM_THREADS) {
-        const double v = value[i];
-        if (!(v > -INFINITY)) continue;
-        int rank = 0;                                      // candidates that come before this one
-        for (int j = 0; j < all; ++j) rank += value[j] > v || (value[j] == v && j < i);   // (a row's own come in order: beside a large score 64 bits may not tell them apart)
+    for (int i = threadIdx.x; i < a.width * a.n; i += 64 * MERGE_WAVES) {
+        const int b = i / a.n, j = i - b * a.n;
+        const double v = value[b][j];
+        if (j >= there[b]) continue;
+        int rank = j;                                      // candidates that come before this one: of equal ones those of lower rows
+        for (int o = 0; o < a.width; ++o) {
+            if (o == b) continue;
+            int lo = 0, hi = there[o];                     // the first of row o that does not
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (value[o][mid] > v || (o < b && value[o][mid] == v)) lo = mid + 1;
+                else hi = mid;
+            }
+            rank += lo;
+        }
         if (rank >= a.n) continue;
         const int64_t to = (int64_t)group * a.n + rank;
         a.out_scores[to] = (float)v;
-        a.parents[to] = i / a.n;
-        a.tokens[to] = token[i];
-        if (a.out_ended) a.out_ended[to] = over[i / a.n] || token[i] == a.end_token;
+        a.parents[to] = b;
+        a.tokens[to] = token[b][j];
+        if (a.out_ended) a.out_ended[to] = over[b] || token[b][j] == a.end_token;
     }
-    int there = 0;
-    for (int j = 0; j < all; ++j) there += value[j] > -INFINITY;
-    for (int i = there + threadIdx.x; i < a.n; i += BEAM_THREADS) {
+    int all = 0;
+    for (int b = 0; b < a.width; ++b) all += there[b];
+    for (int i = all + threadIdx.x; i < a.n; i += 64 * MERGE_WAVES) {
         const int64_t to = (int64_t)group * a.n + i;
         a.out_scores[to] = -INFINITY;
         a.parents[to] = a.tokens[to] = -1;
