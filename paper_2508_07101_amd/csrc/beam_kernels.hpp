@@ -43,33 +43,75 @@ __device__ __forceinline__ float key_logit(uint64_t key) {
 }
 __device__ __forceinline__ uint32_t key_token(uint64_t key) { return 0xffffffffu - (uint32_t)key; }
 
-__device__ __forceinline__ uint64_t shuffle_key(uint64_t k, int mask) { return __shfl_xor((unsigned long long)k, mask); }
-// The wave's 64 values in falling order, over the lanes: a bitonic network.
-template <typename T, typename F>
-__device__ __forceinline__ T sort_lanes(T v, int lane, F other) {
+// The value of the lane whose number differs in bit `stride`, without LDS.
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v, int stride) {
+    const int x = (int)v;
+    switch (stride) {                                      // (a constant wherever it is called)
+        case 1: return __builtin_amdgcn_mov_dpp(x, 0xb1, 0xf, 0xf, true);              // within four lanes: 1 0 3 2
+        case 2: return __builtin_amdgcn_mov_dpp(x, 0x4e, 0xf, 0xf, true);              // 2 3 0 1
+        case 4: return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true), 0x1b, 0xf, 0xf, true);   // eight lanes turned, then four
+        case 8: return __builtin_amdgcn_mov_dpp(x, 0x128, 0xf, 0xf, true);             // sixteen lanes rotated by eight
+        case 16: {
+            const auto w = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+            return (threadIdx.x & 16) ? w[0] : w[1];
+        }
+        default: {
+            const auto w = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+            return (threadIdx.x & 32) ? w[0] : w[1];
+        }
+    }
+}
+__device__ __forceinline__ uint64_t lane_xor(uint64_t v, int stride) {
+    return (uint64_t)lane_xor((uint32_t)(v >> 32), stride) << 32 | lane_xor((uint32_t)v, stride);
+}
+__device__ __forceinline__ float lane_xor(float v, int stride) { return __uint_as_float(lane_xor(__float_as_uint(v), stride)); }
+__device__ __forceinline__ double lane_xor(double v, int stride) { return __builtin_bit_cast(double, lane_xor(__builtin_bit_cast(uint64_t, v), stride)); }
+
+// Lanes with a bit in a number of lanes, as a mask.
+constexpr uint64_t lanes_with(int bit) {
+    uint64_t m = 0;
+    for (int i = 0; i < 64; ++i)
+        if (i & bit) m |= 1ull << i;
+    return m;
+}
+// Keeps the larger value in the lanes of `larger`, the smaller in the others.
+template <typename T>
+__device__ __forceinline__ T exchange(T v, int stride, uint64_t larger) {
+    const T o = lane_xor(v, stride);
+    return (o > v) == (bool)__builtin_amdgcn_inverse_ballot_w64(larger) ? o : v;
+}
+// The wave's 64 values in order over the lanes, by a bitonic network.
+template <bool FALLING, typename T>
+__device__ __forceinline__ T sort_lanes(T v) {
 #pragma unroll
     for (int size = 2; size <= 64; size <<= 1)
 #pragma unroll
-        for (int stride = size >> 1; stride > 0; stride >>= 1) {
-            const T o = other(v, stride);
-            v = (((lane & stride) == 0) == ((lane & size) == 0)) ? (v > o ? v : o) : (v > o ? o : v);
-        }
+        for (int stride = size >> 1; stride > 0; stride >>= 1)
+            v = exchange(v, stride, (lanes_with(stride) ^ (size < 64 ? lanes_with(size) : 0)) ^ (FALLING ? ~0ull : 0));
     return v;
 }
-// The 64 largest of two such lists, in falling order.
-__device__ __forceinline__ uint64_t merge_lanes(uint64_t list, uint64_t batch, int lane) {
-    const uint64_t turned = shuffle_key(batch, 63);
-    uint64_t v = list > turned ? list : turned;
+// The 64 largest of a falling and a rising list, in falling order.
+__device__ __forceinline__ uint64_t merge_lanes(uint64_t list, uint64_t rising) {
+    uint64_t v = list > rising ? list : rising;
 #pragma unroll
-    for (int stride = 32; stride > 0; stride >>= 1) {
-        const uint64_t o = shuffle_key(v, stride);
-        v = (lane & stride) == 0 ? (v > o ? v : o) : (v > o ? o : v);
-    }
+    for (int stride = 32; stride > 0; stride >>= 1) v = exchange(v, stride, ~lanes_with(stride));
+    return v;
+}
+template <typename T, typename F>
+__device__ __forceinline__ T over_lanes(T v, F f) {
+#pragma unroll
+    for (int stride = 1; stride < 64; stride <<= 1) v = f(v, lane_xor(v, stride));
     return v;
 }
 __device__ __forceinline__ uint64_t lane_key(uint64_t k, int lane) {
     return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, lane);
 }
+// The smallest number above x (x below +infinity).
+__device__ __forceinline__ float above(float x) {
+    const int32_t u = __float_as_int(x + 0.0f);
+    return __int_as_float(u >= 0 ? u + 1 : u - 1);
+}
+__device__ __forceinline__ int lanes_before(uint64_t who) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0)); }
 
 template <int DTYPE>                       // cusa_dtype
 struct Logits {
@@ -99,11 +141,13 @@ __device__ __forceinline__ void lds_of_wave() {            // what the wave's ot
 // A wave for a part of a row.  One pass: the largest logit and the sum of weights relative to it, a pair in every lane; the best tokens, one in every lane,
 // in falling order.  R loads of 16 bytes a lane are looked at in a step.  Of the step's logits only those above the n-th best so far matter; where n lanes or more have such
 // ones, their maxima are sorted: the n-th largest of them bounds the step's n best from below, and leaves few.  Those few are gathered in LDS, sorted 64 at a time and merged.
+// A weight is 2^((x - top) log2 e): the difference first, so that rows that differ by a constant have the same sums, whatever the constant.
+constexpr int FOUND = 128;
 template <int DTYPE, int R>
 __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) {
     typedef Logits<DTYPE> X;
     constexpr int PER = X::PER;
-    __shared__ uint64_t found_of[BEAM_WAVES][128];
+    __shared__ uint64_t found_of[BEAM_WAVES][FOUND];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint64_t* const found = found_of[wave];
     const int unit = blockIdx.x * BEAM_WAVES + wave, row = unit / a.parts, part = unit - row * a.parts;
@@ -114,31 +158,40 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
     const int whole = (a.vocab - head) / PER, tail = a.vocab - head - whole * PER;
     const u32x4* const body = reinterpret_cast<const u32x4*>(base + head * X::SIZE);
     const int begin = min(part * a.part_len, whole), end = min(begin + a.part_len, whole);
+    const u32x4 none = {X::NONE, X::NONE, X::NONE, X::NONE};
 
     uint64_t list = 0;
     int found_n = 0;                                       // uniform
     auto flush = [&]() {
         lds_of_wave();
-        for (int i = 0; i < found_n; i += 64) list = merge_lanes(list, sort_lanes(i + lane < found_n ? found[i + lane] : 0, lane, shuffle_key), lane);
+        for (int i = 0; i < found_n; i += 64) list = merge_lanes(list, sort_lanes<false>(i + lane < found_n ? found[i + lane] : (uint64_t)0));
         lds_of_wave();
         found_n = 0;
     };
+    auto add = [&](bool hit, uint64_t who, float y, uint32_t token) {
+        const int at = found_n + lanes_before(who);
+        if (hit && at < FOUND) found[at] = beam_key(y, token);
+        found_n += __popcll(who);
+    };
     float top = -INFINITY, sum = 0.0f;
-    auto weigh = [&](float to, float x) { return __builtin_amdgcn_exp2f((x - to) * LOG2E); };
-    auto raise = [&](float to) {
-        const float ref = to > -INFINITY ? to : 0.0f;
-        sum *= weigh(ref, top);
+    auto weight = [&](float x) { return __builtin_amdgcn_exp2f((x - top) * LOG2E); };
+    auto raise = [&](float to) {                           // weights are relative to `to` from now on
+        if (top > -INFINITY) sum *= __builtin_amdgcn_exp2f((top - to) * LOG2E);   // (before the first logit the sum is 0, or NaN)
         top = to;
-        return ref;
     };
 #pragma unroll 1
     for (int v0 = begin; v0 < end; v0 += 64 * R) {
         u32x4 x[R];
+        if (v0 + 64 * R <= end) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            x[r] = u32x4{X::NONE, X::NONE, X::NONE, X::NONE};
-            const int v = v0 + r * 64 + lane;
-            if (v < end) x[r] = __builtin_nontemporal_load(body + v);
+            for (int r = 0; r < R; ++r) x[r] = __builtin_nontemporal_load(body + v0 + r * 64 + lane);
+        } else {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int v = v0 + r * 64 + lane;
+                x[r] = __builtin_nontemporal_load(body + min(v, end - 1));
+                if (v >= end) x[r] = none;
+            }
         }
         float most[R], largest = -INFINITY;
 #pragma unroll
@@ -148,65 +201,81 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
             for (int k = 1; k < PER; ++k) most[r] = fmaxf(most[r], X::at(x[r], k));
             largest = fmaxf(largest, most[r]);
         }
-        const float ref = raise(fmaxf(top, largest));
+        raise(fmaxf(top, largest));
+        if (top > -INFINITY) {                                // (else nothing but -infinity, or NaN)
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float w[PER];
+            for (int r = 0; r < R; ++r) {
+                float w[PER];
 #pragma unroll
-            for (int k = 0; k < PER; ++k) w[k] = weigh(ref, X::at(x[r], k));
+                for (int k = 0; k < PER; ++k) w[k] = weight(X::at(x[r], k));
 #pragma unroll
-            for (int o = PER / 2; o > 0; o >>= 1)
+                for (int o = PER / 2; o > 0; o >>= 1)
 #pragma unroll
-                for (int k = 0; k < o; ++k) w[k] += w[k + o];
-            sum += w[0];
+                    for (int k = 0; k < o; ++k) w[k] += w[k + o];
+                sum += w[0];
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int k = 0; k < PER; ++k) sum += X::at(x[r], k) == -INFINITY ? 0.0f : NAN;
         }
         // The tokens that may be among the n best.  (Tokens of later steps are larger: of equal logits those that are there already come first.)
         const uint64_t last = lane_key(list, a.n - 1);
-        float least = last ? key_logit(last) : -INFINITY;
-        const int lanes = __popcll(__ballot(largest > least));
+        float least = above(last ? key_logit(last) : -INFINITY);
+        const int lanes = __popcll(__ballot(largest >= least));
         if (lanes == 0) continue;
-        bool ties = false;
-        if (lanes >= a.n) {
-            const float sorted = sort_lanes(largest, lane, [](float v, int mask) { return __shfl_xor(v, mask); });
-            least = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sorted), a.n - 1));   // (above the old one: n lanes are)
-            ties = true;
-        }
+        const bool bound = lanes >= a.n;
+        if (bound) least = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sort_lanes<true>(largest)), a.n - 1));   // (not below the old one: n lanes are)
+        const int before = found_n;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            if (!__any(most[r] > least)) continue;
+            if (!__any(most[r] >= least)) continue;
             const uint32_t token = head + (v0 + r * 64 + lane) * PER;
-#pragma unroll 1
+#pragma unroll
             for (int k = 0; k < PER; ++k) {
                 const float y = X::at(x[r], k);
-                const uint64_t who = __ballot(y > least);
-                if (!who) continue;
-                if (y > least) found[found_n + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = beam_key(y, token + k);
-                found_n += __popcll(who);
-                if (found_n > 64) flush();
+                const bool hit = y >= least;
+                if (const uint64_t who = __ballot(hit)) add(hit, who, y, token + k);
             }
         }
-        if (ties) {                                        // as many as there may be places for, the first ones
-            int left = a.n;
-#pragma unroll
+        if (found_n > FOUND) {                             // more than there is room for: those above the bound 64 at a time, and of those that are equal to it the first n
+            found_n = before;
+            if (found_n > 0) flush();
+#pragma unroll 1
             for (int r = 0; r < R; ++r) {
-                if (left <= 0 || !__any(most[r] >= least)) continue;
+                const int v = v0 + r * 64 + lane;
+                const u32x4 z = v < end ? body[v] : none;
+#pragma unroll 1
+                for (int k = 0; k < PER; ++k) {
+                    const float y = X::at(z, k);
+                    const uint64_t now = lane_key(list, a.n - 1);
+                    const bool hit = (bound ? y > least : y >= least) && (!now || y >= key_logit(now));
+                    if (const uint64_t who = __ballot(hit)) add(hit, who, y, head + v * PER + k);
+                    if (found_n > FOUND - 64) flush();
+                }
+            }
+            if (found_n > 0) flush();
+            int left = bound ? a.n : 0;
+#pragma unroll 1
+            for (int r = 0; r < R && left > 0; ++r) {
+                const int v = v0 + r * 64 + lane;
+                const u32x4 z = v < end ? body[v] : none;
                 int at = 0, total = 0;
 #pragma unroll
                 for (int k = 0; k < PER; ++k) {
-                    const uint64_t who = __ballot(X::at(x[r], k) == least);
-                    at += __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+                    const uint64_t who = __ballot(X::at(z, k) == least);
+                    at += lanes_before(who);
                     total += __popcll(who);
                 }
-                const uint32_t token = head + (v0 + r * 64 + lane) * PER;
 #pragma unroll
                 for (int k = 0; k < PER; ++k) {
-                    if (X::at(x[r], k) != least) continue;
-                    if (at < left) found[found_n + at] = beam_key(least, token + k);
+                    if (X::at(z, k) != least) continue;
+                    if (at < left) found[found_n + at] = beam_key(least, head + v * PER + k);
                     ++at;
                 }
                 found_n += min(total, left);
                 left -= total;
-                if (found_n > 64) flush();
             }
         }
         if (found_n >= 32 || !last) flush();
@@ -214,23 +283,19 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
     if (part == 0 && head + tail > 0) {                    // what is not 16 aligned bytes: PER - 1 logits at either end at most
         const int i = lane < head ? lane : lane >= 32 && lane - 32 < tail ? a.vocab - tail + lane - 32 : -1;
         const float y = i >= 0 ? X::one(base, i) : -INFINITY;
-        const float ref = raise(fmaxf(top, y));
-        sum += weigh(ref, y);
-        const uint64_t who = __ballot(y > -INFINITY);
-        if (y > -INFINITY) found[found_n + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = beam_key(y, i);
-        found_n += __popcll(who);
+        raise(fmaxf(top, y));
+        if (top > -INFINITY) sum += weight(y);
+        else if (y != y) sum = y;
+        const bool hit = y > -INFINITY;
+        add(hit, __ballot(hit), y, i);
     }
     if (found_n > 0) flush();
-    float all = top;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) all = fmaxf(all, __shfl_xor(all, o));
-    double total = (double)(sum * weigh(all > -INFINITY ? all : 0.0f, top));
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o);
+    const float all = over_lanes(top, [](float x, float y) { return fmaxf(x, y); });
+    const double total = over_lanes((double)(top == all || top == -INFINITY ? sum : sum * __builtin_amdgcn_exp2f((top - all) * LOG2E)), [](double x, double y) { return x + y; });
     if (lane < a.n) a.best[(int64_t)unit * a.n + lane] = list;
     if (lane == 0) {
         a.top[unit] = all;
-        a.sum[unit] = total;                               // (NaN with a NaN among the logits, or with +infinity)
+        a.sum[unit] = total;                               // (NaN with a NaN among the logits)
     }
 }
 
@@ -256,18 +321,15 @@ __global__ __launch_bounds__(64 * MERGE_WAVES) void beam_merge_kernel(BeamArgs a
             const bool mine = lane < a.parts;
             const int64_t unit = (int64_t)row * a.parts;
             const float own = mine ? a.top[unit + lane] : -INFINITY;
-            float top = own;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+            const float top = over_lanes(own, [](float x, float y) { return fmaxf(x, y); });
             double sum = mine && own > -INFINITY ? a.sum[unit + lane] * exp((double)own - (double)top) : 0.0;
             if (mine && !(a.sum[unit + lane] >= 0.0)) sum = NAN;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+            sum = over_lanes(sum, [](double x, double y) { return x + y; });
             const uint64_t* const keys = a.best + unit * a.n;
             uint64_t list = 0;
             for (int i = 0; i < a.parts * a.n; i += 64) {
                 const uint64_t k = i + lane < a.parts * a.n ? keys[i + lane] : 0;
-                if (__any(k > lane_key(list, a.n - 1))) list = merge_lanes(list, sort_lanes(k, lane, shuffle_key), lane);
+                if (__any(k > lane_key(list, a.n - 1))) list = merge_lanes(list, sort_lanes<false>(k));
             }
             if (top < INFINITY && sum > 0.0 && lane < a.n && list) {
                 v = (double)s + (((double)key_logit(list) - (double)top) - log(sum));
