@@ -138,18 +138,40 @@ __device__ __forceinline__ void lds_of_wave() {            // what the wave's ot
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// The best 64 of a wave's keys, one in every lane, in falling order; keys are gathered in LDS until they are enough for a sort.
+constexpr int FOUND = 128;
+struct Best {
+    uint64_t* found;
+    uint64_t list = 0;
+    int n = 0;                                             // gathered: uniform
+    __device__ __forceinline__ explicit Best(uint64_t* lds) : found(lds) {}
+    __device__ __forceinline__ void flush() {
+        const int lane = threadIdx.x & 63;
+        lds_of_wave();
+        for (int i = 0; i < n; i += 64) list = merge_lanes(list, sort_lanes<false>(i + lane < n ? found[i + lane] : (uint64_t)0));
+        lds_of_wave();
+        n = 0;
+    }
+    // The keys of the lanes in `who`; those that there is no room for are counted all the same.
+    __device__ __forceinline__ void add(bool hit, uint64_t who, uint64_t key) {
+        const int at = n + lanes_before(who);
+        if (hit && at < FOUND) found[at] = key;
+        n += __popcll(who);
+    }
+};
+
 // A wave for a part of a row.  One pass: the largest logit and the sum of weights relative to it, a pair in every lane; the best tokens, one in every lane,
 // in falling order.  R loads of 16 bytes a lane are looked at in a step.  Of the step's logits only those above the n-th best so far matter; where n lanes or more have such
 // ones, their maxima are sorted: the n-th largest of them bounds the step's n best from below, and leaves few.  Those few are gathered in LDS, sorted 64 at a time and merged.
-// A weight is 2^((x - top) log2 e): the difference first, so that rows that differ by a constant have the same sums, whatever the constant.
-constexpr int FOUND = 128;
+// A weight is 2^((x - ref) log2 e): the difference first, so that rows that differ by a constant have the same sums, whatever the constant.  A lane's ref is a logit of its own
+// that follows the largest when that is 60 above it (2^87: the sum stays in range).
 template <int DTYPE, int R>
 __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) {
     typedef Logits<DTYPE> X;
     constexpr int PER = X::PER;
     __shared__ uint64_t found_of[BEAM_WAVES][FOUND];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    uint64_t* const found = found_of[wave];
+    Best best(found_of[wave]);
     const int unit = blockIdx.x * BEAM_WAVES + wave, row = unit / a.parts, part = unit - row * a.parts;
     if (row >= a.rows) return;
     if ((a.ended && a.ended[row] != 0) || !__builtin_isfinite(a.scores[row])) return;   // (nobody asks for its tokens)
@@ -158,27 +180,19 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
     const int whole = (a.vocab - head) / PER, tail = a.vocab - head - whole * PER;
     const u32x4* const body = reinterpret_cast<const u32x4*>(base + head * X::SIZE);
     const int begin = min(part * a.part_len, whole), end = min(begin + a.part_len, whole);
+    constexpr int HALF = R < 4 ? R : 4;
     const u32x4 none = {X::NONE, X::NONE, X::NONE, X::NONE};
 
-    uint64_t list = 0;
-    int found_n = 0;                                       // uniform
-    auto flush = [&]() {
-        lds_of_wave();
-        for (int i = 0; i < found_n; i += 64) list = merge_lanes(list, sort_lanes<false>(i + lane < found_n ? found[i + lane] : (uint64_t)0));
-        lds_of_wave();
-        found_n = 0;
+    float ref = -INFINITY, top = -INFINITY, sum = 0.0f;
+    auto follow = [&](float largest) {
+        top = fmaxf(top, largest);
+        if (__any(largest > ref + 60.0f)) {                // (the first logit above -infinity is)
+            const float to = largest > ref + 60.0f ? largest : ref;
+            if (ref > -INFINITY) sum *= __builtin_amdgcn_exp2f((ref - to) * LOG2E);   // (before that, the sum is 0, or NaN)
+            ref = to;
+        }
     };
-    auto add = [&](bool hit, uint64_t who, float y, uint32_t token) {
-        const int at = found_n + lanes_before(who);
-        if (hit && at < FOUND) found[at] = beam_key(y, token);
-        found_n += __popcll(who);
-    };
-    float top = -INFINITY, sum = 0.0f;
-    auto weight = [&](float x) { return __builtin_amdgcn_exp2f((x - top) * LOG2E); };
-    auto raise = [&](float to) {                           // weights are relative to `to` from now on
-        if (top > -INFINITY) sum *= __builtin_amdgcn_exp2f((top - to) * LOG2E);   // (before the first logit the sum is 0, or NaN)
-        top = to;
-    };
+    auto weight = [&](float x) { return __builtin_amdgcn_exp2f((x - (ref > -INFINITY ? ref : 0.0f)) * LOG2E); };
 #pragma unroll 1
     for (int v0 = begin; v0 < end; v0 += 64 * R) {
         u32x4 x[R];
@@ -195,16 +209,19 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
         }
         float most[R], largest = -INFINITY;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            most[r] = X::at(x[r], 0);
+        for (int r0 = 0; r0 < R; r0 += HALF) {                // (as many at a time as there are registers for)
+            float some = -INFINITY;
 #pragma unroll
-            for (int k = 1; k < PER; ++k) most[r] = fmaxf(most[r], X::at(x[r], k));
-            largest = fmaxf(largest, most[r]);
-        }
-        raise(fmaxf(top, largest));
-        if (top > -INFINITY) {                                // (else nothing but -infinity, or NaN)
+            for (int r = r0; r < r0 + HALF; ++r) {
+                most[r] = X::at(x[r], 0);
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
+                for (int k = 1; k < PER; ++k) most[r] = fmaxf(most[r], X::at(x[r], k));
+                some = fmaxf(some, most[r]);
+            }
+            largest = fmaxf(largest, some);
+            follow(some);
+#pragma unroll
+            for (int r = r0; r < r0 + HALF; ++r) {
                 float w[PER];
 #pragma unroll
                 for (int k = 0; k < PER; ++k) w[k] = weight(X::at(x[r], k));
@@ -214,20 +231,17 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
                     for (int k = 0; k < o; ++k) w[k] += w[k + o];
                 sum += w[0];
             }
-        } else {
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int k = 0; k < PER; ++k) sum += X::at(x[r], k) == -INFINITY ? 0.0f : NAN;
+            for (int r = r0; r < r0 + HALF; ++r) asm volatile("" : "+v"(x[r]));   // (what is taken apart is not kept for the search below, which mostly looks at none of it)
         }
         // The tokens that may be among the n best.  (Tokens of later steps are larger: of equal logits those that are there already come first.)
-        const uint64_t last = lane_key(list, a.n - 1);
+        const uint64_t last = lane_key(best.list, a.n - 1);
         float least = above(last ? key_logit(last) : -INFINITY);
         const int lanes = __popcll(__ballot(largest >= least));
         if (lanes == 0) continue;
         const bool bound = lanes >= a.n;
         if (bound) least = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sort_lanes<true>(largest)), a.n - 1));   // (not below the old one: n lanes are)
-        const int before = found_n;
+        const int before = best.n;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (!__any(most[r] >= least)) continue;
@@ -236,12 +250,12 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
             for (int k = 0; k < PER; ++k) {
                 const float y = X::at(x[r], k);
                 const bool hit = y >= least;
-                if (const uint64_t who = __ballot(hit)) add(hit, who, y, token + k);
+                if (const uint64_t who = __ballot(hit)) best.add(hit, who, beam_key(y, token + k));
             }
         }
-        if (found_n > FOUND) {                             // more than there is room for: those above the bound 64 at a time, and of those that are equal to it the first n
-            found_n = before;
-            if (found_n > 0) flush();
+        if (best.n > FOUND) {                             // more than there is room for: those above the bound 64 at a time, and of those that are equal to it the first n
+            best.n = before;
+            if (best.n > 0) best.flush();
 #pragma unroll 1
             for (int r = 0; r < R; ++r) {
                 const int v = v0 + r * 64 + lane;
@@ -249,13 +263,13 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
 #pragma unroll 1
                 for (int k = 0; k < PER; ++k) {
                     const float y = X::at(z, k);
-                    const uint64_t now = lane_key(list, a.n - 1);
+                    const uint64_t now = lane_key(best.list, a.n - 1);
                     const bool hit = (bound ? y > least : y >= least) && (!now || y >= key_logit(now));
-                    if (const uint64_t who = __ballot(hit)) add(hit, who, y, head + v * PER + k);
-                    if (found_n > FOUND - 64) flush();
+                    if (const uint64_t who = __ballot(hit)) best.add(hit, who, beam_key(y, head + v * PER + k));
+                    if (best.n > FOUND - 64) best.flush();
                 }
             }
-            if (found_n > 0) flush();
+            if (best.n > 0) best.flush();
             int left = bound ? a.n : 0;
 #pragma unroll 1
             for (int r = 0; r < R && left > 0; ++r) {
@@ -271,41 +285,41 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
 #pragma unroll
                 for (int k = 0; k < PER; ++k) {
                     if (X::at(z, k) != least) continue;
-                    if (at < left) found[found_n + at] = beam_key(least, head + v * PER + k);
+                    if (at < left) best.found[best.n + at] = beam_key(least, head + v * PER + k);
                     ++at;
                 }
-                found_n += min(total, left);
+                best.n += min(total, left);
                 left -= total;
             }
         }
-        if (found_n >= 32 || !last) flush();
+        if (best.n >= 32 || !last) best.flush();
     }
     if (part == 0 && head + tail > 0) {                    // what is not 16 aligned bytes: PER - 1 logits at either end at most
         const int i = lane < head ? lane : lane >= 32 && lane - 32 < tail ? a.vocab - tail + lane - 32 : -1;
         const float y = i >= 0 ? X::one(base, i) : -INFINITY;
-        raise(fmaxf(top, y));
-        if (top > -INFINITY) sum += weight(y);
-        else if (y != y) sum = y;
+        follow(y);
+        sum += weight(y);
         const bool hit = y > -INFINITY;
-        add(hit, __ballot(hit), y, i);
+        best.add(hit, __ballot(hit), beam_key(y, i));
     }
-    if (found_n > 0) flush();
+    if (best.n > 0) best.flush();
     const float all = over_lanes(top, [](float x, float y) { return fmaxf(x, y); });
-    const double total = over_lanes((double)(top == all || top == -INFINITY ? sum : sum * __builtin_amdgcn_exp2f((top - all) * LOG2E)), [](double x, double y) { return x + y; });
-    if (lane < a.n) a.best[(int64_t)unit * a.n + lane] = list;
+    const double total = over_lanes((double)(ref == all || ref == -INFINITY ? sum : sum * __builtin_amdgcn_exp2f((ref - all) * LOG2E)), [](double x, double y) { return x + y; });
+    if (lane < a.n) a.best[(int64_t)unit * a.n + lane] = best.list;
     if (lane == 0) {
         a.top[unit] = all;
         a.sum[unit] = total;                               // (NaN with a NaN among the logits)
     }
 }
 
-// A workgroup for a group, a wave for each of its rows at a time: the parts' sums and lists together, the tokens' worth in 64 bits.  Then every candidate counts, row by row, who comes
-// before it.
+// A workgroup for a group, a wave for each of its rows at a time: the parts' sums and lists together, the tokens' worth in 64 bits.  Where there are n parts or more, the n-th
+// largest of their best bounds the row's n best from below, and few of the lists' keys are left.  Then every candidate counts who comes before it.
 constexpr int MERGE_WAVES = 8;
 __global__ __launch_bounds__(64 * MERGE_WAVES) void beam_merge_kernel(BeamArgs a) {
-    __shared__ double value[BEAM_WIDTH][BEAM_MOST];
-    __shared__ int32_t token[BEAM_WIDTH][BEAM_MOST], over[BEAM_WIDTH], there[BEAM_WIDTH];
-    const int group = blockIdx.x, row0 = group * a.width, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ uint64_t found_of[MERGE_WAVES][FOUND];
+    __shared__ double value[BEAM_WIDTH * BEAM_MOST];
+    __shared__ int32_t token[BEAM_WIDTH * BEAM_MOST], over[BEAM_WIDTH], there[BEAM_WIDTH];
+    const int group = blockIdx.x, row0 = group * a.width, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (int b = wave; b < a.width; b += MERGE_WAVES) {
         const int row = row0 + b;
         const float s = a.scores[row];
@@ -320,25 +334,45 @@ __global__ __launch_bounds__(64 * MERGE_WAVES) void beam_merge_kernel(BeamArgs a
         } else if (counts) {
             const bool mine = lane < a.parts;
             const int64_t unit = (int64_t)row * a.parts;
-            const float own = mine ? a.top[unit + lane] : -INFINITY;
-            const float top = over_lanes(own, [](float x, float y) { return fmaxf(x, y); });
-            double sum = mine && own > -INFINITY ? a.sum[unit + lane] * exp((double)own - (double)top) : 0.0;
-            if (mine && !(a.sum[unit + lane] >= 0.0)) sum = NAN;
-            sum = over_lanes(sum, [](double x, double y) { return x + y; });
             const uint64_t* const keys = a.best + unit * a.n;
-            uint64_t list = 0;
-            for (int i = 0; i < a.parts * a.n; i += 64) {
-                const uint64_t k = i + lane < a.parts * a.n ? keys[i + lane] : 0;
-                if (__any(k > lane_key(list, a.n - 1))) list = merge_lanes(list, sort_lanes<false>(k));
+            const int all = a.parts * a.n;
+            constexpr int RUN = 4;                         // loads under way at once
+            uint64_t k[RUN];
+            auto request = [&](int i0) {
+#pragma unroll
+                for (int j = 0; j < RUN; ++j) k[j] = i0 + j * 64 + lane < all ? keys[i0 + j * 64 + lane] : 0;
+            };
+            const float own = mine ? a.top[unit + lane] : -INFINITY;
+            double sum = mine ? a.sum[unit + lane] : 0.0;
+            const uint64_t first = mine && all > 64 ? keys[(int64_t)lane * a.n] : 0;
+            request(0);
+            const float top = over_lanes(own, [](float x, float y) { return fmaxf(x, y); });
+            if (own != top) sum *= (double)__builtin_amdgcn_exp2f((own - top) * LOG2E);   // (a part without logits above -infinity: 0, or NaN)
+            sum = over_lanes(sum, [](double x, double y) { return x + y; });
+            Best best(found_of[wave]);
+            if (all <= 64) {                               // (a row of one part: in order already)
+                best.list = a.parts == 1 ? k[0] : sort_lanes<true>(k[0]);
+            } else {
+                const uint64_t least = a.parts >= a.n ? lane_key(sort_lanes<true>(first), a.n - 1) : 0;
+                for (int i0 = 0; i0 < all; i0 += 64 * RUN) {
+#pragma unroll
+                    for (int j = 0; j < RUN; ++j) {
+                        const bool hit = k[j] != 0 && k[j] >= least;
+                        if (const uint64_t who = __ballot(hit)) best.add(hit, who, k[j]);
+                        if (best.n > FOUND - 64) best.flush();
+                    }
+                    request(i0 + 64 * RUN);
+                }
+                if (best.n > 0) best.flush();
             }
-            if (top < INFINITY && sum > 0.0 && lane < a.n && list) {
-                v = (double)s + (((double)key_logit(list) - (double)top) - log(sum));
-                t = key_token(list);
+            if (top < INFINITY && sum > 0.0 && lane < a.n && best.list) {
+                v = (double)s + (((double)key_logit(best.list) - (double)top) - log(sum));
+                t = key_token(best.list);
             }
         }
         if (lane < a.n) {
-            value[b][lane] = v;
-            token[b][lane] = t;
+            value[b * a.n + lane] = v;
+            token[b * a.n + lane] = t;
         }
         const int n = __popcll(__ballot(v > -INFINITY));
         if (lane == 0) {
@@ -347,27 +381,36 @@ __global__ __launch_bounds__(64 * MERGE_WAVES) void beam_merge_kernel(BeamArgs a
         }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < a.width * a.n; i += 64 * MERGE_WAVES) {
+    const int candidates = a.width * a.n;
+    for (int i = threadIdx.x; i < candidates; i += 64 * MERGE_WAVES) {
         const int b = i / a.n, j = i - b * a.n;
-        const double v = value[b][j];
+        const double v = value[i];
         if (j >= there[b]) continue;
-        int rank = j;                                      // candidates that come before this one: of equal ones those of lower rows
-        for (int o = 0; o < a.width; ++o) {
-            if (o == b) continue;
-            int lo = 0, hi = there[o];                     // the first of row o that does not
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (value[o][mid] > v || (o < b && value[o][mid] == v)) lo = mid + 1;
-                else hi = mid;
+        int rank;                                          // candidates that come before this one: of equal ones those of lower rows
+        if (candidates <= 256) {
+            rank = 0;
+#pragma unroll 8
+            for (int o = 0; o < candidates; ++o) rank += value[o] > v || (value[o] == v && o < i);
+        } else {                                           // row by row, in as many looks as n has bits
+            rank = j;
+            for (int o = 0; o < a.width; ++o) {
+                if (o == b) continue;
+                int lo = 0, hi = there[o];                 // the first of row o that does not
+                while (lo < hi) {
+                    const int mid = (lo + hi) >> 1;
+                    const double w = value[o * a.n + mid];
+                    if (w > v || (o < b && w == v)) lo = mid + 1;
+                    else hi = mid;
+                }
+                rank += lo;
             }
-            rank += lo;
         }
         if (rank >= a.n) continue;
         const int64_t to = (int64_t)group * a.n + rank;
         a.out_scores[to] = (float)v;
         a.parents[to] = b;
-        a.tokens[to] = token[b][j];
-        if (a.out_ended) a.out_ended[to] = over[b] || token[b][j] == a.end_token;
+        a.tokens[to] = token[i];
+        if (a.out_ended) a.out_ended[to] = over[b] || token[i] == a.end_token;
     }
     int all = 0;
     for (int b = 0; b < a.width; ++b) all += there[b];
