@@ -54,6 +54,8 @@ cusa_status check_beams(int32_t rows, int32_t vocab, int32_t n) {
     return rows > MAX_BATCH || n > BEAM_MOST ? CUSA_ERR_UNSUPPORTED : CUSA_OK;
 }
 
+constexpr int64_t FORK_ALL = 16384;        // entries of a table that one workgroup changes
+
 int fork_chunks(int32_t max_pages) { return (int)(((int64_t)max_pages + FORK_COLS - 1) / FORK_COLS); }
 
 struct ForkWs {
@@ -174,7 +176,11 @@ cusa_status cusa_kv_fork(const cusa_pool* pool, int32_t width, const int32_t* he
     a.grow = grow != 0;
     a.chunks = fork_chunks(pool->max_pages);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    launch(KID_KV_FORK, kv_fork_kernel, 1, PLAN_THREADS, 0, s, a);
+    if (width <= FORK_ALL_WIDTH && a.batch <= PLAN_THREADS && (int64_t)a.batch * a.max_pages <= FORK_ALL) {
+        launch(KID_KV_FORK, kv_fork_kernel<true>, 1, PLAN_THREADS, 0, s, a);
+        return launch_status();
+    }
+    launch(KID_KV_FORK, kv_fork_kernel<false>, 1, PLAN_THREADS, 0, s, a);
     if (launch_status() != CUSA_OK) return CUSA_ERR_LAUNCH;
     launch(KID_FORK_TABLES, fork_tables_kernel, dim3((unsigned)a.chunks, (unsigned)(a.batch / width)), FORK_COLS, 0, s, a);
     if (launch_status() != CUSA_OK) return CUSA_ERR_LAUNCH;

@@ -446,14 +446,50 @@ struct ForkArgs {
 };
 constexpr int FORK_COLS = 256;
 
-// A thread for each row, as many whole groups at a time as 1024 hold.
+// A column of a group: what the rows hold there goes from `table` to `table_out`, all of it read before any is written, so that the tables may be changed in place.  Returns the
+// rows whose entry names a page that nobody holds any more (of several, the first).  entry: a column in LDS, STRIDE entries from row to row.
+template <int STRIDE>
+__device__ __forceinline__ uint32_t fork_column(const ForkArgs& a, const ForkRow* rows, int row0, int col, int32_t* entry) {
+    const int32_t* const from = a.table + (int64_t)row0 * a.max_pages + col;
+    int32_t* const to = a.table_out + (int64_t)row0 * a.max_pages + col;
+    uint32_t alive = 0;                                    // rows that somebody descends from
+#pragma unroll 4
+    for (int b = 0; b < a.width; ++b) {
+        entry[b * STRIDE] = col < rows[b].old ? from[(int64_t)b * a.max_pages] : -1;
+        if (rows[b].src >= 0) alive |= 1u << rows[b].src;
+    }
+    for (int b = 0; b < a.width; ++b) {
+        const ForkRow& r = rows[b];
+        if (col == r.col) to[(int64_t)b * a.max_pages] = r.page;
+        else if (r.src >= 0 && col < r.had) to[(int64_t)b * a.max_pages] = entry[r.src * STRIDE];
+    }
+    uint32_t gone = 0;
+    for (uint32_t ends = ~alive & (a.width < 32 ? (1u << a.width) - 1 : 0xffffffffu); ends; ends &= ends - 1) {
+        const int b = __builtin_ctz(ends);
+        const int32_t e = entry[b * STRIDE];
+        if ((uint32_t)e >= (uint32_t)a.n_pages) continue;
+        bool last = true;                                  // nobody who stays holds it, and no row before this one did
+        for (int o = 0; o < a.width; ++o) last &= !(entry[o * STRIDE] == e && ((alive >> o & 1) || o < b));
+        if (last) gone |= 1u << b;
+    }
+    return gone;
+}
+__device__ __forceinline__ int fork_most(const ForkRow& r) { return max(r.old, max(r.had, r.col + 1)); }
+
+// A thread for each row, as many whole groups at a time as 1024 hold.  Latency is all: the numbers, the parent's length, the open page's entry, two sums, a page of the queue.
+// ALL: the workgroup changes the tables as well, a thread for a column of a group, and gives the pages back; for few rows, whose launches would take longer.
+constexpr int FORK_ALL_WIDTH = 8;          // rows of a group that it has LDS for
+template <bool ALL>
 __global__ __launch_bounds__(PLAN_THREADS) void kv_fork_kernel(ForkArgs a) {
-    __shared__ int64_t scratch[2][2][PLAN_THREADS / 64];
-    __shared__ int32_t s_src[PLAN_THREADS], s_had[PLAN_THREADS], s_page[PLAN_THREADS], s_col[PLAN_THREADS], s_need[PLAN_THREADS];
+    __shared__ int64_t scratch[3][2][PLAN_THREADS / 64];
+    __shared__ int32_t s_src[PLAN_THREADS], s_had[PLAN_THREADS], s_page[PLAN_THREADS], s_col[PLAN_THREADS], s_need[PLAN_THREADS], s_most;
+    __shared__ ForkRow s_rows[ALL ? PLAN_THREADS : 1];
+    __shared__ int32_t s_entry[ALL ? FORK_ALL_WIDTH : 1][PLAN_THREADS];
     const int tid = threadIdx.x, round = PLAN_THREADS / a.width * a.width, mate0 = tid - tid % a.width;
     int first = a.state[0];
     const int avail = clampi(a.state[1], 0, a.n_pages);
     if ((uint32_t)first >= (uint32_t)a.n_pages) first = 0;
+    if (ALL && tid == 0) s_most = 0;
     int64_t needed = 0, taken = 0;                         // of the groups before this round's
     for (int base = 0; base < a.batch; base += round) {
         const int b = base + tid, waves = min((min(a.batch - base, round) + 63) >> 6, PLAN_THREADS / 64);
@@ -480,7 +516,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void kv_fork_kernel(ForkArgs a) {
                 if (s_src[t] < 0 || s_had[t] <= col) continue;
                 const bool writes = s_col[t] == col && s_page[t] == page;
                 writers += writes;
-                holders += writes || a.table[(int64_t)s_src[t] * a.max_pages + col] == page;
+                // (who writes elsewhere in this column holds another page there)
+                holders += writes || (!(s_col[t] == col && s_page[t] >= 0) && a.table[(int64_t)s_src[t] * a.max_pages + col] == page);
                 if (writes && t < tid) lowest = false;
             }
             copy = !(lowest && holders == writers);
@@ -511,18 +548,36 @@ __global__ __launch_bounds__(PLAN_THREADS) void kv_fork_kernel(ForkArgs a) {
             a.slots[b] = ok && wants && (uint32_t)to < (uint32_t)a.n_pages ? (int64_t)to * PAGE + off : -1;
             *reinterpret_cast<i32x4*>(a.copies + (int64_t)b * 4) = ok && copy ? i32x4{page, id, off, 0} : i32x4{-1, -1, 0, 0};
             if (a.granted && leads) a.granted[b / a.width] = ok;
-            a.rows[b] = ok ? ForkRow{parent < 0 || parent >= a.width ? -1 : parent, pages_of(kept), pages_of(held), takes ? col : -1, id}
-                           : ForkRow{tid - mate0, pages_of(held), pages_of(held), -1, -1};
+            const ForkRow r = ok ? ForkRow{valid ? parent : -1, pages_of(kept), pages_of(held), takes ? col : -1, id} : ForkRow{tid - mate0, pages_of(held), pages_of(held), -1, -1};
+            if (ALL) {
+                s_rows[tid] = r;                           // (one round: batch <= 1024)
+                atomicMax(&s_most, fork_most(r));
+            } else {
+                a.rows[b] = r;
+            }
         }
         __syncthreads();
     }
+    int64_t pushed = 0;
+    if constexpr (ALL) {
+        const int cols = s_most, all = a.batch / a.width * cols;
+        int which = 2;                                     // (plan_scan's words: not those of the call before)
+        for (int i0 = 0; i0 < all; i0 += PLAN_THREADS, which = which == 2 ? 0 : 2) {
+            const int i = i0 + tid, group = i < all ? i / cols : 0, row0 = group * a.width;
+            uint32_t gone = i < all ? fork_column<PLAN_THREADS>(a, s_rows + row0, row0, i - group * cols, &s_entry[0][tid]) : 0;
+            int64_t sum, at = (int64_t)first + avail + pushed + plan_scan(__popc(gone), sum, scratch[which], PLAN_THREADS / 64);
+            for (; gone; gone &= gone - 1) a.ring[ring_at(at++, a.n_pages)] = s_entry[__builtin_ctz(gone)][tid];
+            pushed += sum;
+        }
+    }
     if (tid == 0) {
-        *a.head = ForkHead{first, avail, (int)taken};
         a.state_out[0] = (int)ring_at((int64_t)first + taken, a.n_pages);
+        if (ALL) a.state_out[1] = (int)min((int64_t)avail - taken + pushed, (int64_t)a.n_pages);
+        else *a.head = ForkHead{first, avail, (int)taken};
     }
 }
 
-// A thread for a column of a group: it reads the column of all rows before it writes any, so that the tables may be changed in place.
+// A workgroup for FORK_COLS columns of a group.
 __global__ __launch_bounds__(FORK_COLS) void fork_tables_kernel(ForkArgs a) {
     __shared__ int32_t entry[BEAM_WIDTH][FORK_COLS];
     __shared__ ForkRow rows[BEAM_WIDTH];
@@ -530,33 +585,14 @@ __global__ __launch_bounds__(FORK_COLS) void fork_tables_kernel(ForkArgs a) {
     const int tid = threadIdx.x, group = blockIdx.y, row0 = group * a.width, col = blockIdx.x * FORK_COLS + tid, lane = tid & 63, wave = tid >> 6;
     if (tid < a.width) rows[tid] = a.rows[row0 + tid];
     __syncthreads();
-    uint32_t alive = 0;                                    // rows that somebody descends from
     int most = 0;
-    for (int b = 0; b < a.width; ++b) {
-        if (rows[b].src >= 0) alive |= 1u << rows[b].src;
-        most = max(most, max(rows[b].old, max(rows[b].had, rows[b].col + 1)));
-    }
+    for (int b = 0; b < a.width; ++b) most = max(most, fork_most(rows[b]));
     const int64_t chunk = (int64_t)group * a.chunks + blockIdx.x;
     if ((int)blockIdx.x * FORK_COLS >= most) {
         if (tid == 0) a.counts[chunk] = 0;
         return;
     }
-    const int32_t* const from = a.table + (int64_t)row0 * a.max_pages + col;
-    for (int b = 0; b < a.width; ++b) entry[b][tid] = col < rows[b].old ? from[(int64_t)b * a.max_pages] : -1;
-    int32_t* const to = a.table_out + (int64_t)row0 * a.max_pages + col;
-    for (int b = 0; b < a.width; ++b) {
-        const ForkRow& r = rows[b];
-        if (col == r.col) to[(int64_t)b * a.max_pages] = r.page;
-        else if (r.src >= 0 && col < r.had) to[(int64_t)b * a.max_pages] = entry[r.src][tid];
-    }
-    uint32_t gone = 0;
-    for (int b = 0; b < a.width; ++b) {
-        const int32_t e = entry[b][tid];
-        if ((alive >> b & 1) || (uint32_t)e >= (uint32_t)a.n_pages) continue;
-        bool last = true;                                  // nobody who stays holds it, and no row before this one did
-        for (int o = 0; o < a.width; ++o) last &= !(entry[o][tid] == e && ((alive >> o & 1) || o < b));
-        if (last) gone |= 1u << b;
-    }
+    uint32_t gone = fork_column<FORK_COLS>(a, rows, row0, col, &entry[0][tid]);
     const int n = __popc(gone);
     int x = n;
 #pragma unroll
@@ -577,25 +613,24 @@ __global__ __launch_bounds__(FORK_COLS) void fork_tables_kernel(ForkArgs a) {
     if (tid == 0) a.counts[chunk] = total;
 }
 
+// The pages that go back, in order: a thread for each, which looks up its list among 1024.
 __global__ __launch_bounds__(PLAN_THREADS) void fork_pages_kernel(ForkArgs a) {
-    __shared__ int64_t scratch[2][2][PLAN_THREADS / 64], start[PLAN_THREADS];
-    __shared__ int32_t number[PLAN_THREADS];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, chunks = a.batch / a.width * a.chunks;
+    __shared__ int64_t scratch[2][2][PLAN_THREADS / 64];
+    __shared__ int32_t start[PLAN_THREADS];
+    const int tid = threadIdx.x, chunks = a.batch / a.width * a.chunks;
     const ForkHead h = *a.head;
     int64_t pushed = 0;
     int which = 0;
     for (int base = 0; base < chunks; base += PLAN_THREADS, which ^= 1) {
-        const int n = base + tid < chunks ? a.counts[base + tid] : 0;
         int64_t sum;
-        const int64_t before = pushed + plan_scan(n, sum, scratch[which], PLAN_THREADS / 64);
-        start[tid] = before;
-        number[tid] = n;
+        start[tid] = (int)plan_scan(base + tid < chunks ? a.counts[base + tid] : 0, sum, scratch[which], PLAN_THREADS / 64);
         __syncthreads();
-        if (sum) {
-            for (int i = wave; i < PLAN_THREADS; i += PLAN_THREADS / 64) {
-                const int32_t* const list = a.freed + (int64_t)(base + i) * FORK_COLS * a.width;
-                for (int j = lane; j < number[i]; j += 64) a.ring[ring_at((int64_t)h.first + h.avail + start[i] + j, a.n_pages)] = list[j];
-            }
+        for (int i = tid; i < (int)sum; i += PLAN_THREADS) {
+            int lo = 0;                                    // the last list that starts at or before i
+#pragma unroll
+            for (int step = PLAN_THREADS / 2; step > 0; step >>= 1)
+                if (start[lo + step] <= i) lo += step;
+            a.ring[ring_at((int64_t)h.first + h.avail + pushed + i, a.n_pages)] = a.freed[(int64_t)(base + lo) * FORK_COLS * a.width + (i - start[lo])];
         }
         pushed += sum;
         __syncthreads();
@@ -619,19 +654,32 @@ struct CopyArgs {
 };
 static_assert(sizeof(CopyArgs) <= 4096, "a launch's arguments");
 
-// A workgroup for a copy in a layer: 16 lanes a row of 256 bytes.
+// A workgroup for a copy in a layer: 16 lanes a row of 256 bytes, four rows of theirs under way.
 __global__ __launch_bounds__(COPY_THREADS) void kv_copy_kernel(CopyArgs a) {
     const CopyLayer& l = a.layer[blockIdx.y];
-    const int32_t* const c = a.copies + (int64_t)blockIdx.x * 4;
-    const int from = c[0], to = c[1], n = min(c[2], PAGE);
-    if ((uint32_t)from >= (uint32_t)l.n_pages || (uint32_t)to >= (uint32_t)l.n_pages || from == to) return;
+    const i32x4 copy = *reinterpret_cast<const i32x4*>(a.copies + (int64_t)blockIdx.x * 4);
+    const int from = copy[0], to = copy[1], n = min(copy[2], PAGE);
+    if ((uint32_t)from >= (uint32_t)l.n_pages || (uint32_t)to >= (uint32_t)l.n_pages || from == to || n <= 0) return;
     const int64_t page = (int64_t)a.G * PAGE * D;
-    for (int i = threadIdx.x; i < 2 * a.G * PAGE * 16; i += COPY_THREADS) {
-        const int row = i >> 4, token = row & (PAGE - 1);
-        if (token >= n) continue;
-        uint16_t* const pool = row < a.G * PAGE ? l.k : l.v;
-        const int64_t at = (int64_t)(row < a.G * PAGE ? row : row - a.G * PAGE) * D + (i & 15) * 8;
-        *reinterpret_cast<u32x4*>(pool + to * page + at) = *reinterpret_cast<const u32x4*>(pool + from * page + at);
+    const int rows = a.G * n, c = (threadIdx.x & 15) * 8;  // of K, and of V
+    const uint32_t over_n = (65536 + n - 1) / n;           // r / n = r over_n >> 16 for r < 4096 (r times what over_n is too large by stays below 65536 / n)
+    constexpr int RUN = 4, STEP = COPY_THREADS / 16;
+    for (int r0 = threadIdx.x >> 4; r0 < 2 * rows; r0 += RUN * STEP) {
+        u32x4 x[RUN];
+        int64_t at[RUN];
+        uint16_t* pool[RUN];
+#pragma unroll
+        for (int j = 0; j < RUN; ++j) {
+            const int r = r0 + j * STEP, row = r < rows ? r : r - rows;
+            if (r >= 2 * rows) continue;
+            const int head = rows <= 4096 ? (int)(row * over_n >> 16) : row / n;
+            pool[j] = r < rows ? l.k : l.v;
+            at[j] = (int64_t)(head * PAGE + row - head * n) * D + c;
+            x[j] = *reinterpret_cast<const u32x4*>(pool[j] + from * page + at[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < RUN; ++j)
+            if (r0 + j * STEP < 2 * rows) *reinterpret_cast<u32x4*>(pool[j] + to * page + at[j]) = x[j];
     }
 }
 
@@ -642,7 +690,7 @@ struct SharedArgs {
     int32_t *entries, *count;
     int32_t batch, width, max_pages, n_pages, max_len, max_entries;
 };
-constexpr int SHARED_COLS = 256;
+constexpr int SHARED_COLS = 1024;
 
 // A workgroup for a group, a thread for a column.
 __global__ __launch_bounds__(SHARED_COLS) void shared_pages_kernel(SharedArgs a) {
