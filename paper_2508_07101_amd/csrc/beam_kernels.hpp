@@ -654,7 +654,7 @@ struct CopyArgs {
 };
 static_assert(sizeof(CopyArgs) <= 4096, "a launch's arguments");
 
-// A workgroup for a copy in a layer: 16 lanes a row of 256 bytes, four rows of theirs under way.
+// A workgroup for a copy in a layer: 16 lanes a row of 256 bytes, eight rows of theirs under way.
 __global__ __launch_bounds__(COPY_THREADS) void kv_copy_kernel(CopyArgs a) {
     const CopyLayer& l = a.layer[blockIdx.y];
     const i32x4 copy = *reinterpret_cast<const i32x4*>(a.copies + (int64_t)blockIdx.x * 4);
@@ -663,7 +663,7 @@ __global__ __launch_bounds__(COPY_THREADS) void kv_copy_kernel(CopyArgs a) {
     const int64_t page = (int64_t)a.G * PAGE * D;
     const int rows = a.G * n, c = (threadIdx.x & 15) * 8;  // of K, and of V
     const uint32_t over_n = (65536 + n - 1) / n;           // r / n = r over_n >> 16 for r < 4096 (r times what over_n is too large by stays below 65536 / n)
-    constexpr int RUN = 4, STEP = COPY_THREADS / 16;
+    constexpr int RUN = 8, STEP = COPY_THREADS / 16;
     for (int r0 = threadIdx.x >> 4; r0 < 2 * rows; r0 += RUN * STEP) {
         u32x4 x[RUN];
         int64_t at[RUN];
