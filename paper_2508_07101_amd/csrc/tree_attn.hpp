@@ -724,6 +724,7 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
         f32x16 x;
         TreeWeights p;
         uint32_t there = 0xffffffffu, common = 0xffffffffu;       // of the tile that p belongs to
+        bool live = true;                                         // some row of the wave attends to it (of a group's pages, mostly few do)
         int it = 0;
         if (!idle) {
             TreeKeys kf;
@@ -738,16 +739,29 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
                     read_values(vf, ring + v_at(it - 1), lane);
                     add_values(row, vf, p);
                 } else if constexpr (BEAM) {
-                    if (there != 0) note_odd(it - 1, add_looked_over(row, p, ring + v_at(it - 1), ~common, lane) & there);
+                    if (live) note_odd(it - 1, add_looked_over(row, p, ring + v_at(it - 1), ~common, lane) & there);
                 } else if (there != 0) {
                     note_odd(it - 1, add_washed(row, p, ring + v_at(it - 1), ~common, lane) & there);
                 }
             }
             if (it >= steps) return;
             there = common = 0xffffffffu;
-            if (it >= plain) mask_scores(x, attended(it, there, common), half);
-            const float sum = weigh(row.m, x, a.scale_log2e, p);
-            raise_and_weigh(row, x, a.scale_log2e, p, sum);
+            if constexpr (BEAM) {
+                live = true;
+                if (it >= plain) {
+                    const uint32_t allowed = attended(it, there, common);
+                    live = __any(allowed != 0);
+                    if (live) mask_scores(x, allowed, half);
+                }
+                if (live) {
+                    const float sum = weigh(row.m, x, a.scale_log2e, p);
+                    raise_and_weigh(row, x, a.scale_log2e, p, sum);
+                }
+            } else {
+                if (it >= plain) mask_scores(x, attended(it, there, common), half);
+                const float sum = weigh(row.m, x, a.scale_log2e, p);
+                raise_and_weigh(row, x, a.scale_log2e, p, sum);
+            }
             if (it + 1 < steps) {
                 TreeKeys kf;
                 read_keys(kf, ring + k_at(it + 1), lane);
