@@ -547,8 +547,25 @@ def kv_commit(params, kv_layers, base, path, n_path, keep=None):
 
 # ---- beam search over paged caches ---------------------------------------------
 
+def _device() -> int:
+    return torch.cuda.current_device()
+
+
+if hasattr(torch._C, "_cuda_getDevice"):
+    _device = torch._C._cuda_getDevice                           # noqa: F811  (what current_device() asks once CUDA is up; a tenth of its time)
+
+
+def _take(what: str, name: str, t: torch.Tensor, dtype, n: int, gpu: int, width: int = 0) -> int:
+    """The address of a tensor that holds n contiguous numbers of this type at least (in rows of `width`, or flat), on the current GPU."""
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous() or t.get_device() != gpu or (width and t.shape[-1] != width and t.dim() > 1):
+        rows = f" in rows of {width}" if width else ""
+        raise ValueError(f"{what}: {name} of {n} or more {dtype}{rows}, contiguous, on the current GPU was expected, not {tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
 def _need_group(what: str, rows: int, width: int):
-    _need(width >= 1 and rows >= 1 and rows % width == 0, f"{what}: groups of {width} rows in {rows}")
+    if width < 1 or rows < 1 or rows % width != 0:
+        raise ValueError(f"{what}: groups of {width} rows in {rows}")
 
 
 def beam_workspace_bytes(rows: int, vocab: int, n: int) -> int:
@@ -564,23 +581,22 @@ def alloc_beam_workspace(rows: int, vocab: int, n: int, device="cuda") -> torch.
 def beam_select(logits, scores, width: int, out_scores, parents, tokens, ws, ended=None, out_ended=None, end_token: int = -1):
     """The best continuations of every group of `width` rows: logits [rows, vocab] (bf16, fp16 or fp32; a view of wider rows, or contiguous), scores float32 [rows];
     out_scores float32, parents, tokens and out_ended int32, [groups, n] each, best first.  ended int32 [rows]: rows that propose nothing but end_token."""
-    _need(logits.dim() == 2 and logits.dtype in DTYPES and logits.is_cuda, "beam_select: logits are [rows, vocab] in bf16, fp16 or fp32, on the GPU")
+    what, gpu = "beam_select", _device()
+    if logits.dim() != 2 or logits.dtype not in DTYPES or logits.get_device() != gpu:
+        raise ValueError(f"{what}: logits are [rows, vocab] in bf16, fp16 or fp32, on the current GPU, not {tuple(logits.shape)} {logits.dtype} on {logits.device}")
     rows, vocab = logits.shape
-    _need_group("beam_select", rows, width)
-    strides = _strides(logits, (vocab, 1))
+    _need_group(what, rows, width)
+    strides = logits.stride() if rows > 1 and vocab > 1 else _strides(logits, (vocab, 1))
     _need(strides[1] == 1 and strides[0] >= vocab, "beam_select: a row's logits stand side by side")
-    _need(out_scores.dim() == 2 and out_scores.shape[0] == rows // width, "beam_select: out_scores is [groups, n]")
+    groups = rows // width
+    _need(out_scores.dim() == 2 and out_scores.shape[0] == groups, "beam_select: out_scores is [groups, n]")
     n = out_scores.shape[1]
-    _need_int("beam_select", rows, torch.float32, scores)
-    _need_int("beam_select", rows, torch.int32, *(() if ended is None else (ended,)))
-    _need_rows("beam_select", "out_scores", out_scores, rows // width, n, torch.float32)
-    for name, t in (("parents", parents), ("tokens", tokens), ("out_ended", out_ended)):
-        if t is not None or name != "out_ended":
-            _need_rows("beam_select", name, t, rows // width, n, torch.int32)
-    _need_workspace("beam_select", ws)
     d = CusaBeams(logits.data_ptr(), DTYPES[logits.dtype], strides[0], rows, width, vocab, n, end_token)
-    _check(load().cusa_beam_select(ctypes.byref(d), scores.data_ptr(), _ptr(ended), out_scores.data_ptr(), parents.data_ptr(), tokens.data_ptr(), _ptr(out_ended),
-                                   ws.data_ptr(), ws.numel(), _stream()), "cusa_beam_select")
+    _check(load().cusa_beam_select(
+        ctypes.byref(d), _take(what, "scores", scores, torch.float32, rows, gpu), None if ended is None else _take(what, "ended", ended, torch.int32, rows, gpu),
+        _take(what, "out_scores", out_scores, torch.float32, groups * n, gpu), _take(what, "parents", parents, torch.int32, groups * n, gpu, n),
+        _take(what, "tokens", tokens, torch.int32, groups * n, gpu, n), None if out_ended is None else _take(what, "out_ended", out_ended, torch.int32, groups * n, gpu, n),
+        _take(what, "workspace", ws, torch.uint8, 0, gpu), ws.numel(), _stream()), "cusa_beam_select")
 
 
 def fork_workspace_bytes(batch: int, max_pages: int) -> int:
@@ -595,20 +611,21 @@ def kv_fork(pool: PagePool, width: int, held, parents, lens, slots, copies, ws, 
     """Rows of a group take over the tokens of the rows that they descend from (parents, int32, numbers within the group; -1: none), and with `grow` each that has a parent and has
     not ended gets room for one token: lens int32 [B], slots int64 [B], copies int32 [B, 4] (from, to, tokens, 0: KvCopy makes them).
     table_out, state_out: where the new table and the queue's state go instead of back into the pool."""
-    n, max_pages = pool.block_table.shape
-    _need_group("kv_fork", n, width)
-    _need_int("kv_fork", n, torch.int32, held, parents, lens, *(() if ended is None else (ended,)))
-    _need_int("kv_fork", n, torch.int64, slots)
-    _need_rows("kv_fork", "copies", copies, n, 4, torch.int32)
-    _need_rows("kv_fork", "table_out", pool.block_table if table_out is None else table_out, n, max_pages, torch.int32)
-    _need_int("kv_fork", 2, torch.int32, pool.state, pool.state if state_out is None else state_out)
-    _need_int("kv_fork", 1, torch.int32, pool.block_table, pool.ring)
-    _need_int("kv_fork", n // width, torch.int32, *(() if granted is None else (granted,)))
-    _need_workspace("kv_fork", ws)
-    d = pool.desc(state_out)
-    _check(load().cusa_kv_fork(ctypes.byref(d), width, held.data_ptr(), parents.data_ptr(), _ptr(ended), 1 if grow else 0,
-                               (pool.block_table if table_out is None else table_out).data_ptr(), lens.data_ptr(), slots.data_ptr(), copies.data_ptr(), _ptr(granted),
-                               ws.data_ptr(), ws.numel(), _stream()), "cusa_kv_fork")
+    what, gpu, i32 = "kv_fork", _device(), torch.int32
+    table, ring, state = pool.block_table, pool.ring, pool.state
+    _need(table.dim() == 2, "kv_fork: the block table is [rows, columns]")
+    n, max_pages = table.shape
+    _need_group(what, n, width)
+    at = _take(what, "block_table", table, i32, 1, gpu)
+    at_state = _take(what, "state", state, i32, 2, gpu)
+    d = CusaPool(KV_PAGED, n, 0, at, max_pages, 16, ring.numel(), _take(what, "ring", ring, i32, 1, gpu), at_state,
+                 at_state if state_out is None else _take(what, "state_out", state_out, i32, 2, gpu))
+    _check(load().cusa_kv_fork(
+        ctypes.byref(d), width, _take(what, "held", held, i32, n, gpu), _take(what, "parents", parents, i32, n, gpu),
+        None if ended is None else _take(what, "ended", ended, i32, n, gpu), 1 if grow else 0,
+        at if table_out is None else _take(what, "table_out", table_out, i32, n * max_pages, gpu, max_pages), _take(what, "lens", lens, i32, n, gpu),
+        _take(what, "slots", slots, torch.int64, n, gpu), _take(what, "copies", copies, i32, n * 4, gpu, 4),
+        None if granted is None else _take(what, "granted", granted, i32, n // width, gpu), _take(what, "workspace", ws, torch.uint8, 0, gpu), ws.numel(), _stream()), "cusa_kv_fork")
 
 
 class KvCopy:
@@ -622,12 +639,12 @@ class KvCopy:
 
     def run(self, copies):
         """copies int32 [n, 4]: from, to, tokens, 0."""
-        n = copies.shape[0]
         _need(copies.dim() == 2, "kv_copy: copies is [n, 4]")
-        _need_rows("kv_copy", "copies", copies, n, 4, torch.int32)
+        n = copies.shape[0]
         if n == 0:
             return
-        _check(load().cusa_kv_copy(ctypes.byref(self.params), self.n, self.kvs, copies.data_ptr(), n, _stream()), "cusa_kv_copy")
+        at = _take("kv_copy", "copies", copies, torch.int32, n * 4, _device(), 4)
+        _check(load().cusa_kv_copy(ctypes.byref(self.params), self.n, self.kvs, at, n, _stream()), "cusa_kv_copy")
 
 
 def kv_copy(params, kv_layers, copies):
@@ -646,13 +663,12 @@ class SharedPages:
         most = min(width * ((max_seq_len + 15) // 16), n_pages)
         return SharedPages(width, torch.zeros((batch // width, most, 4), dtype=torch.int32, device=device), torch.zeros((batch // width, 2), dtype=torch.int32, device=device))
 
-    def desc(self, what: str, batch: int) -> CusaShared:
+    def desc(self, what: str, batch: int, gpu: int) -> CusaShared:
+        e, groups = self.entries, batch // self.width if self.width else 0
         _need_group(what, batch, self.width)
-        e, groups = self.entries, batch // self.width
-        _need(e.dim() == 3 and e.shape[0] >= groups and e.shape[2] == 4, f"{what}: entries are [groups, most, 4]")
-        _need_int(what, groups * e.shape[1] * 4, torch.int32, e)
-        _need_rows(what, "count", self.count, groups, 2, torch.int32)
-        return CusaShared(self.width, e.shape[1], e.data_ptr(), self.count.data_ptr())
+        shape = e.shape
+        _need(len(shape) == 3 and shape[0] >= groups and shape[2] == 4, "entries of shared pages are [groups, most, 4]")
+        return CusaShared(self.width, shape[1], _take(what, "entries", e, torch.int32, groups * shape[1] * 4, gpu), _take(what, "count", self.count, torch.int32, groups * 2, gpu, 2))
 
 
 def pages_workspace_bytes(batch: int, max_seq_len: int) -> int:
@@ -665,17 +681,17 @@ def alloc_pages_workspace(batch: int, max_seq_len: int, device="cuda") -> torch.
 
 def shared_pages(block_table, lens, max_seq_len: int, n_pages: int, shared: SharedPages, ws):
     """Which pages the groups hold, from the rows' block table and lengths: once a step, for all its layers."""
+    what, gpu = "shared_pages", _device()
     _need(block_table.dim() == 2, "shared_pages: block_table is [rows, columns]")
     n, columns = block_table.shape
-    _need_int("shared_pages", n, torch.int32, block_table, lens)
-    _need_workspace("shared_pages", ws)
-    d = shared.desc("shared_pages", n)
-    kv = CusaKv(None, None, KV_PAGED, 0, 0, 0, block_table.data_ptr(), columns, 16, n_pages, lens.data_ptr(), max_seq_len)
-    _check(load().cusa_shared_pages(ctypes.byref(kv), n, ctypes.byref(d), ws.data_ptr(), ws.numel(), _stream()), "cusa_shared_pages")
+    d = shared.desc(what, n, gpu)
+    kv = CusaKv(None, None, KV_PAGED, 0, 0, 0, _take(what, "block_table", block_table, torch.int32, n * columns, gpu), columns, 16, n_pages,
+                _take(what, "lens", lens, torch.int32, n, gpu), max_seq_len)
+    _check(load().cusa_shared_pages(ctypes.byref(kv), n, ctypes.byref(d), _take(what, "workspace", ws, torch.uint8, 0, gpu), ws.numel(), _stream()), "cusa_shared_pages")
 
 
 def beam_attn_workspace_bytes(params: CusaParams, max_seq_len: int, shared: SharedPages) -> int:
-    n, d = ctypes.c_size_t(0), shared.desc("beam_attn", params.batch)
+    n, d = ctypes.c_size_t(0), shared.desc("beam_attn", params.batch, shared.entries.get_device())
     _check(load().cusa_beam_attn_workspace_bytes(ctypes.byref(params), max_seq_len, ctypes.byref(d), ctypes.byref(n)), "cusa_beam_attn_workspace_bytes")
     return int(n.value)
 
@@ -687,18 +703,17 @@ def alloc_beam_attn_workspace(params: CusaParams, max_seq_len: int, shared: Shar
 def beam_attn(params: CusaParams, q, kv: KvCache, shared: SharedPages, out, ws):
     """Full attention of every row's token, q [B, H, 128] (a view of a fused projection's rows, or contiguous), over the pages of its group: each is read once
     for all rows that hold it.  shared: of the same tables and lengths."""
+    what, gpu = "beam_attn", _device()
+    _need(q.dim() == 3, "beam_attn: q is [batch, n_q_heads, 128]")
     n, heads, d = q.shape
     strides = _strides(q, (heads * d, d, 1)) if n == 1 or heads == 1 else q.stride()
-    _need(q.dtype is torch.bfloat16 and n == params.batch and heads == params.n_q_heads and d == params.head_dim and strides[2] == 1 and strides[1] == d,
-          "beam_attn: q is bf16 [batch, n_q_heads, 128], heads side by side")
-    _need(q.is_cuda and out.is_cuda, "beam_attn: q and out are on the GPU")
-    _need(out.dtype is torch.bfloat16 and out.is_contiguous() and out.numel() >= n * heads * d, "beam_attn: out is bf16 [batch, n_q_heads, 128], contiguous")
-    _need_workspace("beam_attn", ws)
-    _need(kv.block_table is not None, "beam_attn: a paged cache")
-    s = shared.desc("beam_attn", n)
-    c = _cache_desc("beam_attn", params, kv)
-    _check(load().cusa_beam_attn(ctypes.byref(params), q.data_ptr(), strides[0], ctypes.byref(c), ctypes.byref(s), out.data_ptr(), ws.data_ptr(), ws.numel(), _stream()),
-           "cusa_beam_attn")
+    _need(q.dtype is torch.bfloat16 and n == params.batch and heads == params.n_q_heads and d == params.head_dim and strides[2] == 1 and strides[1] == d and q.get_device() == gpu,
+          "beam_attn: q is bf16 [batch, n_q_heads, 128], heads side by side, on the current GPU")
+    _need(kv.block_table is not None and kv.k.get_device() == gpu, "beam_attn: a paged cache on the current GPU")
+    s = shared.desc(what, n, gpu)
+    c = _cache_desc(what, params, kv)
+    _check(load().cusa_beam_attn(ctypes.byref(params), q.data_ptr(), strides[0], ctypes.byref(c), ctypes.byref(s), _take(what, "out", out, torch.bfloat16, n * heads * d, gpu),
+                                 _take(what, "workspace", ws, torch.uint8, 0, gpu), ws.numel(), _stream()), "cusa_beam_attn")
 
 
 def probe_stream_read(src: torch.Tensor, sink: torch.Tensor):

@@ -91,7 +91,7 @@ def test_attention_with_heavy_tokens():
     c.check(c.run())
 
 
-@pytest.mark.parametrize("width,H,G", [(4, 16, 4), (20, 8, 2), (32, 8, 1)])
+@pytest.mark.parametrize("width,H,G", [(4, 16, 4), (12, 16, 4), (20, 8, 2), (32, 8, 1)])
 def test_what_a_row_does_not_attend_to_does_not_reach_it(width, H, G):
     """NaN and infinities behind the rows' ends, in pages of other rows and of nobody."""
     print("foreign", width, flush=True)
