@@ -461,6 +461,10 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
     if (tid == 0) lds.first_bad = 0x7fffffff;
     __syncthreads();
 
+    // (a group's list is asked for before q: one way to memory and back instead of two)
+    const i32x4* const list = BEAM ? reinterpret_cast<const i32x4*>(a.entries) + b * a.entry_stride + begin / PAGE : nullptr;
+    i32x4 entry = {0, 0, 0, 0};
+    if constexpr (BEAM) entry = list[min(tid, (end - begin) / PAGE - 1)];
     TreeRow row;
     const int my_row = row0 + mine * 32 + col;
     const bool there = my_row < rows;
@@ -496,9 +500,8 @@ __device__ __forceinline__ void tree_rows(const TreeArgs& a, const TreeSpan& s, 
     int good = end;                                               // tokens before this one are all there
     if constexpr (BEAM) {
         const int entries = (end - begin) / PAGE;
-        const i32x4* const list = reinterpret_cast<const i32x4*>(a.entries) + b * a.entry_stride + begin / PAGE;
         for (int e = tid; e < entries; e += TREE_THREADS) {
-            const i32x4 x = list[e];
+            const i32x4 x = e < TREE_THREADS ? entry : list[e];
             const bool is = (uint32_t)x[0] < (uint32_t)a.cache.n_pages && x[1] >= 0;   // (all are, of a list that cusa_shared_pages made for this pool)
             lds.list[e] = is ? (x[0] * a.cache.kv.G + kvh) * PAGE : 0;
             lds.first[e] = min(x[1], 0x7fffffff / PAGE) * PAGE;
