@@ -1,8 +1,8 @@
 // Host side of beam search over paged caches: argument checks and launches.  Nothing here allocates or synchronises.
 #include "host.hpp"
 
+#include "beam_attn.hpp"
 #include "beam_kernels.hpp"
-#include "tree_attn.hpp"
 
 using namespace cusa;
 
@@ -290,7 +290,10 @@ cusa_status cusa_beam_attn(const cusa_params* params, const void* q, int64_t q_s
     const int64_t units = ((int64_t)pl.n_splits * G * groups + 7) / 8 * 8 * pl.m_tiles;
     if (units > 0x7fffffff) return CUSA_ERR_UNSUPPORTED;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    launch(KID_BEAM_ATTN, tree_attn_kernel<true, false, true>, dim3((unsigned)units), TREE_THREADS, 0, s, a);
+    const dim3 grid((unsigned)units);
+    if (width * g <= 16) launch(KID_BEAM_ATTN, beam_attn_kernel<1>, dim3((unsigned)(pl.n_splits * G * groups)), FEW_THREADS, 0, s, a);
+    else if (width * g <= FEW_ROWS) launch(KID_BEAM_ATTN, beam_attn_kernel<2>, dim3((unsigned)(pl.n_splits * G * groups)), FEW_THREADS, 0, s, a);
+    else launch(KID_BEAM_ATTN, tree_attn_kernel<true, false, true>, grid, TREE_THREADS, 0, s, a);
     if (launch_status() != CUSA_OK) return CUSA_ERR_LAUNCH;
     if (pl.n_splits > 1) {                 // as many workgroups as have a row each, but not more than a few rounds of the chip
         const int64_t rows = ((int64_t)width * params->n_q_heads + REDUCE_WAVES - 1) / REDUCE_WAVES, most = std::max(1, 8192 / groups);
