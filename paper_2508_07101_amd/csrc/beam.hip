@@ -266,7 +266,8 @@ cusa_status cusa_beam_attn(const cusa_params* params, const void* q, int64_t q_s
     if (!tree_len_served(TREE_GROUP, len)) return CUSA_ERR_UNSUPPORTED;
     const TreeWs w = tree_workspace(TREE_GROUP, (int)len, groups, params->n_q_heads, G, params->batch, width);
     if ((st = check_workspace(ws, ws_bytes, w.total)) != CUSA_OK) return st;
-    const TreePlan pl = plan_tree(TREE_GROUP, (int)len, groups, G, g, width);
+    const bool few = width * g <= FEW_ROWS;
+    const TreePlan pl = few ? plan_few((int)len, groups, G) : plan_tree(TREE_GROUP, (int)len, groups, G, g, width);
     TreeArgs a = {};
     a.cache = cache_args(params, kv);
     a.q = static_cast<const uint16_t*>(q);
@@ -290,10 +291,13 @@ cusa_status cusa_beam_attn(const cusa_params* params, const void* q, int64_t q_s
     const int64_t units = ((int64_t)pl.n_splits * G * groups + 7) / 8 * 8 * pl.m_tiles;
     if (units > 0x7fffffff) return CUSA_ERR_UNSUPPORTED;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const dim3 grid((unsigned)units);
-    if (width * g <= 16) launch(KID_BEAM_ATTN, beam_attn_kernel<1>, dim3((unsigned)(pl.n_splits * G * groups)), FEW_THREADS, 0, s, a);
-    else if (width * g <= FEW_ROWS) launch(KID_BEAM_ATTN, beam_attn_kernel<2>, dim3((unsigned)(pl.n_splits * G * groups)), FEW_THREADS, 0, s, a);
-    else launch(KID_BEAM_ATTN, tree_attn_kernel<true, false, true>, grid, TREE_THREADS, 0, s, a);
+    if (few) {
+        const dim3 grid((unsigned)(pl.n_splits * G * groups));
+        if (width * g <= 16) launch(KID_BEAM_ATTN, beam_attn_kernel<1>, grid, FEW_THREADS, 0, s, a);
+        else launch(KID_BEAM_ATTN, beam_attn_kernel<2>, grid, FEW_THREADS, 0, s, a);
+    } else {
+        launch(KID_BEAM_ATTN, tree_attn_kernel<true, false, true>, dim3((unsigned)units), TREE_THREADS, 0, s, a);
+    }
     if (launch_status() != CUSA_OK) return CUSA_ERR_LAUNCH;
     if (pl.n_splits > 1) {                 // as many workgroups as have a row each, but not more than a few rounds of the chip
         const int64_t rows = ((int64_t)width * params->n_q_heads + REDUCE_WAVES - 1) / REDUCE_WAVES, most = std::max(1, 8192 / groups);

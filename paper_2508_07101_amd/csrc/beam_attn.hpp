@@ -8,7 +8,6 @@
 namespace cusa {
 
 constexpr int FEW_WAVES = 4, FEW_THREADS = 64 * FEW_WAVES;
-constexpr int FEW_ROWS = 32;
 
 template <int NB>                          // blocks of 16 rows
 struct FewLds {
@@ -108,7 +107,7 @@ __global__ __launch_bounds__(FEW_THREADS, 2) void beam_attn_kernel(TreeArgs a) {
         for (int j = 0; j < 2; ++j) {
             const uint16_t* const kp = a.cache.kv.k + t.at[j];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) k[j][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + k_part + i * 32));
+            for (int i = 0; i < 4; ++i) k[j][i] = *reinterpret_cast<const u32x4*>(kp + k_part + i * 32);
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j)
