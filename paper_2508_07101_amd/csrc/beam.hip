@@ -292,7 +292,7 @@ cusa_status cusa_beam_attn(const cusa_params* params, const void* q, int64_t q_s
     if (units > 0x7fffffff) return CUSA_ERR_UNSUPPORTED;
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (few) {
-        const dim3 grid((unsigned)(pl.n_splits * G * groups));
+        const dim3 grid((unsigned)units);
         if (width * g <= 16) launch(KID_BEAM_ATTN, beam_attn_kernel<1>, grid, FEW_THREADS, 0, s, a);
         else launch(KID_BEAM_ATTN, beam_attn_kernel<2>, grid, FEW_THREADS, 0, s, a);
     } else {

@@ -50,16 +50,19 @@ __device__ __forceinline__ float of_row_max(float v) {      // over the four lan
 template <int NB>
 __global__ __launch_bounds__(FEW_THREADS, 2) void beam_attn_kernel(TreeArgs a) {
     __shared__ FewLds<NB> lds;
-    const uint32_t G = a.cache.kv.G, pairs = G * (uint32_t)a.batch, unit = blockIdx.x, pair = unit % pairs;
-    const int split = unit / pairs, b = pair / G, kvh = pair - b * G;
+    // Workgroups go to the 8 XCDs in turn: those of one KV head's pages come 8 apart, to the same L2.
+    const uint32_t turn = blockIdx.x >> 3, block = turn % (uint32_t)a.m_tiles, unit = turn / (uint32_t)a.m_tiles * 8 + (blockIdx.x & 7);
+    TreeSpan s;
+    int b, kvh, split;
+    if (!group_work(a, (int)unit, s, b, kvh, split)) return;
+    const int row0 = block * (16 * NB);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, q4 = lane >> 4;
-    const int g = 1 << a.g_shift, rows = a.max_nodes << a.g_shift, beam0 = b * a.max_nodes;
-    // the queries, rows' lengths: on their way while the pieces are found
+    const int g = 1 << a.g_shift, all_rows = a.max_nodes << a.g_shift, rows = min(all_rows - row0, 16 * NB), beam0 = b * a.max_nodes;
     u32x4 qv[NB][4];
     int len[NB];
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-        const int row = min(i * 16 + n, rows - 1), beam = beam0 + (row >> a.g_shift);
+        const int row = row0 + min(i * 16 + n, rows - 1), beam = beam0 + (row >> a.g_shift);
         const uint16_t* const p = a.q + (int64_t)beam * a.q_stride + ((kvh << a.g_shift) + (row & (g - 1))) * D + q4 * 8;
 #pragma unroll
         for (int k = 0; k < 4; ++k) qv[i][k] = *reinterpret_cast<const u32x4*>(p + k * 32);
@@ -67,18 +70,17 @@ __global__ __launch_bounds__(FEW_THREADS, 2) void beam_attn_kernel(TreeArgs a) {
     }
     if (tid < BEAM_LIST / 32) lds.odd[tid] = 0;
     if (tid == 0) lds.any_odd = 0;
-    const TreeSpan s = tree_work<false, true>(a, b);
-    if (s.all == 0 && split == 0) {                        // a group without tokens
+    if (s.all == 0) {                        // a group without tokens
         for (int i = tid; i < rows * (D / 4); i += FEW_THREADS) {
-            const int row = i >> 5;
+            const int row = row0 + (i >> 5);
             *reinterpret_cast<u32x2*>(a.out + ((int64_t)(beam0 + (row >> a.g_shift)) * a.H + (kvh << a.g_shift) + (row & (g - 1))) * D + (i & 31) * 4) = u32x2{0, 0};
         }
-        if (a.n_splits > 1 && kvh == 0 && tid == 0) a.pieces[b] = 0;
+        if (a.n_splits > 1 && kvh == 0 && block == 0 && tid == 0) a.pieces[b] = 0;
+        return;
     }
     const int begin = split * s.chunk;
-    if (begin >= s.all) return;
     __syncthreads();                                       // (odd is clear before anyone marks a page)
-    if (a.n_splits > 1 && split == 0 && kvh == 0 && tid == 0) a.pieces[b] = (s.all + s.chunk - 1) / s.chunk;
+    if (a.n_splits > 1 && split == 0 && kvh == 0 && block == 0 && tid == 0) a.pieces[b] = (s.all + s.chunk - 1) / s.chunk;
     const int entries = (min(begin + s.chunk, s.all) - begin) / PAGE, tiles = (entries + 1) >> 1;
     const int plain = clampi(s.pre - begin, 0, entries * PAGE) / TREE_TILE;   // tiles that every row attends to as a whole: the first ones
     const int32_t* const list = a.entries + (b * a.entry_stride + begin / PAGE) * 4;
@@ -114,16 +116,22 @@ __global__ __launch_bounds__(FEW_THREADS, 2) void beam_attn_kernel(TreeArgs a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) load_to_lds(a.cache.kv.v + t.at[j], (uint32_t)(v_part + i * 4 * D) * 2, vlds + buffer * (TREE_TILE * 256) + j * (PAGE * 256) + i * 1024);
     };
+    // The first tile from t on that one of this workgroup's rows attends to.
+    const uint32_t here = (uint32_t)((1ull << (((row0 + rows - 1) >> a.g_shift) + 1)) - (1ull << (row0 >> a.g_shift)));
+    auto find = [&](int t, FewTile& tile) {
+        for (; t < tiles; t += FEW_WAVES) {
+            tile = few_tile(a, list, t * 2, entries, kvh);
+            if ((tile.holders[0] | tile.holders[1]) & here) break;
+        }
+        return t;
+    };
     FewTile now, next;
-    if (wave < tiles) {
-        now = few_tile(a, list, wave * 2, entries, kvh);
-        request(now, 0);
-    }
-    int buffer = 0;
+    int t = find(wave, now), buffer = 0;
+    if (t < tiles) request(now, 0);
 #pragma unroll 1
-    for (int t = wave; t < tiles; t += FEW_WAVES, buffer ^= 1) {
-        const bool more = t + FEW_WAVES < tiles;
-        if (more) next = few_tile(a, list, (t + FEW_WAVES) * 2, entries, kvh);
+    for (int t_next; t < tiles; t = t_next, buffer ^= 1) {
+        t_next = find(t + FEW_WAVES, next);
+        const bool more = t_next < tiles;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // K in registers, V in LDS
         f32x4 x[NB][2];
 #pragma unroll
@@ -142,7 +150,7 @@ __global__ __launch_bounds__(FEW_THREADS, 2) void beam_attn_kernel(TreeArgs a) {
             if (!whole) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const uint32_t held = now.holders[j] >> (((i * 16 + n) >> a.g_shift) & 31) & 1;
+                    const uint32_t held = now.holders[j] >> (((row0 + i * 16 + n) >> a.g_shift) & 31) & 1;
                     const int left = held ? len[i] - now.first[j] : 0;
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
@@ -253,7 +261,7 @@ __global__ __launch_bounds__(FEW_THREADS, 2) void beam_attn_kernel(TreeArgs a) {
             sum += lds.l[w][r] * exp2f(lds.m[w][r] - top);
             v += *reinterpret_cast<const f32x4*>(sums + (w * 16 * NB + r) * (D * 4) + ((c ^ (r & 15)) << 4));
         }
-        const int of = r >> a.g_shift, length = clampi(a.cache.kv.seq_lens[beam0 + of], 0, a.cache.max_len);
+        const int of = (row0 + r) >> a.g_shift, length = clampi(a.cache.kv.seq_lens[beam0 + of], 0, a.cache.max_len);
         if (any_odd) {
             // Pages with values that are not finite: the rows that attend to them get those values (whatever the weight: it is not 0).
             for (int e = 0; e < entries; ++e) {
@@ -275,7 +283,7 @@ __global__ __launch_bounds__(FEW_THREADS, 2) void beam_attn_kernel(TreeArgs a) {
             sum = 0.0f;
             v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        const int64_t to = (int64_t)(beam0 + of) * a.H + (kvh << a.g_shift) + (r & (g - 1));
+        const int64_t to = (int64_t)(beam0 + of) * a.H + (kvh << a.g_shift) + ((row0 + r) & (g - 1));
         if (s.chunk >= s.all) {
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
             const u32x2 w = {(uint32_t)f32_to_bf16_rne(v[0] * inv) | (uint32_t)f32_to_bf16_rne(v[1] * inv) << 16, (uint32_t)f32_to_bf16_rne(v[2] * inv) | (uint32_t)f32_to_bf16_rne(v[3] * inv) << 16};

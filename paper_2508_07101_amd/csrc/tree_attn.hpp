@@ -123,18 +123,57 @@ __device__ __forceinline__ int tree_piece(const TreeArgs& a, const TreeSpan& own
     piece = __builtin_amdgcn_readfirstlane(piece);
     return piece > 0 ? piece : most;                              // (0: more sequences than pieces would balance, which stay whole)
 }
-template <bool SPARSE, bool BEAM>
+template <bool SPARSE>
 __device__ __forceinline__ TreeSpan tree_work(const TreeArgs& a, int b) {
-    TreeSpan s = tree_span<SPARSE, BEAM>(a, b);
-    int piece = tree_piece<SPARSE, BEAM>(a, s);
+    TreeSpan s = tree_span<SPARSE, false>(a, b);
+    int piece = tree_piece<SPARSE, false>(a, s);
     if (a.n_splits == 1) {
         piece = tiles_of(s.all);
     } else {
-        piece = min(piece, (SPARSE ? TREE_LIST : (BEAM ? BEAM_LIST : TREE_LIST) * PAGE) / TREE_TILE);   // what a workgroup's list has room for
+        piece = min(piece, (SPARSE ? TREE_LIST : TREE_LIST * PAGE) / TREE_TILE);   // what a workgroup's list has room for
         piece = max(piece, (tiles_of(s.all) + a.n_splits - 1) / a.n_splits);       // what the launch has pieces for
     }
     s.chunk = piece * TREE_TILE;
     return s;
+}
+
+// The same for groups: unit u of a launch is a KV head and the u / G -th of all groups' pieces, one group after the other, so that all that have work come first.  (In order of the pieces' numbers, with
+// those that short groups do not have in between, workgroups waited for places while CUs of other shader engines had some: 8 samples of 8 prompts of 1024 to 2048 tokens, 488 pieces: 24 of the 256 CUs
+// had three, 48 one, and the last began after 146 of 242 us.)  False: there is no such piece.  A group without tokens has one.
+__device__ __forceinline__ bool group_work(const TreeArgs& a, int u, TreeSpan& s, int& b, int& kvh, int& split) {
+    const int G = a.cache.kv.G, v = u / G, lane = threadIdx.x & 63;
+    kvh = u - v * G;
+    split = 0;
+    if (a.n_splits == 1) {
+        b = v;
+        if (b >= a.batch) return false;
+        s = tree_span<false, true>(a, b);
+        s.chunk = tiles_of(s.all) * TREE_TILE;
+        return true;
+    }
+    if (a.batch == 1) s = tree_span<false, true>(a, 0);
+    const int piece = min(tree_piece<false, true>(a, s), BEAM_LIST * PAGE / TREE_TILE);   // (what a workgroup's list has room for)
+    for (int i0 = 0, before = 0; i0 < a.batch; i0 += 64) {
+        const int i = i0 + lane, t = i < a.batch ? tiles_of(tree_span<false, true>(a, i).all) : 0;
+        const int chunk = max(piece, (t + a.n_splits - 1) / a.n_splits), n = i < a.batch ? max((t + chunk - 1) / chunk, 1) : 0;   // (what the launch has pieces for)
+        int sum = n;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(sum, o);
+            if (lane >= o) sum += y;
+        }
+        const uint64_t behind = __ballot(before + sum > v);
+        if (behind) {
+            const int at = __builtin_ctzll(behind);
+            b = i0 + at;
+            split = v - before - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(n, at));
+            s = tree_span<false, true>(a, b);
+            s.chunk = __builtin_amdgcn_readlane(chunk, at) * TREE_TILE;
+            return true;
+        }
+        before += __builtin_amdgcn_readlane(sum, 63);
+    }
+    return false;
 }
 
 // Bits o .. o + 31 of a node's mask (o may be negative; bits before the first and behind the last are 0).
@@ -957,27 +996,40 @@ __global__ __launch_bounds__(TREE_THREADS, 2) void tree_attn_kernel(TreeArgs a) 
     // Workgroups go to the 8 XCDs in turn: those that share a KV head's tokens come 8 apart, to the same L2.  First pieces first: behind them come
     // those that short sequences do not have.
     const uint32_t turn = blockIdx.x >> 3, m_tile = turn % (uint32_t)a.m_tiles, unit = turn / (uint32_t)a.m_tiles * 8 + (blockIdx.x & 7);
-    const uint32_t G = a.cache.kv.G, pairs = G * (uint32_t)a.batch, pair = unit % pairs;
-    const int split = unit / pairs, b = pair / G, kvh = pair - b * G, row0 = m_tile * a.tile_rows;
-    if (split >= a.n_splits) return;
-    const TreeSpan s = tree_work<SPARSE, BEAM>(a, b);
-    const int left = min((s.n << a.g_shift) - row0, a.tile_rows), begin = split * s.chunk;
-    if (BEAM && s.all == 0 && split == 0) {                       // a group without tokens
-        for (int i = threadIdx.x; i < (left << 5); i += TREE_THREADS) {
-            const int row = row0 + (i >> 5);
-            const int64_t to = (int64_t)(s.start + (row >> a.g_shift)) * a.H + (kvh << a.g_shift) + (row & ((1 << a.g_shift) - 1));
-            *reinterpret_cast<u32x2*>(a.out + to * D + (i & 31) * 4) = u32x2{0, 0};
+    if constexpr (BEAM) {
+        TreeSpan s;
+        int b, kvh, split;
+        if (!group_work(a, (int)unit, s, b, kvh, split)) return;
+        const int row0 = m_tile * a.tile_rows, left = min((s.n << a.g_shift) - row0, a.tile_rows), begin = split * s.chunk, end = min(begin + s.chunk, s.all);
+        if (left <= 0) return;
+        if (s.all == 0) {                                         // a group without tokens
+            for (int i = threadIdx.x; i < (left << 5); i += TREE_THREADS) {
+                const int row = row0 + (i >> 5);
+                const int64_t to = (int64_t)(s.start + (row >> a.g_shift)) * a.H + (kvh << a.g_shift) + (row & ((1 << a.g_shift) - 1));
+                *reinterpret_cast<u32x2*>(a.out + to * D + (i & 31) * 4) = u32x2{0, 0};
+            }
         }
-        if (a.n_splits > 1 && kvh == 0 && m_tile == 0 && threadIdx.x == 0) a.pieces[b] = 0;
+        if (a.n_splits > 1 && split == 0 && kvh == 0 && m_tile == 0 && threadIdx.x == 0) a.pieces[b] = s.all ? (s.all + s.chunk - 1) / s.chunk : 0;
+        if (begin >= end) return;
+        if (left <= 32) tree_rows<1, PAGED, SPARSE, BEAM>(a, s, lds, b, kvh, row0, split, begin, end);
+        else if (left <= 64) tree_rows<2, PAGED, SPARSE, BEAM>(a, s, lds, b, kvh, row0, split, begin, end);
+        else if (left <= 128) tree_rows<4, PAGED, SPARSE, BEAM>(a, s, lds, b, kvh, row0, split, begin, end);
+        else tree_rows<8, PAGED, SPARSE, BEAM>(a, s, lds, b, kvh, row0, split, begin, end);
+    } else {
+        const uint32_t G = a.cache.kv.G, pairs = G * (uint32_t)a.batch, pair = unit % pairs;
+        const int split = unit / pairs, b = pair / G, kvh = pair - b * G, row0 = m_tile * a.tile_rows;
+        if (split >= a.n_splits) return;
+        const TreeSpan s = tree_work<SPARSE>(a, b);
+        const int left = min((s.n << a.g_shift) - row0, a.tile_rows), begin = split * s.chunk;
+        if (left <= 0 || begin >= s.all) return;
+        // (a piece has no more tokens or pages than the list has room for: plan_tree)
+        const int end = min(begin + s.chunk, s.all);
+        if (a.n_splits > 1 && split == 0 && kvh == 0 && m_tile == 0 && threadIdx.x == 0) a.pieces[b] = (s.all + s.chunk - 1) / s.chunk;
+        if (left <= 32) tree_rows<1, PAGED, SPARSE, BEAM>(a, s, lds, b, kvh, row0, split, begin, end);
+        else if (left <= 64) tree_rows<2, PAGED, SPARSE, BEAM>(a, s, lds, b, kvh, row0, split, begin, end);
+        else if (left <= 128) tree_rows<4, PAGED, SPARSE, BEAM>(a, s, lds, b, kvh, row0, split, begin, end);
+        else tree_rows<8, PAGED, SPARSE, BEAM>(a, s, lds, b, kvh, row0, split, begin, end);
     }
-    if (left <= 0 || begin >= s.all) return;
-    // (a piece has no more tokens or pages than the list has room for: plan_tree)
-    const int end = min(begin + s.chunk, s.all);
-    if (a.n_splits > 1 && split == 0 && kvh == 0 && m_tile == 0 && threadIdx.x == 0) a.pieces[b] = (s.all + s.chunk - 1) / s.chunk;
-    if (left <= 32) tree_rows<1, PAGED, SPARSE, BEAM>(a, s, lds, b, kvh, row0, split, begin, end);
-    else if (left <= 64) tree_rows<2, PAGED, SPARSE, BEAM>(a, s, lds, b, kvh, row0, split, begin, end);
-    else if (left <= 128) tree_rows<4, PAGED, SPARSE, BEAM>(a, s, lds, b, kvh, row0, split, begin, end);
-    else tree_rows<8, PAGED, SPARSE, BEAM>(a, s, lds, b, kvh, row0, split, begin, end);
 }
 
 // A wave for a row: a lane for each piece's weight, then two columns a lane.  Bound by the partial sums' way back from memory: 31 MB of one sequence (1920 rows in 32
