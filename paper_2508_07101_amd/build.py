@@ -10,7 +10,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libcusa.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("cusa.hip", "tree.hip", "beam.hip", "build_id.hip")]
-HEADERS = [os.path.join(CSRC, f) for f in ("attn_plan.hpp", "beam_attn.hpp", "beam_kernels.hpp", "cache_view.hpp", "call_tag.hpp", "cusa_kernels.hpp", "host.hpp", "plan_scan.hpp", "tree_attn.hpp", "tree_kernels.hpp",
+HEADERS = [os.path.join(CSRC, f) for f in ("attn_parts.hpp", "attn_plan.hpp", "beam_attn.hpp", "beam_kernels.hpp", "beam_plan.hpp", "cache_view.hpp", "call_tag.hpp", "cusa_kernels.hpp", "host.hpp", "plan_scan.hpp", "tree_kernels.hpp",
                                            "tree_plan.hpp")]
 HEADERS.append(os.path.join(os.path.dirname(_HERE), "include", "cusa.h"))
 

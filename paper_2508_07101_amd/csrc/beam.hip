@@ -79,8 +79,8 @@ cusa_status check_shared(const cusa_shared* s, int32_t batch, int32_t max_seq_le
     return s->max_entries < std::min<int64_t>(s->width * pages, n_pages) ? CUSA_ERR_INVALID_ARG : CUSA_OK;
 }
 
-// Tokens of a group's pages that a pass may have to look at.
-int64_t group_len(const cusa_shared* s, int32_t max_seq_len) { return std::min<int64_t>(s->max_entries, s->width * (((int64_t)max_seq_len + PAGE - 1) / PAGE)) * PAGE; }
+// Pages of a group that a pass may have to look at.
+int64_t group_pages(const cusa_shared* s, int32_t max_seq_len) { return std::min<int64_t>(s->max_entries, s->width * (((int64_t)max_seq_len + PAGE - 1) / PAGE)); }
 
 }  // namespace
 
@@ -244,10 +244,10 @@ cusa_status cusa_beam_attn_workspace_bytes(const cusa_params* params, int32_t ma
     if (st != CUSA_OK) return st;
     if (!bytes || max_seq_len < 1 || !shared || shared->max_entries < 1) return CUSA_ERR_INVALID_ARG;
     if ((st = check_group(params->batch, shared->width)) != CUSA_OK) return st;
-    const int64_t len = group_len(shared, max_seq_len);
-    if (!tree_len_served(TREE_GROUP, len)) return CUSA_ERR_UNSUPPORTED;
-    const int groups = params->batch / shared->width;
-    *bytes = std::max<size_t>(256, tree_workspace(TREE_GROUP, (int)len, groups, params->n_q_heads, params->n_kv_heads, params->batch, shared->width).total);
+    const int64_t pages = group_pages(shared, max_seq_len);
+    if (!beam_pages_served(pages)) return CUSA_ERR_UNSUPPORTED;
+    const int groups = params->batch / shared->width, g = params->n_q_heads / params->n_kv_heads;
+    *bytes = beam_attn_workspace(plan_beams(pages, groups, params->n_kv_heads, shared->width * g), params->batch, params->n_q_heads, groups).total;
     return CUSA_OK;
 }
 
@@ -262,46 +262,40 @@ cusa_status cusa_beam_attn(const cusa_params* params, const void* q, int64_t q_s
     if (!q || !out || ((uintptr_t)q & 15) || ((uintptr_t)out & 15) || q_stride < (int64_t)params->n_q_heads * D || (q_stride & 7)) return CUSA_ERR_INVALID_ARG;
     if ((st = check_shared(shared, params->batch, kv->max_seq_len, kv->n_pages)) != CUSA_OK) return st;
     const int g = params->n_q_heads / params->n_kv_heads, G = params->n_kv_heads, width = shared->width, groups = params->batch / width;
-    const int64_t len = group_len(shared, kv->max_seq_len);
-    if (!tree_len_served(TREE_GROUP, len)) return CUSA_ERR_UNSUPPORTED;
-    const TreeWs w = tree_workspace(TREE_GROUP, (int)len, groups, params->n_q_heads, G, params->batch, width);
+    const int64_t pages = group_pages(shared, kv->max_seq_len);
+    if (!beam_pages_served(pages)) return CUSA_ERR_UNSUPPORTED;
+    const BeamPlan pl = plan_beams(pages, groups, G, width * g);
+    const BeamAttnWs w = beam_attn_workspace(pl, params->batch, params->n_q_heads, groups);
     if ((st = check_workspace(ws, ws_bytes, w.total)) != CUSA_OK) return st;
-    const bool few = width * g <= FEW_ROWS;
-    const TreePlan pl = few ? plan_few((int)len, groups, G) : plan_tree(TREE_GROUP, (int)len, groups, G, g, width);
-    TreeArgs a = {};
+    BeamAttnArgs a = {};
     a.cache = cache_args(params, kv);
     a.q = static_cast<const uint16_t*>(q);
     a.q_stride = q_stride;
     a.entries = shared->entries;
     a.count = shared->count;
-    a.max_entries = (int32_t)(len / PAGE);
     a.entry_stride = shared->max_entries;
+    a.max_entries = (int32_t)pages;
     a.out = static_cast<uint16_t*>(out);
     a.part_acc = ws_ptr<float>(ws, w.acc);
     a.part_ml = ws_ptr<float>(ws, w.ml);
     a.pieces = ws_ptr<int32_t>(ws, w.pieces);
     a.scale_log2e = params->sm_scale * 1.4426950408889634f;
-    a.max_nodes = width;
+    a.groups = groups;
+    a.width = width;
     a.H = params->n_q_heads;
     a.g_shift = g == 1 ? 0 : g == 2 ? 1 : g == 4 ? 2 : 3;
-    a.tile_rows = pl.rows;
-    a.m_tiles = pl.m_tiles;
+    a.blocks = pl.blocks;
     a.n_splits = pl.n_splits;
-    a.batch = groups;
-    const int64_t units = ((int64_t)pl.n_splits * G * groups + 7) / 8 * 8 * pl.m_tiles;
+    const int64_t units = ((int64_t)pl.n_splits * G * groups + 7) / 8 * 8 * pl.blocks;
     if (units > 0x7fffffff) return CUSA_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)units);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (few) {
-        const dim3 grid((unsigned)units);
-        if (width * g <= 16) launch(KID_BEAM_ATTN, beam_attn_kernel<1>, grid, FEW_THREADS, 0, s, a);
-        else launch(KID_BEAM_ATTN, beam_attn_kernel<2>, grid, FEW_THREADS, 0, s, a);
-    } else {
-        launch(KID_BEAM_ATTN, tree_attn_kernel<true, false, true>, dim3((unsigned)units), TREE_THREADS, 0, s, a);
-    }
+    if (width * g <= 16) launch(KID_BEAM_ATTN, beam_attn_kernel<1>, grid, BEAM_ATTN_THREADS, 0, s, a);
+    else launch(KID_BEAM_ATTN, beam_attn_kernel<2>, grid, BEAM_ATTN_THREADS, 0, s, a);
     if (launch_status() != CUSA_OK) return CUSA_ERR_LAUNCH;
     if (pl.n_splits > 1) {                 // as many workgroups as have a row each, but not more than a few rounds of the chip
-        const int64_t rows = ((int64_t)width * params->n_q_heads + REDUCE_WAVES - 1) / REDUCE_WAVES, most = std::max(1, 8192 / groups);
-        launch(KID_BEAM_REDUCE, tree_reduce_kernel<true>, dim3((unsigned)std::min(rows, most), (unsigned)groups), 64 * REDUCE_WAVES, 0, s, a);
+        const int64_t rows = ((int64_t)width * params->n_q_heads + BEAM_REDUCE_WAVES - 1) / BEAM_REDUCE_WAVES, most = std::max(1, 8192 / groups);
+        launch(KID_BEAM_REDUCE, beam_reduce_kernel, dim3((unsigned)std::min(rows, most), (unsigned)groups), 64 * BEAM_REDUCE_WAVES, 0, s, a);
     }
     return launch_status();
 }

@@ -1,31 +1,129 @@
-// Attention over a group's pages where a KV head has few queries: up to 16 or 32 rows (row of the group, query head).
-//
-// What it does for more of them, tree_attn_kernel's form for groups, needs 160 KB of LDS and eight waves that meet; here a workgroup is four waves that go their own ways until their sums
-// come together, two or more of them share a CU, and nothing but V passes through LDS.
+// Attention over a group's pages: each is read once for all rows of the group that hold it.
 #pragma once
-#include "tree_attn.hpp"
+#include "attn_parts.hpp"
+#include "beam_plan.hpp"
+#include "plan_scan.hpp"
 
 namespace cusa {
 
-constexpr int FEW_WAVES = 4, FEW_THREADS = 64 * FEW_WAVES;
+constexpr int BEAM_ATTN_WAVES = 4, BEAM_ATTN_THREADS = 64 * BEAM_ATTN_WAVES;
+constexpr int BEAM_TILE = 32;              // tokens of a tile, two pages: pieces are whole tiles
+constexpr int BEAM_TILE_BYTES = BEAM_TILE * 256;
+
+struct BeamAttnArgs {
+    CacheArgs cache;
+    const uint16_t* q;
+    int64_t q_stride;
+    const int32_t *entries, *count;
+    int64_t entry_stride;                  // entries of a group's list, and of these the ones that are looked at
+    int32_t max_entries;
+    uint16_t* out;
+    float *part_acc, *part_ml;
+    int32_t* pieces;                       // of each group's pages, for the merge
+    float scale_log2e;
+    int32_t groups, width, H, g_shift, blocks, n_splits;
+};
+
+struct BeamSpan {
+    int b, kvh, split;                     // the group, the KV head, the piece
+    int pre, all;                          // tokens of pages that every row attends to as a whole (the first ones), of all pages
+    int chunk;                             // tokens of a piece
+};
+__device__ __forceinline__ int tiles_of_group(const BeamAttnArgs& a, int b) { return (clampi(a.count[b * 2], 0, a.max_entries) + 1) / 2; }
+
+// The pieces are of one length, which goes by the lists that there are.  With the tiles T of all workgroups' rows and KV heads, W of these in number and at most M tiles in one, pieces of
+// ceil(M / floor(R / W)) tiles are R at most, and so are pieces of T / (R - W) tiles (a last piece each is shorter): the first is exact for lists of one length, the second close for any.
+// R: one to eight workgroups for each CU; more are better balanced, but each costs about BEAM_PIECE_COST tiles besides its own (its start, and partial sums written and read).  0: more groups than
+// pieces would balance, which stay whole.
+__device__ __forceinline__ int group_piece(const BeamAttnArgs& a) {
+    const int lane = threadIdx.x & 63;
+    int total = 0, most = 0;
+    for (int i = lane; i < a.groups; i += 64) {
+        const int t = tiles_of_group(a, i);
+        total += t;
+        most = max(most, t);
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        total += __shfl_xor(total, o);
+        most = max(most, __shfl_xor(most, o));
+    }
+    const int of_group = a.cache.kv.G * a.blocks, pairs = of_group * a.groups, r = (lane & 7) + 1, wgs = r * BEAM_CUS;   // a lane for each R (the others repeat them)
+    int cost = 0x7fffffff, piece = 0;
+    if (wgs >= pairs) {
+        piece = (most + wgs / pairs - 1) / (wgs / pairs);
+        if (wgs > pairs) piece = min(piece, (int)(((int64_t)total * of_group + wgs - pairs - 1) / (wgs - pairs)));
+        piece = max(piece, BEAM_MIN_PIECE / BEAM_TILE);
+        cost = r * (piece + BEAM_PIECE_COST);
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+        const int other_cost = __shfl_xor(cost, o), other_piece = __shfl_xor(piece, o);
+        if (other_cost < cost || (other_cost == cost && other_piece > piece)) {
+            cost = other_cost;
+            piece = other_piece;
+        }
+    }
+    piece = __builtin_amdgcn_readfirstlane(piece);
+    return piece > 0 ? piece : __builtin_amdgcn_readfirstlane(most);
+}
+// Unit u of a launch is a KV head and the u / G -th of all groups' pieces, one group after the other, so that all that have work come first.  (In order of the pieces' numbers, with
+// those that short groups do not have in between, workgroups waited for places while CUs of other shader engines had some: 8 samples of 8 prompts of 1024 to 2048 tokens, 488 pieces: 24 of the 256 CUs
+// had three, 48 one, and the last began after 146 of 242 us; so 195.)  False: there is no such piece.  A group without tokens has one.
+__device__ __forceinline__ bool group_work(const BeamAttnArgs& a, int u, BeamSpan& s) {
+    const int G = a.cache.kv.G, v = u / G, lane = threadIdx.x & 63;
+    s.kvh = u - v * G;
+    s.b = a.n_splits == 1 ? v : a.groups;
+    s.split = 0;
+    int tiles = 0;                                         // of a piece
+    if (a.n_splits > 1) {
+        const int piece = min(group_piece(a), BEAM_LIST / 2);   // (LDS has bits for BEAM_LIST pages)
+        for (int i0 = 0, before = 0; i0 < a.groups; i0 += 64) {
+            const int i = i0 + lane, t = i < a.groups ? tiles_of_group(a, i) : 0;
+            const int chunk = max(piece, (t + a.n_splits - 1) / a.n_splits), n = i < a.groups ? max((t + chunk - 1) / chunk, 1) : 0;   // (what the launch has pieces for)
+            int sum = n;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int y = __shfl_up(sum, o);
+                if (lane >= o) sum += y;
+            }
+            const uint64_t behind = __ballot(before + sum > v);
+            if (behind) {
+                const int at = __builtin_ctzll(behind);
+                s.b = i0 + at;
+                s.split = v - before - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(n, at));
+                tiles = __builtin_amdgcn_readlane(chunk, at);
+                break;
+            }
+            before += __builtin_amdgcn_readlane(sum, 63);
+        }
+    }
+    if (s.b >= a.groups) return false;
+    const int n = clampi(a.count[s.b * 2], 0, a.max_entries);
+    s.all = n * PAGE;
+    s.pre = clampi(a.count[s.b * 2 + 1], 0, n) * PAGE;
+    s.chunk = a.n_splits > 1 ? tiles * BEAM_TILE : (n + 1) / 2 * BEAM_TILE;
+    return true;
+}
 
 template <int NB>                          // blocks of 16 rows
-struct FewLds {
-    __attribute__((aligned(16))) unsigned char v[FEW_WAVES][2][TREE_TILE * 256];   // V of a tile, and of the next one; the waves' sums at the end
-    float m[FEW_WAVES][16 * NB], l[FEW_WAVES][16 * NB];
+struct BeamAttnLds {
+    __attribute__((aligned(16))) unsigned char v[BEAM_ATTN_WAVES * 2 * BEAM_TILE_BYTES];   // V of a wave's tile, and of the next one; the waves' sums at the end
+    float m[BEAM_ATTN_WAVES * 16 * NB], l[BEAM_ATTN_WAVES * 16 * NB];
     uint32_t odd[BEAM_LIST / 32];          // pages with a value that is not finite and that not all rows attend to
     int32_t any_odd;
 };
+static_assert(BEAM_LIST / 32 == BEAM_ATTN_THREADS, "a thread clears a word");
 
 // A tile: two pages of the list, uniform.
-struct FewTile {
+struct BeamTile {
     int64_t at[2];                         // elements in front of the KV head's rows
     int32_t first[2];                      // position of the page's first token
     uint32_t holders[2];
 };
-__device__ __forceinline__ FewTile few_tile(const TreeArgs& a, const int32_t* list, int e, int n, int kvh) {
+__device__ __forceinline__ BeamTile beam_tile(const BeamAttnArgs& a, const int32_t* list, int e, int n, int kvh) {
     typedef const __attribute__((address_space(4))) i32x4* uniform_entry;   // (no kernel of the launch writes the list)
-    FewTile t;
+    BeamTile t;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const i32x4 x = *(uniform_entry)(uintptr_t)(list + (int64_t)min(e + j, n - 1) * 4);
@@ -48,42 +146,25 @@ __device__ __forceinline__ float of_row_max(float v) {      // over the four lan
 // Weights are two bf16 numbers each, as in tree_rows for few rows.  The reference m follows the maximum when that is 2^8 above it.
 // K goes to registers, V to LDS, both for the next tile as soon as this one's scores are there; eight waves on a CU have 128 KB under way.
 template <int NB>
-__global__ __launch_bounds__(FEW_THREADS, 2) void beam_attn_kernel(TreeArgs a) {
-    __shared__ FewLds<NB> lds;
-    // Workgroups go to the 8 XCDs in turn: those of one KV head's pages come 8 apart, to the same L2.
-    const uint32_t turn = blockIdx.x >> 3, block = turn % (uint32_t)a.m_tiles, unit = turn / (uint32_t)a.m_tiles * 8 + (blockIdx.x & 7);
-    TreeSpan s;
-    int b, kvh, split;
-    if (!group_work(a, (int)unit, s, b, kvh, split)) return;
-    const int row0 = block * (16 * NB);
+__device__ __forceinline__ void beam_rows(const BeamAttnArgs& a, const BeamSpan& s, BeamAttnLds<NB>& lds, int row0) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, q4 = lane >> 4;
-    const int g = 1 << a.g_shift, all_rows = a.max_nodes << a.g_shift, rows = min(all_rows - row0, 16 * NB), beam0 = b * a.max_nodes;
+    const int g = 1 << a.g_shift, rows = min((a.width << a.g_shift) - row0, 16 * NB), beam0 = s.b * a.width, begin = s.split * s.chunk;
     u32x4 qv[NB][4];
     int len[NB];
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
         const int row = row0 + min(i * 16 + n, rows - 1), beam = beam0 + (row >> a.g_shift);
-        const uint16_t* const p = a.q + (int64_t)beam * a.q_stride + ((kvh << a.g_shift) + (row & (g - 1))) * D + q4 * 8;
+        const uint16_t* const p = a.q + (int64_t)beam * a.q_stride + ((s.kvh << a.g_shift) + (row & (g - 1))) * D + q4 * 8;
 #pragma unroll
         for (int k = 0; k < 4; ++k) qv[i][k] = *reinterpret_cast<const u32x4*>(p + k * 32);
         len[i] = a.cache.kv.seq_lens[beam];
     }
-    if (tid < BEAM_LIST / 32) lds.odd[tid] = 0;
+    lds.odd[tid] = 0;
     if (tid == 0) lds.any_odd = 0;
-    if (s.all == 0) {                        // a group without tokens
-        for (int i = tid; i < rows * (D / 4); i += FEW_THREADS) {
-            const int row = row0 + (i >> 5);
-            *reinterpret_cast<u32x2*>(a.out + ((int64_t)(beam0 + (row >> a.g_shift)) * a.H + (kvh << a.g_shift) + (row & (g - 1))) * D + (i & 31) * 4) = u32x2{0, 0};
-        }
-        if (a.n_splits > 1 && kvh == 0 && block == 0 && tid == 0) a.pieces[b] = 0;
-        return;
-    }
-    const int begin = split * s.chunk;
     __syncthreads();                                       // (odd is clear before anyone marks a page)
-    if (a.n_splits > 1 && split == 0 && kvh == 0 && block == 0 && tid == 0) a.pieces[b] = (s.all + s.chunk - 1) / s.chunk;
     const int entries = (min(begin + s.chunk, s.all) - begin) / PAGE, tiles = (entries + 1) >> 1;
-    const int plain = clampi(s.pre - begin, 0, entries * PAGE) / TREE_TILE;   // tiles that every row attends to as a whole: the first ones
-    const int32_t* const list = a.entries + (b * a.entry_stride + begin / PAGE) * 4;
+    const int plain = clampi(s.pre - begin, 0, entries * PAGE) / BEAM_TILE;   // tiles that every row attends to as a whole: the first ones
+    const int32_t* const list = a.entries + (s.b * a.entry_stride + begin / PAGE) * 4;
 
     bf16x8 qf[NB][4];
     f32x4 o[NB][8];
@@ -99,12 +180,12 @@ __global__ __launch_bounds__(FEW_THREADS, 2) void beam_attn_kernel(TreeArgs a) {
         l[i] = 0.0f;
         len[i] = there ? clampi(len[i], 0, a.cache.max_len) : 0;
     }
-    const uint32_t vlds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)&lds.v[wave][0][0];
+    const uint32_t vlds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds.v + wave * (2 * BEAM_TILE_BYTES);
     // A lane's part of K's operand; of V's rows as LDS holds them: 16-byte chunk c of token t stands at c ^ 4 (t % 4), so that the transposing reads of 16 lanes meet in no bank.
     const int k_part = n * D + q4 * 8, v_part = q4 * D + ((n ^ (q4 << 2)) << 3);
     const uint32_t v_read = (4 * q4 + ((lane >> 2) & 3)) * 256 + (((lane & 3) >> 1) << 4) + (lane & 1) * 8;
     u32x4 k[2][4];
-    auto request = [&](const FewTile& t, int buffer) {
+    auto request = [&](const BeamTile& t, int buffer) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const uint16_t* const kp = a.cache.kv.k + t.at[j];
@@ -114,23 +195,23 @@ __global__ __launch_bounds__(FEW_THREADS, 2) void beam_attn_kernel(TreeArgs a) {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) load_to_lds(a.cache.kv.v + t.at[j], (uint32_t)(v_part + i * 4 * D) * 2, vlds + buffer * (TREE_TILE * 256) + j * (PAGE * 256) + i * 1024);
+            for (int i = 0; i < 4; ++i) load_to_lds(a.cache.kv.v + t.at[j], (uint32_t)(v_part + i * 4 * D) * 2, vlds + buffer * BEAM_TILE_BYTES + j * (PAGE * 256) + i * 1024);
     };
     // The first tile from t on that one of this workgroup's rows attends to.
     const uint32_t here = (uint32_t)((1ull << (((row0 + rows - 1) >> a.g_shift) + 1)) - (1ull << (row0 >> a.g_shift)));
-    auto find = [&](int t, FewTile& tile) {
-        for (; t < tiles; t += FEW_WAVES) {
-            tile = few_tile(a, list, t * 2, entries, kvh);
+    auto find = [&](int t, BeamTile& tile) {
+        for (; t < tiles; t += BEAM_ATTN_WAVES) {
+            tile = beam_tile(a, list, t * 2, entries, s.kvh);
             if ((tile.holders[0] | tile.holders[1]) & here) break;
         }
         return t;
     };
-    FewTile now, next;
+    BeamTile now, next;
     int t = find(wave, now), buffer = 0;
     if (t < tiles) request(now, 0);
 #pragma unroll 1
     for (int t_next; t < tiles; t = t_next, buffer ^= 1) {
-        t_next = find(t + FEW_WAVES, next);
+        t_next = find(t + BEAM_ATTN_WAVES, next);
         const bool more = t_next < tiles;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // K in registers, V in LDS
         f32x4 x[NB][2];
@@ -168,7 +249,7 @@ __global__ __launch_bounds__(FEW_THREADS, 2) void beam_attn_kernel(TreeArgs a) {
             }
             typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-            for (int c = 0; c < 8; c += 2) {               // (as weigh for TreeFineWeights)
+            for (int c = 0; c < 8; c += 2) {               // (f: cut to bf16, less one step; the rest a step to two, rounded: neither is negative or, from 2^-132 on, 0, so that an infinite value stays so in both products)
                 const float w0 = weight(m[i], x[i][c >> 2][c & 3], a.scale_log2e), w1 = weight(m[i], x[i][c >> 2][(c & 3) + 1], a.scale_log2e);
                 const uint32_t cut = __builtin_amdgcn_perm(__float_as_uint(w1), __float_as_uint(w0), 0x07060302);
                 const uint32_t less = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, cut), u16x2{1, 1}));
@@ -182,7 +263,7 @@ __global__ __launch_bounds__(FEW_THREADS, 2) void beam_attn_kernel(TreeArgs a) {
             }
         }
         u32x4 v[8];
-        const uint32_t from = vlds + buffer * (TREE_TILE * 256) + v_read, turn = ((lane >> 2) & 3) << 6;
+        const uint32_t from = vlds + buffer * BEAM_TILE_BYTES + v_read, turn = ((lane >> 2) & 3) << 6;
 #pragma unroll
         for (int d = 0; d < 8; ++d) {
             const uint32_t at = from + ((((d >> 1) << 6) ^ turn) | (d & 1) << 5);
@@ -230,43 +311,42 @@ __global__ __launch_bounds__(FEW_THREADS, 2) void beam_attn_kernel(TreeArgs a) {
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         if (q4 == 0) {
-            lds.m[wave][i * 16 + n] = m[i];
-            lds.l[wave][i * 16 + n] = sum;
+            lds.m[(wave * NB + i) * 16 + n] = m[i];
+            lds.l[(wave * NB + i) * 16 + n] = sum;
         }
     }
     __syncthreads();
-    unsigned char* const sums = &lds.v[0][0][0];
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
         const int r = i * 16 + n;
-        float top = lds.m[0][r];
+        float top = lds.m[r];
 #pragma unroll
-        for (int w = 1; w < FEW_WAVES; ++w) top = fmaxf(top, lds.m[w][r]);
+        for (int w = 1; w < BEAM_ATTN_WAVES; ++w) top = fmaxf(top, lds.m[w * 16 * NB + r]);
         const float f = exp2f(m[i] - top);
 #pragma unroll
         for (int d = 0; d < 8; ++d)                        // columns 16 d + 4 q ..
-            *reinterpret_cast<f32x4*>(sums + (wave * 16 * NB + r) * (D * 4) + (((4 * d + q4) ^ n) << 4)) = f32x4{o[i][d][0] * f, o[i][d][1] * f, o[i][d][2] * f, o[i][d][3] * f};
+            *reinterpret_cast<f32x4*>(lds.v + (wave * 16 * NB + r) * (D * 4) + (((4 * d + q4) ^ n) << 4)) = f32x4{o[i][d][0] * f, o[i][d][1] * f, o[i][d][2] * f, o[i][d][3] * f};
     }
     __syncthreads();
-    const bool any_odd = lds.any_odd != 0;
+    const bool some_odd = lds.any_odd != 0;
     const int c = tid & 31;
 #pragma unroll 1
-    for (int r = tid >> 5; r < rows; r += FEW_THREADS / 32) {
-        float top = lds.m[0][r], sum = 0.0f;
+    for (int r = tid >> 5; r < rows; r += BEAM_ATTN_WAVES * 2) {
+        float top = lds.m[r], sum = 0.0f;
 #pragma unroll
-        for (int w = 1; w < FEW_WAVES; ++w) top = fmaxf(top, lds.m[w][r]);
+        for (int w = 1; w < BEAM_ATTN_WAVES; ++w) top = fmaxf(top, lds.m[w * 16 * NB + r]);
         f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int w = 0; w < FEW_WAVES; ++w) {
-            sum += lds.l[w][r] * exp2f(lds.m[w][r] - top);
-            v += *reinterpret_cast<const f32x4*>(sums + (w * 16 * NB + r) * (D * 4) + ((c ^ (r & 15)) << 4));
+        for (int w = 0; w < BEAM_ATTN_WAVES; ++w) {
+            sum += lds.l[w * 16 * NB + r] * exp2f(lds.m[w * 16 * NB + r] - top);
+            v += *reinterpret_cast<const f32x4*>(lds.v + (w * 16 * NB + r) * (D * 4) + ((c ^ (r & 15)) << 4));
         }
         const int of = (row0 + r) >> a.g_shift, length = clampi(a.cache.kv.seq_lens[beam0 + of], 0, a.cache.max_len);
-        if (any_odd) {
+        if (some_odd) {
             // Pages with values that are not finite: the rows that attend to them get those values (whatever the weight: it is not 0).
             for (int e = 0; e < entries; ++e) {
                 if (!(lds.odd[e >> 5] >> (e & 31) & 1)) continue;
-                const FewTile t = few_tile(a, list, e, entries, kvh);
+                const BeamTile t = beam_tile(a, list, e, entries, s.kvh);
                 if (!(t.holders[0] >> of & 1)) continue;
                 for (int j = 0; j < min(length - t.first[0], PAGE); ++j) {
                     const u32x2 w = *reinterpret_cast<const u32x2*>(a.cache.kv.v + t.at[0] + j * D + c * 4);
@@ -283,16 +363,46 @@ __global__ __launch_bounds__(FEW_THREADS, 2) void beam_attn_kernel(TreeArgs a) {
             sum = 0.0f;
             v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        const int64_t to = (int64_t)(beam0 + of) * a.H + (kvh << a.g_shift) + ((row0 + r) & (g - 1));
+        const int64_t to = (int64_t)(beam0 + of) * a.H + (s.kvh << a.g_shift) + ((row0 + r) & (g - 1));
         if (s.chunk >= s.all) {
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
             const u32x2 w = {(uint32_t)f32_to_bf16_rne(v[0] * inv) | (uint32_t)f32_to_bf16_rne(v[1] * inv) << 16, (uint32_t)f32_to_bf16_rne(v[2] * inv) | (uint32_t)f32_to_bf16_rne(v[3] * inv) << 16};
             *reinterpret_cast<u32x2*>(a.out + to * D + c * 4) = w;
         } else {
-            const int64_t piece = to * a.n_splits + split;
+            const int64_t piece = to * a.n_splits + s.split;
             *reinterpret_cast<f32x4*>(a.part_acc + piece * D + c * 4) = v;
             if (c == 0) *reinterpret_cast<f32x2*>(a.part_ml + piece * 2) = f32x2{top, sum};
         }
+    }
+}
+
+template <int NB>
+__global__ __launch_bounds__(BEAM_ATTN_THREADS, 2) void beam_attn_kernel(BeamAttnArgs a) {
+    __shared__ BeamAttnLds<NB> lds;
+    // Blocks of rows that share a KV head's pages: workgroups go to the 8 XCDs in turn, and theirs come 8 apart, to the same L2.
+    const uint32_t turn = blockIdx.x >> 3, block = turn % (uint32_t)a.blocks, unit = turn / (uint32_t)a.blocks * 8 + (blockIdx.x & 7);
+    BeamSpan s;
+    if (!group_work(a, (int)unit, s)) return;
+    const int row0 = block * (16 * NB), rows = min((a.width << a.g_shift) - row0, 16 * NB);
+    if (a.n_splits > 1 && s.split == 0 && s.kvh == 0 && block == 0 && threadIdx.x == 0) a.pieces[s.b] = s.all ? (s.all + s.chunk - 1) / s.chunk : 0;
+    if (s.all > 0) {
+        beam_rows<NB>(a, s, lds, row0);
+        return;
+    }
+    for (int i = threadIdx.x; i < rows * (D / 4); i += BEAM_ATTN_THREADS) {   // a group without tokens
+        const int row = row0 + (i >> 5);
+        *reinterpret_cast<u32x2*>(a.out + ((int64_t)(s.b * a.width + (row >> a.g_shift)) * a.H + (s.kvh << a.g_shift) + (row & ((1 << a.g_shift) - 1))) * D + (i & 31) * 4) = u32x2{0, 0};
+    }
+}
+
+// A wave for a row.
+constexpr int BEAM_REDUCE_WAVES = 4;
+__global__ __launch_bounds__(64 * BEAM_REDUCE_WAVES) void beam_reduce_kernel(BeamAttnArgs a) {
+    const int b = blockIdx.y, pieces = a.pieces[b];
+    if (pieces <= 1) return;
+    for (int r = blockIdx.x * BEAM_REDUCE_WAVES + (threadIdx.x >> 6); r < a.width * a.H; r += gridDim.x * BEAM_REDUCE_WAVES) {
+        const int64_t row = (int64_t)b * a.width * a.H + r, first = row * a.n_splits;
+        merge_pieces(a.part_acc + first * D, a.part_ml + first * 2, pieces, a.out + row * D, threadIdx.x & 63);
     }
 }
 

@@ -1,4 +1,4 @@
-// Device code for beam search over paged caches: groups of rows that share pages.  (Attention over a group's pages is a form of tree_attn_kernel.)
+// Device code for beam search over paged caches: groups of rows that share pages.  (Attention over a group's pages: beam_attn.hpp.)
 //
 //   beam_rows_kernel     the best tokens of each row and the sum of its weights
 //   beam_merge_kernel    the best of a group's rows

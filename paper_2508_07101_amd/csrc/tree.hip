@@ -158,7 +158,7 @@ cusa_status cusa_tree_attn(const cusa_params* params, const void* q, const cusa_
     const TreeWs w = tree_workspace(kind, (int)len, params->batch, params->n_q_heads, G, tree->max_tokens, tree->max_nodes);
     if (ws_bytes < w.total) return CUSA_ERR_WORKSPACE_TOO_SMALL;
     const TreePlan pl = plan_tree(kind, (int)len, params->batch, G, g, tree->max_nodes);
-    TreeArgs a = {};
+    TreeArgs a;
     a.cache = cache_args(params, kv);
     a.q = static_cast<const uint16_t*>(q);
     a.q_stride = tree->q_stride;
@@ -190,7 +190,7 @@ cusa_status cusa_tree_attn(const cusa_params* params, const void* q, const cusa_
     if (launch_status() != CUSA_OK) return CUSA_ERR_LAUNCH;
     if (pl.n_splits > 1) {                 // as many workgroups as have a row each, but not more than a few rounds of the chip
         const int64_t rows = ((int64_t)tree->max_nodes * params->n_q_heads + REDUCE_WAVES - 1) / REDUCE_WAVES, most = std::max(1, 8192 / params->batch);
-        launch(KID_TREE_REDUCE, tree_reduce_kernel<>, dim3((unsigned)std::min(rows, most), params->batch), 64 * REDUCE_WAVES, 0, s, a);
+        launch(KID_TREE_REDUCE, tree_reduce_kernel, dim3((unsigned)std::min(rows, most), params->batch), 64 * REDUCE_WAVES, 0, s, a);
     }
     return launch_status();
 }

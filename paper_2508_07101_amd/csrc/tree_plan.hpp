@@ -17,9 +17,8 @@ constexpr int TREE_ROWS = 256;          // rows (node, query head) of one KV hea
 
 // Entries of a workgroup's list of cache rows: tokens of a chosen prefix, pages of 16 of a whole one.
 constexpr int TREE_LIST = 5120;
-constexpr int BEAM_LIST = 2304;         // pages of a group, with their columns and the rows that hold them
-enum TreeKind { TREE_FULL, TREE_CHOSEN, TREE_GROUP /* tokens: those of a group's pages */ };
-inline int tree_piece_most(TreeKind kind) { return kind == TREE_CHOSEN ? TREE_LIST : (kind == TREE_GROUP ? BEAM_LIST : TREE_LIST) * 16; }
+enum TreeKind { TREE_FULL, TREE_CHOSEN };
+inline int tree_piece_most(TreeKind kind) { return kind == TREE_CHOSEN ? TREE_LIST : TREE_LIST * 16; }
 inline bool tree_len_served(TreeKind kind, int64_t len) { return len <= (int64_t)tree_piece_most(kind) * TREE_MAX_SPLITS; }
 
 // Tokens up to which sequences stay whole: what a workgroup of up to 64 rows takes in three steps (its teams take 256 or 128 tokens a step), which is less than the
@@ -69,21 +68,6 @@ inline TreePlan plan_tree(TreeKind kind, int max_len, int batch, int G, int g, i
     return p;
 }
 
-// The same for groups whose rows of a KV head are few (beam_attn_kernel: four waves, steps of 128 tokens, two workgroups on a CU).  The host knows no more than width * max_seq_len tokens, of which
-// rows that share have a fraction: a group stays whole up to a bound that costs little if they share nothing (4 beams of one group, 8 KV heads: 1000 tokens whole 14.2 us, cut and merged 14.4;
-// 700: 10.8 and 12.4; 1550: 17.7 and 14.8), a higher one where half of the CUs have a workgroup anyway (16 groups of 4 beams: 600 tokens, bound 2600, whole 13.2, cut 16.5; 1000, bound 4100, 17.1 and 19.9).
-// There is room for twice as many pieces as for trees; the kernel makes as many as balance 256 workgroups (512: the serving batch 948 us, so 968; 64 samples 176 and 191).
-constexpr int FEW_ROWS = 32;
-constexpr int FEW_WHOLE = 2048, FEW_WHOLE_MANY = 4096;   // tokens
-inline TreePlan plan_few(int max_len, int groups, int G) {
-    const int64_t pairs = (int64_t)groups * G;
-    const int64_t want = groups == 1 ? 2 * TREE_CUS / pairs : pairs >= 16 * TREE_CUS ? 1 : std::max<int64_t>(4, 4 * TREE_CUS / pairs);
-    const int64_t by_list = ((int64_t)max_len + tree_piece_most(TREE_GROUP) - 1) / tree_piece_most(TREE_GROUP);
-    const int64_t least = pairs >= 2 * TREE_CUS ? 4096 : TREE_MIN_PIECE;   // (where all have a workgroup already, pieces only make up for lengths)
-    const int64_t pieces = max_len <= (pairs >= TREE_CUS / 2 ? FEW_WHOLE_MANY : FEW_WHOLE) ? 1 : (max_len + least - 1) / least;
-    return {FEW_ROWS, 1, (int)std::max<int64_t>({1, by_list, std::min<int64_t>({want, pieces, TREE_MAX_SPLITS})})};
-}
-
 // Bytes of partial results: 128 sums, a maximum and a denominator per row and piece.  Trees of fewer nodes may be cut into more
 // pieces, but have fewer rows: the bound is over all of them, so that a workspace serves every smaller batch of tokens as well.
 struct TreeWs {
@@ -94,7 +78,7 @@ inline TreeWs tree_workspace(TreeKind kind, int max_len, int batch, int H, int G
     size_t worst = 0;
     for (int rows = 32;; rows += 32) {               // (all that a plan asks of the rows changes behind multiples of 32)
         const int nodes = std::min(max_nodes, rows / g);
-        const TreePlan p = kind == TREE_GROUP && max_nodes * g <= FEW_ROWS ? plan_few(max_len, batch, G) : plan_tree(kind, max_len, batch, G, g, nodes);
+        const TreePlan p = plan_tree(kind, max_len, batch, G, g, nodes);
         const size_t tokens = (size_t)std::min<int64_t>(max_tokens, (int64_t)batch * nodes);
         if (p.n_splits > 1) worst = std::max(worst, tokens * H * p.n_splits);
         if (nodes == max_nodes) break;
