@@ -371,8 +371,8 @@ typedef struct {
  * that has not ended with a logit that is NaN or +infinity, or with none above -infinity.  Of equal ones the lower row's comes first, then the lower token.
  * out_scores, parents, tokens, out_ended: device [rows / width][n], best first: the value rounded to binary32, the row's number in its group, the token, and 1 if
  * the row had ended or the token is end_token (NULL: not wanted).  Behind the last: -infinity, -1, -1, 0.  With n = width these are the next step's rows: out_scores may
- * be scores and out_ended may be ended then.  The sum of a row: binary32 terms, off by 2^-21 of each other at most, and sums of 64 of them; the rest in
- * binary64.  scores: device float [rows].  ws: cusa_beam_workspace_bytes, 256-byte aligned.  ended needs an end_token.
+ * be scores and out_ended may be ended then.  The sum of a row: terms and sums of up to 64 of them in binary32, all else in binary64, so that a value is off by 2^-16
+ * at most before it is rounded.  scores: device float [rows].  ws: cusa_beam_workspace_bytes, 256-byte aligned.  ended needs an end_token.
  * Errors: INVALID_ARG, UNSUPPORTED (width > 32, n > 64, rows > 65535), WORKSPACE_TOO_SMALL, LAUNCH. */
 cusa_status cusa_beam_workspace_bytes(int32_t rows, int32_t vocab, int32_t n, size_t* bytes);
 cusa_status cusa_beam_select(const cusa_beams* beams, const float* scores, const int32_t* ended, float* out_scores, int32_t* parents, int32_t* tokens,
@@ -421,11 +421,10 @@ cusa_status cusa_shared_pages(const cusa_kv* kv, int32_t batch, const cusa_share
 /* FullAttention of every row's one query over its seq_lens[b] tokens (Eq. 1), as cusa_full_attn, but over the list that cusa_shared_pages made of the same tables and
  * lengths: a page is read once for all rows that hold it.  A row without tokens gives zeros.  NaN and infinities in rows of the cache that a query does not attend to do not
  * reach its output; an infinite value of a token that not all rows of the group attend to makes the outputs of those that do infinite whatever the weight, one that all
- * attend to does if the weight is not below 2^-126 of the row's largest (else infinite or NaN).  Weights as in cusa_tree_attn: off by 2^-15 of themselves where width times the query
- * heads of a KV head are up to 64, else rounded to bf16, in the product with V as in their sum.
+ * attend to does if the weight is not below 2^-126 of the row's largest (else infinite or NaN).  Weights are off by 2^-15 of themselves, in the product with V alone.
  * q: device bf16, row b head h at q + b * q_stride + h * 128 (q_stride a multiple of 8, >= n_q_heads * 128); out: device bf16 [batch][n_q_heads][128].  params->batch: rows, a multiple of
  * width.  kv's block_table is not read.  ws: cusa_beam_attn_workspace_bytes, 256-byte aligned, content not preserved.
- * Errors as cusa_full_attn, and UNSUPPORTED for contiguous caches, width > 32, pools of 2^31 or more rows, and more than 147456 pages
+ * Errors as cusa_full_attn, and UNSUPPORTED for contiguous caches, width > 32, pools of 2^31 or more rows, and more than 524288 pages
  * in a group, min(max_entries, width * ceil(max_seq_len / 16)). */
 cusa_status cusa_beam_attn_workspace_bytes(const cusa_params* params, int32_t max_seq_len, const cusa_shared* shared, size_t* bytes);
 cusa_status cusa_beam_attn(const cusa_params* params, const void* q, int64_t q_stride, const cusa_kv* kv, const cusa_shared* shared, void* out,

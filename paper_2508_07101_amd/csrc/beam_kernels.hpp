@@ -15,8 +15,6 @@ namespace cusa {
 constexpr int BEAM_WIDTH = 32;             // rows of a group: a bit each
 constexpr int BEAM_MOST = 64;              // continuations of a group: a lane each
 
-
-
 // ---------------------------------------------------------------- selection
 
 struct BeamArgs {
@@ -164,7 +162,8 @@ struct Best {
 // in falling order.  R loads of 16 bytes a lane are looked at in a step.  Of the step's logits only those above the n-th best so far matter; where n lanes or more have such
 // ones, their maxima are sorted: the n-th largest of them bounds the step's n best from below, and leaves few.  Those few are gathered in LDS, sorted 64 at a time and merged.
 // A weight is 2^((x - ref) log2 e): the difference first, so that rows that differ by a constant have the same sums, whatever the constant.  A lane's ref is a logit of its own
-// that follows the largest when that is 60 above it (2^87: the sum stays in range).
+// that follows the largest when that is 8 above it.  So an exponent is 12 above 0 at most, and below 0 by as much as the row's entropy in bits and one or two more in the weighted mean: its three
+// roundings (difference, product, constant) move the sum by less than 2^-17 of itself, or 2^-16.5 with 2^31 tokens.
 template <int DTYPE, int R>
 __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) {
     typedef Logits<DTYPE> X;
@@ -183,12 +182,13 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
     constexpr int HALF = R < 4 ? R : 4;
     const u32x4 none = {X::NONE, X::NONE, X::NONE, X::NONE};
 
-    float ref = -INFINITY, top = -INFINITY, sum = 0.0f;
+    float ref = -INFINITY, top = -INFINITY;
+    double sum = 0.0;
     auto follow = [&](float largest) {
         top = fmaxf(top, largest);
-        if (__any(largest > ref + 60.0f)) {                // (the first logit above -infinity is)
-            const float to = largest > ref + 60.0f ? largest : ref;
-            if (ref > -INFINITY) sum *= __builtin_amdgcn_exp2f((ref - to) * LOG2E);   // (before that, the sum is 0, or NaN)
+        if (__any(largest > ref + 8.0f)) {                // (the first logit above -infinity is)
+            const float to = largest > ref + 8.0f ? largest : ref;
+            if (ref > -INFINITY) sum *= (double)__builtin_amdgcn_exp2f((ref - to) * LOG2E);   // (before that, the sum is 0, or NaN)
             ref = to;
         }
     };
@@ -220,6 +220,7 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
             }
             largest = fmaxf(largest, some);
             follow(some);
+            float half = 0.0f;
 #pragma unroll
             for (int r = r0; r < r0 + HALF; ++r) {
                 float w[PER];
@@ -229,8 +230,9 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
                 for (int o = PER / 2; o > 0; o >>= 1)
 #pragma unroll
                     for (int k = 0; k < o; ++k) w[k] += w[k + o];
-                sum += w[0];
+                half += w[0];
             }
+            sum += (double)half;
 #pragma unroll
             for (int r = r0; r < r0 + HALF; ++r) asm volatile("" : "+v"(x[r]));   // (what is taken apart is not kept for the search below, which mostly looks at none of it)
         }
@@ -298,13 +300,13 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
         const int i = lane < head ? lane : lane >= 32 && lane - 32 < tail ? a.vocab - tail + lane - 32 : -1;
         const float y = i >= 0 ? X::one(base, i) : -INFINITY;
         follow(y);
-        sum += weight(y);
+        sum += (double)weight(y);
         const bool hit = y > -INFINITY;
         best.add(hit, __ballot(hit), beam_key(y, i));
     }
     if (best.n > 0) best.flush();
     const float all = over_lanes(top, [](float x, float y) { return fmaxf(x, y); });
-    const double total = over_lanes((double)(ref == all || ref == -INFINITY ? sum : sum * __builtin_amdgcn_exp2f((ref - all) * LOG2E)), [](double x, double y) { return x + y; });
+    const double total = over_lanes(ref == all || ref == -INFINITY ? sum : sum * (double)__builtin_amdgcn_exp2f((ref - all) * LOG2E), [](double x, double y) { return x + y; });
     if (lane < a.n) a.best[(int64_t)unit * a.n + lane] = best.list;
     if (lane == 0) {
         a.top[unit] = all;
