@@ -400,7 +400,7 @@ cusa_status cusa_kv_fork(const cusa_pool* pool, int32_t width, const int32_t* he
 
 /* Pages copied in all layers, K and V, all KV heads: of copy i the first copies[i][2] (cut to [0, 16]) tokens of page copies[i][0] into page copies[i][1]; copies whose
  * pages are none of the pool's are left out.  No page is written by two copies or read by one and written by another.  copies: device int32 [n][4], 16-byte aligned.
- * kv's seq_lens, max_seq_len and block_table are not read. */
+ * kv's seq_lens, max_seq_len and block_table are not read.  Errors: INVALID_ARG, UNSUPPORTED (contiguous caches, 2^24 copies or more), LAUNCH. */
 cusa_status cusa_kv_copy(const cusa_params* params, int32_t n_layers, const cusa_kv* kv_layers, const int32_t* copies, int32_t n, void* stream);
 
 /* The pages of groups, host memory.  entries: device int32 [batch / width][max_entries][4], 16-byte aligned: page, column, rows that hold it (bit b: row b of the
@@ -424,8 +424,8 @@ cusa_status cusa_shared_pages(const cusa_kv* kv, int32_t batch, const cusa_share
  * attend to does if the weight is not below 2^-126 of the row's largest (else infinite or NaN).  Weights are off by 2^-15 of themselves, in the product with V alone.
  * q: device bf16, row b head h at q + b * q_stride + h * 128 (q_stride a multiple of 8, >= n_q_heads * 128); out: device bf16 [batch][n_q_heads][128].  params->batch: rows, a multiple of
  * width.  kv's block_table is not read.  ws: cusa_beam_attn_workspace_bytes, 256-byte aligned, content not preserved.
- * Errors as cusa_full_attn, and UNSUPPORTED for contiguous caches, width > 32, pools of 2^31 or more rows, and more than 524288 pages
- * in a group, min(max_entries, width * ceil(max_seq_len / 16)). */
+ * Errors as cusa_full_attn, and UNSUPPORTED for contiguous caches, width > 32, pools of 2^31 or more rows, more than 524288 pages
+ * in a group, min(max_entries, width * ceil(max_seq_len / 16)), and more than 2^24 workgroups (rows times KV heads, at most). */
 cusa_status cusa_beam_attn_workspace_bytes(const cusa_params* params, int32_t max_seq_len, const cusa_shared* shared, size_t* bytes);
 cusa_status cusa_beam_attn(const cusa_params* params, const void* q, int64_t q_stride, const cusa_kv* kv, const cusa_shared* shared, void* out,
                            void* ws, size_t ws_bytes, void* stream);

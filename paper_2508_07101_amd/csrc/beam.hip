@@ -199,6 +199,7 @@ cusa_status cusa_kv_copy(const cusa_params* params, int32_t n_layers, const cusa
         if ((st = check_cache(params, &c, false)) != CUSA_OK) return st;
     }
     if (n == 0) return CUSA_OK;
+    if (n > COPY_MOST) return CUSA_ERR_UNSUPPORTED;
     CopyArgs a = {};
     a.copies = copies;
     a.G = params->n_kv_heads;
@@ -287,7 +288,7 @@ cusa_status cusa_beam_attn(const cusa_params* params, const void* q, int64_t q_s
     a.blocks = pl.blocks;
     a.n_splits = pl.n_splits;
     const int64_t units = ((int64_t)pl.n_splits * G * groups + 7) / 8 * 8 * pl.blocks;
-    if (units > 0x7fffffff) return CUSA_ERR_UNSUPPORTED;
+    if (units * BEAM_ATTN_THREADS > 0xffffffff) return CUSA_ERR_UNSUPPORTED;   // (threads of a launch)
     const dim3 grid((unsigned)units);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (width * g <= 16) launch(KID_BEAM_ATTN, beam_attn_kernel<1>, grid, BEAM_ATTN_THREADS, 0, s, a);

@@ -643,7 +643,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void fork_pages_kernel(ForkArgs a) {
 // ---------------------------------------------------------------- copy
 
 constexpr int COPY_LAYERS = 40;            // layers of a launch: their descriptors travel as arguments (4 KB at most)
-constexpr int COPY_THREADS = 256;
+constexpr int COPY_THREADS = 256, COPY_MOST = (1 << 24) - 1;   // copies of a launch: 2^32 threads are too many
 
 struct CopyLayer {
     uint16_t *k, *v;

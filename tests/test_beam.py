@@ -128,7 +128,7 @@ def test_copies_that_cannot_be():
     assert call(_paged(layout=cb.KV_CONTIGUOUS, stride_token=128)) == cb.ERR_UNSUPPORTED
     assert call(_paged(page_size=8)) == cb.ERR_UNSUPPORTED
     assert call(_paged(k=None)) == cb.ERR_INVALID_ARG and call(_paged(v=FAKE + 8)) == cb.ERR_INVALID_ARG and call(_paged(n_pages=0)) == cb.ERR_INVALID_ARG
-    assert call(_paged(n_pages=1 << 30)) == cb.ERR_UNSUPPORTED
+    assert call(_paged(n_pages=1 << 30)) == cb.ERR_UNSUPPORTED and call(_paged(), n=1 << 24) == cb.ERR_UNSUPPORTED
     assert call(None) == cb.ERR_INVALID_ARG and call(_paged(), layers=0) == cb.ERR_INVALID_ARG and call(_paged(), n=-1) == cb.ERR_INVALID_ARG
     assert call(_paged(), copies=None) == cb.ERR_INVALID_ARG and call(_paged(), copies=FAKE + 8) == cb.ERR_INVALID_ARG
     assert call(_paged(block_table=None, seq_lens=None, max_seq_len=0), n=0) == cb.OK    # nothing to copy, and nothing else is read
@@ -183,3 +183,30 @@ def test_attention_that_cannot_be():
     assert lib.cusa_beam_attn_workspace_bytes(ctypes.byref(p), 160, None, ctypes.byref(n)) == cb.ERR_INVALID_ARG
     assert lib.cusa_beam_attn_workspace_bytes(ctypes.byref(p), 0, ctypes.byref(_list()), ctypes.byref(n)) == cb.ERR_INVALID_ARG
     assert lib.cusa_beam_attn_workspace_bytes(ctypes.byref(p), 160, ctypes.byref(_list(width=5)), ctypes.byref(n)) == cb.ERR_INVALID_ARG
+
+
+def test_attention_over_long_lists():
+    """Groups of up to 2^19 pages, whatever the lengths; a launch of up to 2^24 workgroups."""
+    lib, n = cb.load(), ctypes.c_size_t(0)
+
+    def need(batch, width, max_entries, max_len, H=4, G=2):
+        return lib.cusa_beam_attn_workspace_bytes(ctypes.byref(cb.make_params(batch, H, G, 1, 0)), max_len, ctypes.byref(_list(width=width, max_entries=max_entries)), ctypes.byref(n))
+
+    assert need(32, 32, 1 << 19, 1 << 20) == cb.OK and n.value > 0
+    assert need(32, 32, (1 << 19) + 1, 1 << 20) == cb.ERR_UNSUPPORTED
+    assert need(32, 32, 1 << 30, 1 << 18) == cb.OK and need(32, 32, 1 << 30, (1 << 18) + 1) == cb.ERR_UNSUPPORTED
+    assert need(4, 4, 1 << 30, 1 << 21) == cb.OK and need(4, 4, 1 << 30, (1 << 21) + 1) == cb.ERR_UNSUPPORTED
+    assert _attn(batch=65535, n_q_heads=512, n_kv_heads=512, stride=512 * 128, shared=_list(width=1, max_entries=10)) == cb.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("rows,G", [(1, 8), (16, 8), (256, 1), (65535, 1)])
+def test_workspaces_grow_with_the_lists(rows, G):
+    """A piece for each 256 tokens and no more than 64: a workspace made for longer sequences serves shorter ones."""
+    lib, width = cb.load(), 1
+    sizes = []
+    for max_len in (1, 16, 1000, 2048, 2049, 4096, 4097, 10000, 1 << 17, 1 << 20, 1 << 23):
+        n = ctypes.c_size_t(0)
+        p = cb.make_params(rows, 4 * G, G, 1, 0)
+        assert lib.cusa_beam_attn_workspace_bytes(ctypes.byref(p), max_len, ctypes.byref(_list(width=width, max_entries=1 << 30)), ctypes.byref(n)) == cb.OK
+        sizes.append(n.value)
+    assert sizes == sorted(sizes) and sizes[-1] <= rows * 4 * G * 64 * 130 * 4 + rows * 4 + 1024
