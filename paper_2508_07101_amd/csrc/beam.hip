@@ -56,13 +56,16 @@ cusa_status check_beams(int32_t rows, int32_t vocab, int32_t n) {
 
 constexpr int64_t FORK_ALL = 16384;        // entries of a table that one workgroup changes
 
-int fork_chunks(int32_t max_pages) { return (int)(((int64_t)max_pages + FORK_COLS - 1) / FORK_COLS); }
+// Columns that a workgroup changes, PLAN_THREADS entries, in FORK_COLS columns at most.
+constexpr int FORK_COLS = 256;
+int fork_rows(int32_t width) { return width <= 4 ? 4 : width <= 8 ? 8 : width <= 16 ? 16 : 32; }
+int64_t chunks_of(int64_t max_pages, int cols) { return (max_pages + cols - 1) / cols; }
 
 struct ForkWs {
     size_t rows, counts, freed, total;
 };
 ForkWs fork_ws(int32_t batch, int32_t max_pages) {
-    const size_t chunks = (size_t)batch * fork_chunks(max_pages);     // (one row to a group at least)
+    const size_t chunks = (size_t)batch * chunks_of(max_pages, FORK_COLS);   // (a group of more than 4 rows has shorter chunks, but not more than FORK_COLS columns of each of its rows would be)
     ForkWs w;
     w.rows = 256;
     w.counts = w.rows + align256((size_t)batch * sizeof(ForkRow));
@@ -174,7 +177,8 @@ cusa_status cusa_kv_fork(const cusa_pool* pool, int32_t width, const int32_t* he
     a.n_pages = (int32_t)pool->n_pages;
     a.cap = (int32_t)std::min<int64_t>((int64_t)pool->max_pages * PAGE, 0x7fffffff);
     a.grow = grow != 0;
-    a.chunks = fork_chunks(pool->max_pages);
+    a.cols = PLAN_THREADS / fork_rows(width);
+    a.chunks = (int32_t)chunks_of(pool->max_pages, a.cols);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (width <= FORK_ALL_WIDTH && a.batch <= PLAN_THREADS && (int64_t)a.batch * a.max_pages <= FORK_ALL) {
         launch(KID_KV_FORK, kv_fork_kernel<true>, 1, PLAN_THREADS, 0, s, a);
@@ -182,7 +186,8 @@ cusa_status cusa_kv_fork(const cusa_pool* pool, int32_t width, const int32_t* he
     }
     launch(KID_KV_FORK, kv_fork_kernel<false>, 1, PLAN_THREADS, 0, s, a);
     if (launch_status() != CUSA_OK) return CUSA_ERR_LAUNCH;
-    launch(KID_FORK_TABLES, fork_tables_kernel, dim3((unsigned)a.chunks, (unsigned)(a.batch / width)), FORK_COLS, 0, s, a);
+    const auto tables = width <= 4 ? fork_tables_kernel<4> : width <= 8 ? fork_tables_kernel<8> : width <= 16 ? fork_tables_kernel<16> : fork_tables_kernel<32>;
+    launch(KID_FORK_TABLES, tables, dim3((unsigned)a.chunks, (unsigned)(a.batch / width)), PLAN_THREADS, 0, s, a);
     if (launch_status() != CUSA_OK) return CUSA_ERR_LAUNCH;
     launch(KID_FORK_PAGES, fork_pages_kernel, 1, PLAN_THREADS, 0, s, a);
     return launch_status();
@@ -236,7 +241,8 @@ cusa_status cusa_shared_pages(const cusa_kv* kv, int32_t batch, const cusa_share
     a.n_pages = (int32_t)kv->n_pages;
     a.max_len = kv->max_seq_len;
     a.max_entries = shared->max_entries;
-    launch(KID_SHARED_PAGES, shared_pages_kernel, dim3((unsigned)(batch / shared->width)), SHARED_COLS, 0, static_cast<hipStream_t>(stream), a);
+    const auto kernel = a.width <= 1 ? shared_pages_kernel<1> : a.width <= 2 ? shared_pages_kernel<2> : a.width <= 4 ? shared_pages_kernel<4> : a.width <= 8 ? shared_pages_kernel<8> : a.width <= 16 ? shared_pages_kernel<16> : shared_pages_kernel<32>;
+    launch(KID_SHARED_PAGES, kernel, dim3((unsigned)(batch / a.width)), SHARED_THREADS, 0, static_cast<hipStream_t>(stream), a);
     return launch_status();
 }
 

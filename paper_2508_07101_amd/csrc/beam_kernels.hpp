@@ -62,6 +62,7 @@ __device__ __forceinline__ uint32_t lane_xor(uint32_t v, int stride) {
 __device__ __forceinline__ uint64_t lane_xor(uint64_t v, int stride) {
     return (uint64_t)lane_xor((uint32_t)(v >> 32), stride) << 32 | lane_xor((uint32_t)v, stride);
 }
+__device__ __forceinline__ int lane_xor(int v, int stride) { return (int)lane_xor((uint32_t)v, stride); }
 __device__ __forceinline__ float lane_xor(float v, int stride) { return __uint_as_float(lane_xor(__float_as_uint(v), stride)); }
 __device__ __forceinline__ double lane_xor(double v, int stride) { return __builtin_bit_cast(double, lane_xor(__builtin_bit_cast(uint64_t, v), stride)); }
 
@@ -137,7 +138,7 @@ __device__ __forceinline__ void lds_of_wave() {            // what the wave's ot
 }
 
 // The best 64 of a wave's keys, one in every lane, in falling order; keys are gathered in LDS until they are enough for a sort.
-constexpr int FOUND = 128;
+constexpr int FOUND = 384;
 struct Best {
     uint64_t* found;
     uint64_t list = 0;
@@ -146,6 +147,7 @@ struct Best {
     __device__ __forceinline__ void flush() {
         const int lane = threadIdx.x & 63;
         lds_of_wave();
+#pragma unroll 1
         for (int i = 0; i < n; i += 64) list = merge_lanes(list, sort_lanes<false>(i + lane < n ? found[i + lane] : (uint64_t)0));
         lds_of_wave();
         n = 0;
@@ -193,8 +195,7 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
         }
     };
     auto weight = [&](float x) { return __builtin_amdgcn_exp2f((x - (ref > -INFINITY ? ref : 0.0f)) * LOG2E); };
-#pragma unroll 1
-    for (int v0 = begin; v0 < end; v0 += 64 * R) {
+    auto search = [&](int v0) {
         u32x4 x[R];
         if (v0 + 64 * R <= end) {
 #pragma unroll
@@ -240,7 +241,7 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
         const uint64_t last = lane_key(best.list, a.n - 1);
         float least = above(last ? key_logit(last) : -INFINITY);
         const int lanes = __popcll(__ballot(largest >= least));
-        if (lanes == 0) continue;
+        if (lanes == 0) return;
         const bool bound = lanes >= a.n;
         if (bound) least = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sort_lanes<true>(largest)), a.n - 1));   // (not below the old one: n lanes are)
         const int before = best.n;
@@ -294,17 +295,22 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
                 left -= total;
             }
         }
-        if (best.n >= 32 || !last) best.flush();
+    };
+#pragma unroll 1
+    for (int v0 = begin;; v0 += 64 * R) {
+        if (v0 < end) search(v0);
+        const bool ends = v0 + 64 * R >= end;
+        if (ends && part == 0 && head + tail > 0) {        // what is not 16 aligned bytes: PER - 1 logits at either end at most
+            const int i = lane < head ? lane : lane >= 32 && lane - 32 < tail ? a.vocab - tail + lane - 32 : -1;
+            const float y = i >= 0 ? X::one(base, i) : -INFINITY;
+            follow(y);
+            sum += (double)weight(y);
+            const bool hit = y > -INFINITY;
+            best.add(hit, __ballot(hit), beam_key(y, i));
+        }
+        if (best.n >= 32 || v0 == begin || ends) best.flush();
+        if (ends) break;
     }
-    if (part == 0 && head + tail > 0) {                    // what is not 16 aligned bytes: PER - 1 logits at either end at most
-        const int i = lane < head ? lane : lane >= 32 && lane - 32 < tail ? a.vocab - tail + lane - 32 : -1;
-        const float y = i >= 0 ? X::one(base, i) : -INFINITY;
-        follow(y);
-        sum += (double)weight(y);
-        const bool hit = y > -INFINITY;
-        best.add(hit, __ballot(hit), beam_key(y, i));
-    }
-    if (best.n > 0) best.flush();
     const float all = over_lanes(top, [](float x, float y) { return fmaxf(x, y); });
     const double total = over_lanes(ref == all || ref == -INFINITY ? sum : sum * (double)__builtin_amdgcn_exp2f((ref - all) * LOG2E), [](double x, double y) { return x + y; });
     if (lane < a.n) a.best[(int64_t)unit * a.n + lane] = best.list;
@@ -314,14 +320,32 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
     }
 }
 
-// A workgroup for a group, a wave for each of its rows at a time: the parts' sums and lists together, the tokens' worth in 64 bits.  Where there are n parts or more, the n-th
-// largest of their best bounds the row's n best from below, and few of the lists' keys are left.  Then every candidate counts who comes before it.
-constexpr int MERGE_WAVES = 8;
+// A wave's list of candidates of a group, a lane for each, best first: worth more, of equal ones the lower number (row, place in the row's list).
+struct Candidate {
+    double v;
+    int32_t i;
+    __device__ __forceinline__ bool before(const Candidate& o) const { return v > o.v || (v == o.v && i < o.i); }
+};
+// The best 64 of a list and of one in reverse order.
+__device__ __forceinline__ Candidate merge_candidates(Candidate c, const Candidate& rising) {
+    if (rising.before(c)) c = rising;
+#pragma unroll
+    for (int stride = 32; stride > 0; stride >>= 1) {
+        const Candidate o = {lane_xor(c.v, stride), lane_xor(c.i, stride)};
+        if (o.before(c) == (bool)__builtin_amdgcn_inverse_ballot_w64(~lanes_with(stride))) c = o;
+    }
+    return c;
+}
+
+// A workgroup for a group, a wave for each of its rows at a time: the parts' sums and lists together, the tokens' worth in 64 bits.  Of the parts' q-th best, the m-th largest
+// bounds the row's best m q from below.  With m near half of the parts and m q >= n few of the lists' keys are left.  Then the rows' lists are merged, two at a time.
+constexpr int MERGE_WAVES = 16;
 __global__ __launch_bounds__(64 * MERGE_WAVES) void beam_merge_kernel(BeamArgs a) {
     __shared__ uint64_t found_of[MERGE_WAVES][FOUND];
-    __shared__ double value[BEAM_WIDTH * BEAM_MOST];
-    __shared__ int32_t token[BEAM_WIDTH * BEAM_MOST], over[BEAM_WIDTH], there[BEAM_WIDTH];
+    __shared__ Candidate list_of[MERGE_WAVES][64];
+    __shared__ int32_t token[BEAM_WIDTH * BEAM_MOST], over[BEAM_WIDTH];
     const int group = blockIdx.x, row0 = group * a.width, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Candidate c = {-INFINITY, 0x7fffffff};
     for (int b = wave; b < a.width; b += MERGE_WAVES) {
         const int row = row0 + b;
         const float s = a.scores[row];
@@ -338,90 +362,84 @@ __global__ __launch_bounds__(64 * MERGE_WAVES) void beam_merge_kernel(BeamArgs a
             const int64_t unit = (int64_t)row * a.parts;
             const uint64_t* const keys = a.best + unit * a.n;
             const int all = a.parts * a.n;
+            const bool few = all <= 64;                    // (a row of one part among them)
             constexpr int RUN = 4;                         // loads under way at once
             uint64_t k[RUN];
-            auto request = [&](int i0) {
+            auto request = [&](int j0) {                   // a lane for each list, which is in order: what is above the bound stands in front
 #pragma unroll
-                for (int j = 0; j < RUN; ++j) k[j] = i0 + j * 64 + lane < all ? keys[i0 + j * 64 + lane] : 0;
+                for (int j = 0; j < RUN; ++j) k[j] = mine && j0 + j < a.n ? keys[(int64_t)lane * a.n + j0 + j] : 0;
             };
             const float own = mine ? a.top[unit + lane] : -INFINITY;
             double sum = mine ? a.sum[unit + lane] : 0.0;
-            const uint64_t first = mine && all > 64 ? keys[(int64_t)lane * a.n] : 0;
-            request(0);
+            const int q = max(1, (2 * a.n + a.parts - 1) / a.parts);
+            const uint64_t some = few ? lane < all ? keys[lane] : 0 : mine ? keys[(int64_t)lane * a.n + (q - 1)] : 0;   // (two parts or more: q <= n)
+            if (!few) request(0);
             const float top = over_lanes(own, [](float x, float y) { return fmaxf(x, y); });
             if (own != top) sum *= (double)__builtin_amdgcn_exp2f((own - top) * LOG2E);   // (a part without logits above -infinity: 0, or NaN)
             sum = over_lanes(sum, [](double x, double y) { return x + y; });
             Best best(found_of[wave]);
-            if (all <= 64) {                               // (a row of one part: in order already)
-                best.list = a.parts == 1 ? k[0] : sort_lanes<true>(k[0]);
+            const uint64_t sorted = a.parts == 1 ? some : sort_lanes<true>(some);   // (one part's are in order)
+            if (few) {
+                best.list = sorted;
             } else {
-                const uint64_t least = a.parts >= a.n ? lane_key(sort_lanes<true>(first), a.n - 1) : 0;
-                for (int i0 = 0; i0 < all; i0 += 64 * RUN) {
-#pragma unroll
+                const uint64_t least = lane_key(sorted, (a.n + q - 1) / q - 1);
+                for (int j0 = 0;;) {                       // (code that runs once waits for itself: few copies of the sorts)
+                    uint64_t key = 0;
+#pragma unroll 1
                     for (int j = 0; j < RUN; ++j) {
-                        const bool hit = k[j] != 0 && k[j] >= least;
-                        if (const uint64_t who = __ballot(hit)) best.add(hit, who, k[j]);
-                        if (best.n > FOUND - 64) best.flush();
+                        key = k[0];
+#pragma unroll
+                        for (int i = 1; i < RUN; ++i) k[i - 1] = k[i];
+                        const bool hit = key != 0 && key >= least;
+                        best.add(hit, __ballot(hit), key);
                     }
-                    request(i0 + 64 * RUN);
+                    j0 += RUN;
+                    const bool more = j0 < a.n && __any(key != 0 && key >= least);
+                    if (more) request(j0);
+                    if (!more || best.n > FOUND - 64 * RUN) best.flush();
+                    if (!more) break;
                 }
-                if (best.n > 0) best.flush();
             }
             if (top < INFINITY && sum > 0.0 && lane < a.n && best.list) {
                 v = (double)s + (((double)key_logit(best.list) - (double)top) - log(sum));
                 t = key_token(best.list);
             }
         }
-        if (lane < a.n) {
-            value[b * a.n + lane] = v;
-            token[b * a.n + lane] = t;
-        }
-        const int n = __popcll(__ballot(v > -INFINITY));
-        if (lane == 0) {
-            over[b] = ended;
-            there[b] = n;
-        }
+        if (lane < a.n) token[b * a.n + lane] = t;
+        if (lane == 0) over[b] = ended;
+        const int i = lane < a.n ? b * a.n + lane : 0x7fffffff;
+        c = b == wave ? Candidate{v, i} : merge_candidates(c, {__shfl(v, 63 - lane), __shfl(i, 63 - lane)});
     }
-    __syncthreads();
-    const int candidates = a.width * a.n;
-    for (int i = threadIdx.x; i < candidates; i += 64 * MERGE_WAVES) {
-        const int b = i / a.n, j = i - b * a.n;
-        const double v = value[i];
-        if (j >= there[b]) continue;
-        int rank;                                          // candidates that come before this one: of equal ones those of lower rows
-        if (candidates <= 256) {
-            rank = 0;
-#pragma unroll 8
-            for (int o = 0; o < candidates; ++o) rank += value[o] > v || (value[o] == v && o < i);
-        } else {                                           // row by row, in as many looks as n has bits
-            rank = j;
-            for (int o = 0; o < a.width; ++o) {
-                if (o == b) continue;
-                int lo = 0, hi = there[o];                 // the first of row o that does not
-                while (lo < hi) {
-                    const int mid = (lo + hi) >> 1;
-                    const double w = value[o * a.n + mid];
-                    if (w > v || (o < b && w == v)) lo = mid + 1;
-                    else hi = mid;
-                }
-                rank += lo;
-            }
-        }
-        if (rank >= a.n) continue;
-        const int64_t to = (int64_t)group * a.n + rank;
-        a.out_scores[to] = (float)v;
-        a.parents[to] = b;
-        a.tokens[to] = token[i];
-        if (a.out_ended) a.out_ended[to] = over[b] || token[i] == a.end_token;
+    const int lists = min(a.width, MERGE_WAVES);
+    for (int step = 1; step < lists; step <<= 1) {
+        if ((wave & (2 * step - 1)) == step) list_of[wave][lane] = c;
+        __syncthreads();
+        if ((wave & (2 * step - 1)) == 0 && wave + step < lists) c = merge_candidates(c, list_of[wave + step][63 - lane]);
     }
-    int all = 0;
-    for (int b = 0; b < a.width; ++b) all += there[b];
-    for (int i = all + threadIdx.x; i < a.n; i += 64 * MERGE_WAVES) {
-        const int64_t to = (int64_t)group * a.n + i;
-        a.out_scores[to] = -INFINITY;
-        a.parents[to] = a.tokens[to] = -1;
-        if (a.out_ended) a.out_ended[to] = 0;
+    lds_of_wave();
+    if (wave != 0 || lane >= a.n) return;
+    const bool is = c.v > -INFINITY;
+    const int b = is ? c.i / a.n : -1, t = is ? token[c.i] : -1;
+    const int64_t to = (int64_t)group * a.n + lane;
+    a.out_scores[to] = (float)c.v;
+    a.parents[to] = b;
+    a.tokens[to] = t;
+    if (a.out_ended) a.out_ended[to] = is && (over[b] || t == a.end_token);
+}
+
+// Which of a column's rows hold this page; column: LDS, theirs side by side.
+template <int ROWS>
+__device__ __forceinline__ uint32_t holders_of(const int32_t* column, int32_t page) {
+    constexpr int RUN = ROWS < 4 ? ROWS : 4;               // to a read
+    typedef int32_t entries __attribute__((ext_vector_type(RUN)));
+    uint32_t holders = 0;
+#pragma unroll
+    for (int o = 0; o < ROWS; o += RUN) {
+        const entries x = *reinterpret_cast<const entries*>(column + o);
+#pragma unroll
+        for (int k = 0; k < RUN; ++k) holders |= x[k] == page ? 1u << (o + k) : 0u;
     }
+    return holders;
 }
 
 // ---------------------------------------------------------------- fork
@@ -443,35 +461,33 @@ struct ForkArgs {
     int32_t* state_out;
     ForkHead* head;
     ForkRow* rows;
-    int32_t *counts, *freed;               // of each (group, FORK_COLS columns): how many pages go back, and which
-    int32_t batch, width, max_pages, n_pages, cap, grow, chunks;
+    int32_t *counts, *freed;               // of each (group, cols columns): how many pages go back, and which
+    int32_t batch, width, max_pages, n_pages, cap, grow, cols, chunks;
 };
-constexpr int FORK_COLS = 256;
 
 // A column of a group: what the rows hold there goes from `table` to `table_out`, all of it read before any is written, so that the tables may be changed in place.  Returns the
-// rows whose entry names a page that nobody holds any more (of several, the first).  entry: a column in LDS, STRIDE entries from row to row.
-template <int STRIDE>
+// rows whose entry names a page that nobody holds any more (of several, the first).  entry: a column in LDS, PLAN_THREADS entries from row to row.
 __device__ __forceinline__ uint32_t fork_column(const ForkArgs& a, const ForkRow* rows, int row0, int col, int32_t* entry) {
     const int32_t* const from = a.table + (int64_t)row0 * a.max_pages + col;
     int32_t* const to = a.table_out + (int64_t)row0 * a.max_pages + col;
     uint32_t alive = 0;                                    // rows that somebody descends from
 #pragma unroll 4
     for (int b = 0; b < a.width; ++b) {
-        entry[b * STRIDE] = col < rows[b].old ? from[(int64_t)b * a.max_pages] : -1;
+        entry[b * PLAN_THREADS] = col < rows[b].old ? from[(int64_t)b * a.max_pages] : -1;
         if (rows[b].src >= 0) alive |= 1u << rows[b].src;
     }
     for (int b = 0; b < a.width; ++b) {
         const ForkRow& r = rows[b];
         if (col == r.col) to[(int64_t)b * a.max_pages] = r.page;
-        else if (r.src >= 0 && col < r.had) to[(int64_t)b * a.max_pages] = entry[r.src * STRIDE];
+        else if (r.src >= 0 && col < r.had) to[(int64_t)b * a.max_pages] = entry[r.src * PLAN_THREADS];
     }
     uint32_t gone = 0;
     for (uint32_t ends = ~alive & (a.width < 32 ? (1u << a.width) - 1 : 0xffffffffu); ends; ends &= ends - 1) {
         const int b = __builtin_ctz(ends);
-        const int32_t e = entry[b * STRIDE];
+        const int32_t e = entry[b * PLAN_THREADS];
         if ((uint32_t)e >= (uint32_t)a.n_pages) continue;
         bool last = true;                                  // nobody who stays holds it, and no row before this one did
-        for (int o = 0; o < a.width; ++o) last &= !(entry[o * STRIDE] == e && ((alive >> o & 1) || o < b));
+        for (int o = 0; o < a.width; ++o) last &= !(entry[o * PLAN_THREADS] == e && ((alive >> o & 1) || o < b));
         if (last) gone |= 1u << b;
     }
     return gone;
@@ -566,7 +582,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void kv_fork_kernel(ForkArgs a) {
         int which = 2;                                     // (plan_scan's words: not those of the call before)
         for (int i0 = 0; i0 < all; i0 += PLAN_THREADS, which = which == 2 ? 0 : 2) {
             const int i = i0 + tid, group = i < all ? i / cols : 0, row0 = group * a.width;
-            uint32_t gone = i < all ? fork_column<PLAN_THREADS>(a, s_rows + row0, row0, i - group * cols, &s_entry[0][tid]) : 0;
+            uint32_t gone = i < all ? fork_column(a, s_rows + row0, row0, i - group * cols, &s_entry[0][tid]) : 0;
             int64_t sum, at = (int64_t)first + avail + pushed + plan_scan(__popc(gone), sum, scratch[which], PLAN_THREADS / 64);
             for (; gone; gone &= gone - 1) a.ring[ring_at(at++, a.n_pages)] = s_entry[__builtin_ctz(gone)][tid];
             pushed += sum;
@@ -579,39 +595,43 @@ __global__ __launch_bounds__(PLAN_THREADS) void kv_fork_kernel(ForkArgs a) {
     }
 }
 
-// A workgroup for FORK_COLS columns of a group.
-__global__ __launch_bounds__(FORK_COLS) void fork_tables_kernel(ForkArgs a) {
-    __shared__ int32_t entry[BEAM_WIDTH][FORK_COLS];
-    __shared__ ForkRow rows[BEAM_WIDTH];
-    __shared__ int32_t sums[FORK_COLS / 64];
-    const int tid = threadIdx.x, group = blockIdx.y, row0 = group * a.width, col = blockIdx.x * FORK_COLS + tid, lane = tid & 63, wave = tid >> 6;
-    if (tid < a.width) rows[tid] = a.rows[row0 + tid];
-    __syncthreads();
-    int most = 0;
-    for (int b = 0; b < a.width; ++b) most = max(most, fork_most(rows[b]));
+// A workgroup for PLAN_THREADS / ROWS columns of a group, a thread for a row's entry in a column, rows side by side (ROWS: the width, or the next power of two).  A column's rows are one wave's, which
+// reads all before it writes any.
+template <int ROWS>
+__global__ __launch_bounds__(PLAN_THREADS) void fork_tables_kernel(ForkArgs a) {
+    constexpr int WAVES = PLAN_THREADS / 64, COLS = PLAN_THREADS / ROWS;
+    __shared__ __attribute__((aligned(16))) int32_t entry[WAVES][64];
+    __shared__ int32_t sums[WAVES];
+    const int tid = threadIdx.x, group = blockIdx.y, row0 = group * a.width, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = lane & (ROWS - 1);
+    const ForkRow r = b < a.width ? a.rows[row0 + b] : ForkRow{-1, 0, 0, -1, -1};
+    const int most = over_lanes(fork_most(r), [](int x, int y) { return max(x, y); });
+    const uint32_t alive = over_lanes(r.src >= 0 ? 1u << r.src : 0u, [](uint32_t x, uint32_t y) { return x | y; });   // rows that somebody descends from
     const int64_t chunk = (int64_t)group * a.chunks + blockIdx.x;
-    if ((int)blockIdx.x * FORK_COLS >= most) {
+    if ((int)blockIdx.x * COLS >= most) {
         if (tid == 0) a.counts[chunk] = 0;
         return;
     }
-    uint32_t gone = fork_column<FORK_COLS>(a, rows, row0, col, &entry[0][tid]);
-    const int n = __popc(gone);
-    int x = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(x, o);
-        if (lane >= o) x += y;
-    }
-    if (lane == 63) sums[wave] = x;
+    const int col = blockIdx.x * COLS + tid / ROWS, mates = lane & ~(ROWS - 1);
+    const int64_t at_table = (int64_t)(row0 + b) * a.max_pages + col;
+    const int32_t e = col < r.old ? a.table[at_table] : -1;
+    entry[wave][lane] = e;
+    lds_of_wave();
+    const uint32_t holders = holders_of<ROWS>(&entry[wave][mates], e);
+    const int32_t taken = entry[wave][mates + max(r.src, 0)];
+    if (col == r.col) a.table_out[at_table] = r.page;
+    else if (r.src >= 0 && col < r.had) a.table_out[at_table] = taken;
+    // Pages that nobody who stays holds go back, each once.
+    const bool gone = !(alive >> b & 1) && (uint32_t)e < (uint32_t)a.n_pages && (holders & (alive | ((1u << b) - 1))) == 0;
+    const uint64_t who = __ballot(gone);
+    if (lane == 0) sums[wave] = __popcll(who);
     __syncthreads();
-    int at = x - n, total = 0;
+    int at = lanes_before(who), total = 0;
 #pragma unroll
-    for (int w = 0; w < FORK_COLS / 64; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         if (w < wave) at += sums[w];
         total += sums[w];
     }
-    int32_t* const list = a.freed + chunk * FORK_COLS * a.width;
-    for (; gone; gone &= gone - 1) list[at++] = entry[__builtin_ctz(gone)][tid];
+    if (gone) a.freed[chunk * COLS * a.width + at] = e;
     if (tid == 0) a.counts[chunk] = total;
 }
 
@@ -632,7 +652,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void fork_pages_kernel(ForkArgs a) {
 #pragma unroll
             for (int step = PLAN_THREADS / 2; step > 0; step >>= 1)
                 if (start[lo + step] <= i) lo += step;
-            a.ring[ring_at((int64_t)h.first + h.avail + pushed + i, a.n_pages)] = a.freed[(int64_t)(base + lo) * FORK_COLS * a.width + (i - start[lo])];
+            a.ring[ring_at((int64_t)h.first + h.avail + pushed + i, a.n_pages)] = a.freed[(int64_t)(base + lo) * a.cols * a.width + (i - start[lo])];
         }
         pushed += sum;
         __syncthreads();
@@ -692,62 +712,74 @@ struct SharedArgs {
     int32_t *entries, *count;
     int32_t batch, width, max_pages, n_pages, max_len, max_entries;
 };
-constexpr int SHARED_COLS = 1024;
+constexpr int SHARED_THREADS = 1024, SHARED_STEPS = 4;
 
-// A workgroup for a group, a thread for a column.
-__global__ __launch_bounds__(SHARED_COLS) void shared_pages_kernel(SharedArgs a) {
-    __shared__ int32_t entry[BEAM_WIDTH][SHARED_COLS], len[BEAM_WIDTH], sums[SHARED_COLS / 64], broken;
-    const int tid = threadIdx.x, group = blockIdx.x, row0 = group * a.width, lane = tid & 63, wave = tid >> 6;
-    if (tid < a.width) len[tid] = clampi(a.lens[row0 + tid], 0, a.max_len);
+// A workgroup for a group; a thread for a row's entry in a column, rows side by side (ROWS: the width, or the next power of two), which is the list's order.  Each compares its page with those of
+// the column's other rows; SHARED_STEPS entries a thread between two barriers.
+template <int ROWS>
+__global__ __launch_bounds__(SHARED_THREADS) void shared_pages_kernel(SharedArgs a) {
+    constexpr int WAVES = SHARED_THREADS / 64, COLS = SHARED_THREADS / ROWS;
+    static_assert(WAVES * SHARED_STEPS == 64, "a lane for each of the waves' sums");
+    __shared__ __attribute__((aligned(16))) int32_t entry[WAVES][SHARED_STEPS][64];
+    __shared__ int32_t len[BEAM_WIDTH], sums[2][SHARED_STEPS * WAVES], broken;
+    const int tid = threadIdx.x, group = blockIdx.x, row0 = group * a.width, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = lane & (ROWS - 1);
+    if (tid < BEAM_WIDTH) len[tid] = tid < a.width ? clampi(a.lens[row0 + tid], 0, a.max_len) : 0;
     if (tid == 0) broken = 0x7fffffff;                     // the first entry that some row does not attend to as a whole
     __syncthreads();
-    uint32_t everyone = 0;
-    int least = 0x7fffffff, most = 0;
-    for (int b = 0; b < a.width; ++b) {
-        if (len[b] == 0) continue;
-        everyone |= 1u << b;
-        least = min(least, len[b]);
-        most = max(most, len[b]);
-    }
+    const uint64_t with = __ballot(lane < BEAM_WIDTH && len[lane & (BEAM_WIDTH - 1)] > 0);
+    const uint32_t everyone = (uint32_t)with;
+    const int own = len[lane & (BEAM_WIDTH - 1)], mine = b < a.width ? pages_of(len[b]) : 0;
+    const int most = over_lanes(own, [](int x, int y) { return max(x, y); }), least = over_lanes(own > 0 ? own : 0x7fffffff, [](int x, int y) { return min(x, y); });
+    const int32_t* const table = a.table + (int64_t)(row0 + min(b, a.width - 1)) * a.max_pages;
     i32x4* const list = reinterpret_cast<i32x4*>(a.entries) + (int64_t)group * a.max_entries;
+    const int columns = pages_of(most);
     int64_t found = 0;
-    for (int c0 = 0; c0 < pages_of(most); c0 += SHARED_COLS) {
-        const int col = c0 + tid;
-        for (int b = 0; b < a.width; ++b) {
-            const int32_t e = col < pages_of(len[b]) ? a.table[(int64_t)(row0 + b) * a.max_pages + col] : -1;
-            entry[b][tid] = (uint32_t)e < (uint32_t)a.n_pages ? e : -1;
+    int32_t next[SHARED_STEPS];
+    auto request = [&](int c0) {
+#pragma unroll
+        for (int j = 0; j < SHARED_STEPS; ++j) {
+            const int col = c0 + j * COLS + tid / ROWS;
+            next[j] = col < mine ? table[col] : -1;
         }
-        uint32_t leads = 0;
-        for (int b = 0; b < a.width; ++b) {
-            const int32_t e = entry[b][tid];
-            bool first = e >= 0;
-            for (int o = 0; o < b; ++o) first &= entry[o][tid] != e;
-            if (first) leads |= 1u << b;
+    };
+    request(0);
+    for (int c0 = 0, which = 0; c0 < columns; c0 += SHARED_STEPS * COLS, which ^= 1) {
+        int32_t e[SHARED_STEPS];
+#pragma unroll
+        for (int j = 0; j < SHARED_STEPS; ++j) {
+            e[j] = (uint32_t)next[j] < (uint32_t)a.n_pages ? next[j] : -1;
+            entry[wave][j][lane] = e[j];
         }
-        const int n = __popc(leads);
-        int x = n;
+        request(c0 + SHARED_STEPS * COLS);
+        lds_of_wave();
+        uint32_t holders[SHARED_STEPS];
+        uint64_t leads[SHARED_STEPS];
+#pragma unroll
+        for (int j = 0; j < SHARED_STEPS; ++j) {
+            holders[j] = c0 + j * COLS < columns ? holders_of<ROWS>(&entry[wave][j][lane & ~(ROWS - 1)], e[j]) : 0;
+            leads[j] = __ballot(e[j] >= 0 && (holders[j] & ((1u << b) - 1)) == 0);
+            if (lane == 0) sums[which][j * WAVES + wave] = __popcll(leads[j]);
+        }
+        __syncthreads();                                   // (entry is the wave's own; sums of the step after the next wait for this one's readers at the next barrier)
+        int x = sums[which][lane];
+        const int own_sum = x;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
             const int y = __shfl_up(x, o);
             if (lane >= o) x += y;
         }
-        if (lane == 63) sums[wave] = x;
-        __syncthreads();
-        int64_t at = found + x - n;
-        for (int w = 0; w < SHARED_COLS / 64; ++w) {
-            if (w < wave) at += sums[w];
-            found += sums[w];
+#pragma unroll
+        for (int j = 0; j < SHARED_STEPS; ++j) {
+            const int64_t at = found + __shfl(x - own_sum, j * WAVES + wave) + lanes_before(leads[j]);
+            const int col = c0 + j * COLS + tid / ROWS;
+            const bool is = leads[j] >> lane & 1;
+            if (is && at < a.max_entries) list[at] = i32x4{e[j], col, (int)holders[j], 0};
+            const uint64_t bad = __ballot(is && (holders[j] != everyone || (int64_t)(col + 1) * PAGE > least));
+            if (bad && lane == __builtin_ctzll(bad)) atomicMin(&broken, (int)min(at, (int64_t)0x7fffffff));
         }
-        for (; leads; leads &= leads - 1, ++at) {
-            const int32_t e = entry[__builtin_ctz(leads)][tid];
-            uint32_t holders = 0;
-            for (int b = 0; b < a.width; ++b)
-                if (entry[b][tid] == e) holders |= 1u << b;
-            if (at < a.max_entries) list[at] = i32x4{e, col, (int)holders, 0};
-            if (holders != everyone || (int64_t)(col + 1) * PAGE > least) atomicMin(&broken, (int)min(at, (int64_t)0x7fffffff));
-        }
-        __syncthreads();
+        found += __builtin_amdgcn_readlane(x, 63);
     }
+    __syncthreads();
     if (tid == 0) {
         const int n = (int)min(found, (int64_t)a.max_entries);
         a.count[group * 2] = n;
