@@ -756,7 +756,11 @@ __global__ __launch_bounds__(SHARED_THREADS) void shared_pages_kernel(SharedArgs
         uint64_t leads[SHARED_STEPS];
 #pragma unroll
         for (int j = 0; j < SHARED_STEPS; ++j) {
-            holders[j] = c0 + j * COLS < columns ? holders_of<ROWS>(&entry[wave][j][lane & ~(ROWS - 1)], e[j]) : 0;
+            const int mates = lane & ~(ROWS - 1);
+            const uint64_t there = __ballot(e[j] >= 0);
+            if (there == 0) holders[j] = 0;
+            else if (__all(e[j] < 0 || e[j] == entry[wave][j][mates])) holders[j] = (uint32_t)(there >> mates) & (uint32_t)((1ull << ROWS) - 1);   // (a common prompt's)
+            else holders[j] = holders_of<ROWS>(&entry[wave][j][mates], e[j]);
             leads[j] = __ballot(e[j] >= 0 && (holders[j] & ((1u << b) - 1)) == 0);
             if (lane == 0) sums[which][j * WAVES + wave] = __popcll(leads[j]);
         }
