@@ -18,14 +18,15 @@ cusa_status check_workspace(const void* ws, size_t have, size_t need) {
     return have < need ? CUSA_ERR_WORKSPACE_TOO_SMALL : CUSA_OK;
 }
 
-// Parts of a row, a wave each: enough waves for the chip, but parts of 4 KB at least, and a lane each where they come together.
-constexpr int PART_LEAST = 256;            // loads of 16 bytes
+// Parts of a row, a wave each: enough waves for the chip, but parts of 4 KB at least, and a lane each where they come together.  (512 rows of 131072 bf16 logits: 1024 waves 47 us,
+// 2048 35, 4096 31, 6144 35.  4 rows of 32000, selection and merge: parts of 2 KB 12.2, 4 KB 12.4, 8 KB 15.3; 52 rows of 67306 for 59 places: 20.8, 18.8, 24.5.)
+constexpr int PART_WAVES = 4096, PART_LEAST = 256;   // loads of 16 bytes
 struct BeamParts {
     int parts, len;                        // len: loads of 16 bytes
 };
 BeamParts beam_parts(int32_t rows, int32_t vocab, int size) {
     const int64_t loads = std::max<int64_t>(1, ((int64_t)vocab * size + 15) / 16);
-    const int64_t want = std::min<int64_t>({(loads + PART_LEAST - 1) / PART_LEAST, std::max(1, 4096 / rows), 64});
+    const int64_t want = std::min<int64_t>({(loads + PART_LEAST - 1) / PART_LEAST, std::max(1, PART_WAVES / rows), 64});
     const int64_t len = ((loads + want - 1) / want + 63) / 64 * 64;
     return {(int)((loads + len - 1) / len), (int)len};
 }
@@ -45,6 +46,7 @@ BeamWs beam_ws(int32_t rows, int parts, int32_t n) {
 template <int DTYPE>
 void launch_rows(hipStream_t s, const BeamArgs& a) {
     const dim3 grid((unsigned)(((int64_t)a.rows * a.parts + BEAM_WAVES - 1) / BEAM_WAVES));
+    // Eight loads a lane under way, or four where a part has no more.  (512 rows of 131072 bf16 logits: eight 31 us, four 35; 256 rows of 32000 for 64 places, parts of 4 KB: 36 and 28.)
     if (a.part_len <= PART_LEAST) launch(KID_BEAM_ROWS, beam_rows_kernel<DTYPE, 4>, grid, 64 * BEAM_WAVES, 0, s, a);
     else launch(KID_BEAM_ROWS, beam_rows_kernel<DTYPE, 8>, grid, 64 * BEAM_WAVES, 0, s, a);
 }
@@ -54,7 +56,8 @@ cusa_status check_beams(int32_t rows, int32_t vocab, int32_t n) {
     return rows > MAX_BATCH || n > BEAM_MOST ? CUSA_ERR_UNSUPPORTED : CUSA_OK;
 }
 
-constexpr int64_t FORK_ALL = 16384;        // entries of a table that one workgroup changes
+// Entries of a table that one workgroup changes.  (One launch and three, as a program sees them: 1100 entries 10.5 and 15.9 us, 4400 13.6 and 15.7, 4500 of short rows 15.5 and 16.1, 17000 27 and 16.)
+constexpr int64_t FORK_ALL = 4096;
 
 // Columns that a workgroup changes, PLAN_THREADS entries, in FORK_COLS columns at most.
 constexpr int FORK_COLS = 256;

@@ -166,6 +166,9 @@ struct Best {
 // A weight is 2^((x - ref) log2 e): the difference first, so that rows that differ by a constant have the same sums, whatever the constant.  A lane's ref is a logit of its own
 // that follows the largest when that is 8 above it.  So an exponent is 12 above 0 at most, and below 0 by as much as the row's entropy in bits and one or two more in the weighted mean: its three
 // roundings (difference, product, constant) move the sum by less than 2^-17 of itself, or 2^-16.5 with 2^31 tokens.
+// Bound by what a wave does between its loads, four waves to a SIMD: 512 rows of 131072 bf16 logits, 134 MB: 31 us, 4.3 TB/s (a plain read 19.6 us), with vector instructions under way for 20.5 us of
+// it.  Asking for the next step's logits before this one's search: 37 us.  A rougher bound from maxima over groups of lanes instead of the sort: 14 % fewer instructions and as long, and with
+// nine logits in ten masked 26 us for 17, for the keys that it lets through.
 template <int DTYPE, int R>
 __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) {
     typedef Logits<DTYPE> X;
@@ -339,6 +342,8 @@ __device__ __forceinline__ Candidate merge_candidates(Candidate c, const Candida
 
 // A workgroup for a group, a wave for each of its rows at a time: the parts' sums and lists together, the tokens' worth in 64 bits.  Of the parts' q-th best, the m-th largest
 // bounds the row's best m q from below.  With m near half of the parts and m q >= n few of the lists' keys are left.  Then the rows' lists are merged, two at a time.
+// Bound by its chain of sorts and of code that runs once, a copy of which is fetched first: 64 groups of 8 rows for 8 places 6 us, 8 groups of 32 rows for 64 places 25 (each candidate counting those in
+// front of it: 145).  4 rows of 32000 logits: 6 us here and 6 in beam_rows_kernel, of which a launch and the way to memory and back are most.
 constexpr int MERGE_WAVES = 16;
 __global__ __launch_bounds__(64 * MERGE_WAVES) void beam_merge_kernel(BeamArgs a) {
     __shared__ uint64_t found_of[MERGE_WAVES][FOUND];
@@ -494,7 +499,8 @@ __device__ __forceinline__ uint32_t fork_column(const ForkArgs& a, const ForkRow
 }
 __device__ __forceinline__ int fork_most(const ForkRow& r) { return max(r.old, max(r.had, r.col + 1)); }
 
-// A thread for each row, as many whole groups at a time as 1024 hold.  Latency is all: the numbers, the parent's length, the open page's entry, two sums, a page of the queue.
+// A thread for each row, as many whole groups at a time as 1024 hold.  Latency is all: the numbers, the parent's length, the open page's entry, two sums, a page of the queue: 6.2 us for one group,
+// 7.3 for 64 of 4 rows, 16 for 8 of 32, whose rows look at each other's pages one after the other.
 // ALL: the workgroup changes the tables as well, a thread for a column of a group, and gives the pages back; for few rows, whose launches would take longer.
 constexpr int FORK_ALL_WIDTH = 8;          // rows of a group that it has LDS for
 template <bool ALL>
@@ -596,7 +602,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void kv_fork_kernel(ForkArgs a) {
 }
 
 // A workgroup for PLAN_THREADS / ROWS columns of a group, a thread for a row's entry in a column, rows side by side (ROWS: the width, or the next power of two).  A column's rows are one wave's, which
-// reads all before it writes any.
+// reads all before it writes any.  64 groups of 4 rows, 2080 columns: 4.5 us; 8 groups of 32 beams: 6.5 (a thread for a column, which goes over its rows: 6.3 and 38).
 template <int ROWS>
 __global__ __launch_bounds__(PLAN_THREADS) void fork_tables_kernel(ForkArgs a) {
     constexpr int WAVES = PLAN_THREADS / 64, COLS = PLAN_THREADS / ROWS;
@@ -635,7 +641,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void fork_tables_kernel(ForkArgs a) {
     if (tid == 0) a.counts[chunk] = total;
 }
 
-// The pages that go back, in order: a thread for each, which looks up its list among 1024.
+// The pages that go back, in order: a thread for each, which looks up its list among 1024.  4 to 6 us, a launch's own time and two ways to memory.
 __global__ __launch_bounds__(PLAN_THREADS) void fork_pages_kernel(ForkArgs a) {
     __shared__ int64_t scratch[2][2][PLAN_THREADS / 64];
     __shared__ int32_t start[PLAN_THREADS];
@@ -676,7 +682,8 @@ struct CopyArgs {
 };
 static_assert(sizeof(CopyArgs) <= 4096, "a launch's arguments");
 
-// A workgroup for a copy in a layer: 16 lanes a row of 256 bytes, eight rows of theirs under way.
+// A workgroup for a copy in a layer: 16 lanes a row of 256 bytes, eight rows of theirs under way.  Bound by memory: 256 pages of 1 to 15 tokens, a quarter of them none, 8 KV heads, 32 layers: 106 us, 4.36 TB/s read and
+// written (with 8 tokens in each 4.94, a plain copy of a large tensor 5.08).  Four pages of 36 layers: 5.7 us, a launch's own time.
 __global__ __launch_bounds__(COPY_THREADS) void kv_copy_kernel(CopyArgs a) {
     const CopyLayer& l = a.layer[blockIdx.y];
     const i32x4 copy = *reinterpret_cast<const i32x4*>(a.copies + (int64_t)blockIdx.x * 4);
@@ -715,7 +722,8 @@ struct SharedArgs {
 constexpr int SHARED_THREADS = 1024, SHARED_STEPS = 4;
 
 // A workgroup for a group; a thread for a row's entry in a column, rows side by side (ROWS: the width, or the next power of two), which is the list's order.  Each compares its page with those of
-// the column's other rows; SHARED_STEPS entries a thread between two barriers.
+// the column's other rows; SHARED_STEPS entries a thread between two barriers.  Bound by the steps' latency, each waiting for the table's entries and the list's stores: 4.4 us for one group of 4 rows
+// and 300 columns, 9 for 64 groups and 2080 columns, 51 for 8 groups of 32 and 2080 (a thread for a column, which goes over its rows: 5.7, 13, 170; 15 groups of 16 rows and 7 columns 28, so 5).
 template <int ROWS>
 __global__ __launch_bounds__(SHARED_THREADS) void shared_pages_kernel(SharedArgs a) {
     constexpr int WAVES = SHARED_THREADS / 64, COLS = SHARED_THREADS / ROWS;
