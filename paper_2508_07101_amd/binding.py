@@ -664,11 +664,15 @@ class SharedPages:
         return SharedPages(width, torch.zeros((batch // width, most, 4), dtype=torch.int32, device=device), torch.zeros((batch // width, 2), dtype=torch.int32, device=device))
 
     def desc(self, what: str, batch: int, gpu: int) -> CusaShared:
-        e, groups = self.entries, batch // self.width if self.width else 0
-        _need_group(what, batch, self.width)
-        shape = e.shape
-        _need(len(shape) == 3 and shape[0] >= groups and shape[2] == 4, "entries of shared pages are [groups, most, 4]")
-        return CusaShared(self.width, shape[1], _take(what, "entries", e, torch.int32, groups * shape[1] * 4, gpu), _take(what, "count", self.count, torch.int32, groups * 2, gpu, 2))
+        e, c, width, i32 = self.entries, self.count, self.width, torch.int32
+        shape, groups = e.shape, batch // width if width > 0 else 0
+        # (each layer's call makes one: everything is asked once, and what is wrong only where something is)
+        if (groups < 1 or groups * width != batch or len(shape) != 3 or shape[0] < groups or shape[2] != 4 or e.dtype is not i32 or c.dtype is not i32
+                or c.numel() < groups * 2 or c.shape[-1] != 2 or not e.is_contiguous() or not c.is_contiguous() or e.get_device() != gpu or c.get_device() != gpu):
+            _need_group(what, batch, width)
+            _need(len(shape) == 3 and shape[0] >= groups and shape[2] == 4, "entries of shared pages are [groups, most, 4]")
+            return CusaShared(width, shape[1], _take(what, "entries", e, i32, groups * shape[1] * 4, gpu), _take(what, "count", c, i32, groups * 2, gpu, 2))
+        return CusaShared(width, shape[1], e.data_ptr(), c.data_ptr())
 
 
 def pages_workspace_bytes(batch: int, max_seq_len: int) -> int:
@@ -704,12 +708,14 @@ def beam_attn(params: CusaParams, q, kv: KvCache, shared: SharedPages, out, ws):
     """Full attention of every row's token, q [B, H, 128] (a view of a fused projection's rows, or contiguous), over the pages of its group: each is read once
     for all rows that hold it.  shared: of the same tables and lengths."""
     what, gpu = "beam_attn", _device()
-    _need(q.dim() == 3, "beam_attn: q is [batch, n_q_heads, 128]")
-    n, heads, d = q.shape
+    shape = q.shape
+    _need(len(shape) == 3, "beam_attn: q is [batch, n_q_heads, 128]")
+    n, heads, d = shape
     strides = _strides(q, (heads * d, d, 1)) if n == 1 or heads == 1 else q.stride()
-    _need(q.dtype is torch.bfloat16 and n == params.batch and heads == params.n_q_heads and d == params.head_dim and strides[2] == 1 and strides[1] == d and q.get_device() == gpu,
-          "beam_attn: q is bf16 [batch, n_q_heads, 128], heads side by side, on the current GPU")
-    _need(kv.block_table is not None and kv.k.get_device() == gpu, "beam_attn: a paged cache on the current GPU")
+    if q.dtype is not torch.bfloat16 or n != params.batch or heads != params.n_q_heads or d != params.head_dim or strides[2] != 1 or strides[1] != d or q.get_device() != gpu:
+        raise ValueError("beam_attn: q is bf16 [batch, n_q_heads, 128], heads side by side, on the current GPU")
+    if kv.block_table is None or kv.k.get_device() != gpu:
+        raise ValueError("beam_attn: a paged cache on the current GPU")
     s = shared.desc(what, n, gpu)
     c = _cache_desc(what, params, kv)
     _check(load().cusa_beam_attn(ctypes.byref(params), q.data_ptr(), strides[0], ctypes.byref(c), ctypes.byref(s), _take(what, "out", out, torch.bfloat16, n * heads * d, gpu),
