@@ -500,13 +500,14 @@ __device__ __forceinline__ uint32_t fork_column(const ForkArgs& a, const ForkRow
 __device__ __forceinline__ int fork_most(const ForkRow& r) { return max(r.old, max(r.had, r.col + 1)); }
 
 // A thread for each row, as many whole groups at a time as 1024 hold.  Latency is all: the numbers, the parent's length, the open page's entry, two sums, a page of the queue: 6.2 us for one group,
-// 7.3 for 64 of 4 rows, 16 for 8 of 32, whose rows look at each other's pages one after the other.
+// 6.6 for 64 of 4 rows, 9.1 for 8 of 32 (a row's numbers one word after the other, each asked for only if the one before called for it: 16).
 // ALL: the workgroup changes the tables as well, a thread for a column of a group, and gives the pages back; for few rows, whose launches would take longer.
 constexpr int FORK_ALL_WIDTH = 8;          // rows of a group that it has LDS for
 template <bool ALL>
 __global__ __launch_bounds__(PLAN_THREADS) void kv_fork_kernel(ForkArgs a) {
     __shared__ int64_t scratch[3][2][PLAN_THREADS / 64];
-    __shared__ int32_t s_src[PLAN_THREADS], s_had[PLAN_THREADS], s_page[PLAN_THREADS], s_col[PLAN_THREADS], s_need[PLAN_THREADS], s_most;
+    __shared__ i32x4 s_open[PLAN_THREADS];                 // of a row: whose tokens it takes, in how many pages, the page that it is to write into (-1: none with tokens), and its column
+    __shared__ int32_t s_need[PLAN_THREADS], s_most;
     __shared__ ForkRow s_rows[ALL ? PLAN_THREADS : 1];
     __shared__ int32_t s_entry[ALL ? FORK_ALL_WIDTH : 1][PLAN_THREADS];
     const int tid = threadIdx.x, round = PLAN_THREADS / a.width * a.width, mate0 = tid - tid % a.width;
@@ -527,22 +528,21 @@ __global__ __launch_bounds__(PLAN_THREADS) void kv_fork_kernel(ForkArgs a) {
         int page = -1;                                     // that the new token goes to, where it holds tokens
         if (wants && off) page = a.table[(int64_t)src * a.max_pages + col];
         const bool open = (uint32_t)page < (uint32_t)a.n_pages;
-        s_src[tid] = src;
-        s_had[tid] = pages_of(kept);
-        s_page[tid] = open ? page : -1;
-        s_col[tid] = col;
+        s_open[tid] = i32x4{src, pages_of(kept), open ? page : -1, col};
         __syncthreads();
         bool copy = false;
         if (open) {
             int holders = 0, writers = 0;
             bool lowest = true;
+#pragma unroll 4
             for (int t = mate0; t < mate0 + a.width; ++t) {
-                if (s_src[t] < 0 || s_had[t] <= col) continue;
-                const bool writes = s_col[t] == col && s_page[t] == page;
+                const i32x4 r = s_open[t];
+                const bool there = r[0] >= 0 && r[1] > col, here_too = r[3] == col, writes = there && here_too && r[2] == page;
                 writers += writes;
+                holders += writes;
+                lowest &= !(writes && t < tid);
                 // (who writes elsewhere in this column holds another page there)
-                holders += writes || (!(s_col[t] == col && s_page[t] >= 0) && a.table[(int64_t)s_src[t] * a.max_pages + col] == page);
-                if (writes && t < tid) lowest = false;
+                if (there && !(here_too && r[2] >= 0)) holders += a.table[(int64_t)r[0] * a.max_pages + col] == page;
             }
             copy = !(lowest && holders == writers);
         }
