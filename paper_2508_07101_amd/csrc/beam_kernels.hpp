@@ -161,8 +161,8 @@ struct Best {
 };
 
 // A wave for a part of a row.  One pass: the largest logit and the sum of weights relative to it, a pair in every lane; the best tokens, one in every lane,
-// in falling order.  R loads of 16 bytes a lane are looked at in a step.  Of the step's logits only those above the n-th best so far matter; where n lanes or more have such
-// ones, their maxima are sorted: the n-th largest of them bounds the step's n best from below, and leaves few.  Those few are gathered in LDS, sorted 64 at a time and merged.
+// in falling order.  R loads of 16 bytes a lane are looked at in a step.  Of the step's logits only those above a bound matter that n logits reach; where many lanes have such
+// ones, their maxima are sorted: the n-th largest of them is the next bound, and leaves few.  Those few are gathered in LDS, and when there are enough sorted 64 at a time and merged.
 // A weight is 2^((x - ref) log2 e): the difference first, so that rows that differ by a constant have the same sums, whatever the constant.  A lane's ref is a logit of its own
 // that follows the largest when that is 8 above it.  So an exponent is 12 above 0 at most, and below 0 by as much as the row's entropy in bits and one or two more in the weighted mean: its three
 // roundings (difference, product, constant) move the sum by less than 2^-17 of itself, or 2^-16.5 with 2^31 tokens.
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
     constexpr int HALF = R < 4 ? R : 4;
     const u32x4 none = {X::NONE, X::NONE, X::NONE, X::NONE};
 
-    float ref = -INFINITY, top = -INFINITY;
+    float ref = -INFINITY, top = -INFINITY, seen = -INFINITY;   // seen: there are n logits or more that are not below it
     double sum = 0.0;
     auto follow = [&](float largest) {
         top = fmaxf(top, largest);
@@ -241,12 +241,11 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
             for (int r = r0; r < r0 + HALF; ++r) asm volatile("" : "+v"(x[r]));   // (what is taken apart is not kept for the search below, which mostly looks at none of it)
         }
         // The tokens that may be among the n best.  (Tokens of later steps are larger: of equal logits those that are there already come first.)
-        const uint64_t last = lane_key(best.list, a.n - 1);
-        float least = above(last ? key_logit(last) : -INFINITY);
+        float least = above(seen);
         const int lanes = __popcll(__ballot(largest >= least));
         if (lanes == 0) return;
-        const bool bound = lanes >= a.n;
-        if (bound) least = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sort_lanes<true>(largest)), a.n - 1));   // (not below the old one: n lanes are)
+        const bool bound = lanes >= min(2 * a.n, 64);      // (fewer are not worth a sort)
+        if (bound) seen = least = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sort_lanes<true>(largest)), a.n - 1));   // (not below the old one: n lanes are)
         const int before = best.n;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -311,7 +310,11 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
             const bool hit = y > -INFINITY;
             best.add(hit, __ballot(hit), beam_key(y, i));
         }
-        if (best.n >= 32 || v0 == begin || ends) best.flush();
+        if (best.n >= 64 || ends) {
+            best.flush();
+            const uint64_t last = lane_key(best.list, a.n - 1);
+            if (last) seen = fmaxf(seen, key_logit(last));
+        }
         if (ends) break;
     }
     const float all = over_lanes(top, [](float x, float y) { return fmaxf(x, y); });
