@@ -166,9 +166,9 @@ struct Best {
 // A weight is 2^((x - ref) log2 e): the difference first, so that rows that differ by a constant have the same sums, whatever the constant.  A lane's ref is a logit of its own
 // that follows the largest when that is 8 above it.  So an exponent is 12 above 0 at most, and below 0 by as much as the row's entropy in bits and one or two more in the weighted mean: its three
 // roundings (difference, product, constant) move the sum by less than 2^-17 of itself, or 2^-16.5 with 2^31 tokens.
-// Bound by what a wave does between its loads, four waves to a SIMD: 512 rows of 131072 bf16 logits, 134 MB: 31 us, 4.3 TB/s (a plain read 19.6 us), with vector instructions under way for 20.5 us of
-// it.  Asking for the next step's logits before this one's search: 37 us.  A rougher bound from maxima over groups of lanes instead of the sort: 14 % fewer instructions and as long, and with
-// nine logits in ten masked 26 us for 17, for the keys that it lets through.
+// Bound by its instructions, four waves to a SIMD: 512 rows of 131072 bf16 logits, 134 MB: 30 us, 4.5 TB/s (a plain read 19.6 us), vector instructions under way for 79 % of the CUs' busy time; without the
+// search for the best 25 us.  The list sorted after each step instead of a running bound 32 us; the next step's logits asked for before this one's search 39, for the registers; by four loads 36; a bound from
+// maxima over groups of lanes instead of the sort as long, and with nine logits in ten masked 26 us for 17, for the keys that it lets through; weights by one multiply-add as long.
 template <int DTYPE, int R>
 __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) {
     typedef Logits<DTYPE> X;
@@ -685,8 +685,8 @@ struct CopyArgs {
 };
 static_assert(sizeof(CopyArgs) <= 4096, "a launch's arguments");
 
-// A workgroup for a copy in a layer: 16 lanes a row of 256 bytes, eight rows of theirs under way.  Bound by memory: 256 pages of 1 to 15 tokens, a quarter of them none, 8 KV heads, 32 layers: 106 us, 4.36 TB/s read and
-// written (with 8 tokens in each 4.94, a plain copy of a large tensor 5.08).  Four pages of 36 layers: 5.7 us, a launch's own time.
+// A workgroup for a copy in a layer: 16 lanes a row of 256 bytes, eight rows of theirs under way.  Bound by memory: 256 pages of 1 to 15 tokens, a quarter of them none, 8 KV heads, 32 layers, 403 MB read and
+// written: 103.5 us, 3.9 TB/s (a plain copy of a large tensor 5.08).  Four rows under way 109 us, sixteen 138; stores that the caches keep 106.  Four pages of 36 layers: 5.6 us, a launch's own time.
 __global__ __launch_bounds__(COPY_THREADS) void kv_copy_kernel(CopyArgs a) {
     const CopyLayer& l = a.layer[blockIdx.y];
     const i32x4 copy = *reinterpret_cast<const i32x4*>(a.copies + (int64_t)blockIdx.x * 4);
@@ -711,7 +711,7 @@ __global__ __launch_bounds__(COPY_THREADS) void kv_copy_kernel(CopyArgs a) {
         }
 #pragma unroll
         for (int j = 0; j < RUN; ++j)
-            if (r0 + j * STEP < 2 * rows) *reinterpret_cast<u32x4*>(pool[j] + to * page + at[j]) = x[j];
+            if (r0 + j * STEP < 2 * rows) __builtin_nontemporal_store(x[j], reinterpret_cast<u32x4*>(pool[j] + to * page + at[j]));
     }
 }
 
