@@ -138,7 +138,7 @@ __device__ __forceinline__ void lds_of_wave() {            // what the wave's ot
 }
 
 // The best 64 of a wave's keys, one in every lane, in falling order; keys are gathered in LDS until they are enough for a sort.
-constexpr int FOUND = 384;
+constexpr int FOUND = 400, FOUND_ENDS = 16;               // of these for what stands at a row's ends: a search leaves them free
 struct Best {
     uint64_t* found;
     uint64_t list = 0;
@@ -183,6 +183,7 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
     const int head = min((int)((16 - ((uintptr_t)base & 15)) & 15) / X::SIZE, a.vocab);   // logits before the first 16 bytes that are aligned
     const int whole = (a.vocab - head) / PER, tail = a.vocab - head - whole * PER;
     const u32x4* const body = reinterpret_cast<const u32x4*>(base + head * X::SIZE);
+    static_assert(2 * (PER - 1) <= FOUND_ENDS, "logits at the ends");
     const int begin = min(part * a.part_len, whole), end = min(begin + a.part_len, whole);
     constexpr int HALF = R < 4 ? R : 4;
     const u32x4 none = {X::NONE, X::NONE, X::NONE, X::NONE};
@@ -258,7 +259,7 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
                 if (const uint64_t who = __ballot(hit)) best.add(hit, who, beam_key(y, token + k));
             }
         }
-        if (best.n > FOUND) {                             // more than there is room for: those above the bound 64 at a time, and of those that are equal to it the first n
+        if (best.n > FOUND - FOUND_ENDS) {                // more than there is room for: those above the bound 64 at a time, and of those that are equal to it the first n
             best.n = before;
             if (best.n > 0) best.flush();
 #pragma unroll 1

@@ -58,6 +58,25 @@ def test_selection_of_many_equal_logits(vocab, kind):
         _check_select(torch.tensor(x, device=DEV).to(kind), torch.zeros(8, device=DEV), 1, n)
 
 
+@pytest.mark.parametrize("kind,at", [(torch.bfloat16, 0), (torch.bfloat16, 3), (torch.float32, 1)])
+def test_selection_of_as_many_logits_as_there_is_room_for(kind, at):
+    """Rows with 370 to 410 logits that a search keeps, and the best ones at their ends, which are looked at last."""
+    vocab, rows = 64 * 8 + 9, 48
+    rng = np.random.default_rng(at)
+    x = np.full((rows, vocab), -5.0, dtype=np.float32)
+    for r in range(rows):
+        low = np.r_[200:224, 456:480]                            # a lane's, whose best is the bound: 1.0
+        some = np.setdiff1d(np.arange(8, vocab - 8), low)
+        some = rng.permutation(some)[: 368 + r - len(low)]
+        x[r, some], x[r, low] = 1.0 + (1 + rng.permutation(len(some))) / 64.0, 1.0
+        x[r, :3], x[r, -4:] = 9.0 + np.arange(3) / 8.0, 9.5 + np.arange(4) / 8.0
+    flat = torch.zeros(rows * vocab + at, device=DEV).to(kind)
+    logits = flat[at:].view(rows, vocab)
+    logits.copy_(torch.tensor(x, device=DEV))
+    for n in (64, 63):
+        _check_select(logits, torch.zeros(rows, device=DEV), 1, n)
+
+
 @pytest.mark.parametrize("width", WIDTHS)
 @pytest.mark.parametrize("H,G", [(8, 8), (16, 2)])
 def test_attention(width, H, G):
