@@ -146,7 +146,7 @@ __device__ __forceinline__ float of_row_max(float v) {      // over the four lan
 // Weights are two bf16 numbers each, as in tree_rows for few rows.  The reference m follows the maximum when that is 2^8 above it.
 // K goes to registers, V to LDS, both for the next tile as soon as this one's scores are there; eight waves on a CU have 128 KB under way.  Waves meet at the end alone.
 // Bound by memory: 64 groups of 4 beams, prompts of 8192 to 32768 tokens, 32 query heads on 8: 5.7 GB of pages in 925 us, 6.2 TB/s (a plain read 836 us); 8 groups of 8 samples, 2048 tokens and up to 8192
-// of their own: 175 us (162).  A short search, 4 beams of 4096 tokens: 10 us and 4.5 for the merge (2.7), a chain of waits: list, pages, sums.
+// of their own: 175 us (162).  A short search, 4 beams of 4096 tokens: 9 us and 4.3 for the merge (2.7), a chain of waits: list, pages, sums.
 // Rows beyond 32 are other workgroups', which read the pages again, mostly from their XCD's L2: 4 groups of 32 samples 118 us (one workgroup for all rows that share a KV head, the tiles in LDS: 162), 8 groups of
 // 32 beams of 4096 tokens 67 (61), of 64 query heads 112 (105); the blocks one after the other in a workgroup 139, 252 and 222.
 // K past the caches 1003 us for the 965 of then; one buffer for V and three workgroups on a CU: as long; eight waves on one workgroup's pages 908 for 926, but 180 for 175 and 28 for 24 on 64 groups of 500 tokens.
@@ -400,14 +400,48 @@ __global__ __launch_bounds__(BEAM_ATTN_THREADS, 2) void beam_attn_kernel(BeamAtt
     }
 }
 
-// A wave for a row.
+// A wave for a row: a lane for each piece's weight, then two columns a lane, eight pieces asked for at once, and the last ones by four.
 constexpr int BEAM_REDUCE_WAVES = 4;
 __global__ __launch_bounds__(64 * BEAM_REDUCE_WAVES) void beam_reduce_kernel(BeamAttnArgs a) {
-    const int b = blockIdx.y, pieces = a.pieces[b];
+    const int b = blockIdx.y, pieces = a.pieces[b], lane = threadIdx.x & 63;
     if (pieces <= 1) return;
     for (int r = blockIdx.x * BEAM_REDUCE_WAVES + (threadIdx.x >> 6); r < a.width * a.H; r += gridDim.x * BEAM_REDUCE_WAVES) {
         const int64_t row = (int64_t)b * a.width * a.H + r, first = row * a.n_splits;
-        merge_pieces(a.part_acc + first * D, a.part_ml + first * 2, pieces, a.out + row * D, threadIdx.x & 63);
+        const float* const part = a.part_acc + first * D + lane * 2;
+        const f32x2 ml = lane < pieces ? *reinterpret_cast<const f32x2*>(a.part_ml + (first + lane) * 2) : f32x2{LOWEST, 0.0f};
+        float top = ml[0];
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+        const float w = exp2f(ml[0] - top);
+        float sum = lane < pieces ? w * ml[1] : 0.0f;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+        f32x2 acc = {0.0f, 0.0f};
+        auto add = [&](int p, f32x2 v, bool is) {          // (a sum that is infinite stays so whatever its piece weighs)
+            const float wp = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), p));
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float x = __builtin_isfinite(v[j]) ? wp * v[j] : v[j];
+                acc[j] += is ? x : 0.0f;
+            }
+        };
+        int p = 0;
+        for (; p + 8 <= pieces; p += 8) {
+            f32x2 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const f32x2*>(part + (p + i) * D);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) add(p + i, v[i], true);
+        }
+        for (; p < pieces; p += 4) {
+            f32x2 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const f32x2*>(part + min(p + i, pieces - 1) * D);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) add(min(p + i, pieces - 1), v[i], p + i < pieces);
+        }
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        *reinterpret_cast<uint32_t*>(a.out + row * D + lane * 2) = (uint32_t)f32_to_bf16_rne(acc[0] * inv) | (uint32_t)f32_to_bf16_rne(acc[1] * inv) << 16;
     }
 }
 

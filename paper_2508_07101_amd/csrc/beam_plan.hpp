@@ -11,14 +11,15 @@ constexpr int BEAM_ROWS = 32;           // rows (row of the group, query head) o
 constexpr int BEAM_CUS = 256;
 constexpr int BEAM_LIST = 8192;         // pages of a piece: a bit each in LDS
 constexpr int BEAM_MAX_SPLITS = 64;     // pieces of a group's pages: one lane each in the merge
-constexpr int BEAM_MIN_PIECE = 256;     // tokens
+constexpr int BEAM_MIN_PIECE = 128;     // tokens: a tile for each wave (4 beams of 4096 tokens 7.8 us, by 256 8.8; 8 of 2000 9.9 and 11.6; longer ones alike)
 constexpr int BEAM_PIECE_COST = 16;     // tiles of 32 tokens that a piece costs besides its own
 inline bool beam_pages_served(int64_t pages) { return pages <= (int64_t)BEAM_LIST * BEAM_MAX_SPLITS; }
 
-// The host knows no more than width * max_seq_len tokens, of which rows that share have a fraction: a group stays whole up to a bound that costs little if they share nothing (4 beams of one group,
-// 8 KV heads: 1000 tokens whole 14.2 us, cut and merged 14.4; 700: 10.8 and 12.4; 1550: 17.7 and 14.8), a higher one where half of the CUs have a workgroup anyway (16 groups of 4 beams: 600 tokens, bound 2600,
-// whole 13.2, cut 16.5; 1000, bound 4100, 17.1 and 19.9).  Where all have two already, pieces only make up for lengths.
-constexpr int BEAM_WHOLE = 2048, BEAM_WHOLE_MANY = 4096;   // tokens
+// The host knows no more than a bound, width * max_seq_len tokens or the pool's, of which rows that share have a fraction.  Few groups stay whole up to a bound that costs little whether it is near the truth or far above it,
+// a lower one where a workgroup has more than 16 rows; many up to a higher one.  Us a call, whole and cut, 8 KV heads: one group of 4 beams, 500 tokens 10.4 and 14.5, 900 12.6 and 14.2, 1200 15.6 and 14.1, 1700 19.8 and 14.0;
+// of 8 beams (32 rows) 400 12.5 and 13.8, 600 14.1 and 13.9, 1000 18.1 and 13.6; 4 groups of 4, bound 1800, 500 tokens 10.0 and 13.9; 16 of 4, 1200 19.0 and 20.9, 2700 34 and 34; 24 of 4 28 and 31 at 1700.
+// Where all CUs have two workgroups, pieces only make up for lengths.
+constexpr int BEAM_WHOLE = 1280, BEAM_WHOLE_WIDE = 768, BEAM_WHOLE_MANY = 4096;   // tokens
 
 struct BeamPlan {
     int blocks;      // workgroups that share a KV head's pages
@@ -31,7 +32,7 @@ inline BeamPlan plan_beams(int64_t max_pages, int groups, int G, int rows) {
     const int64_t wgs = (int64_t)groups * G * p.blocks;
     const int64_t want = groups == 1 ? 2 * BEAM_CUS / wgs : wgs >= 16 * BEAM_CUS ? 1 : std::max<int64_t>(4, 4 * BEAM_CUS / wgs);
     const int64_t by_list = (max_pages + BEAM_LIST - 1) / BEAM_LIST, least = wgs >= 2 * BEAM_CUS ? 4096 : BEAM_MIN_PIECE;
-    const int64_t pieces = max_len <= (wgs >= BEAM_CUS / 2 ? BEAM_WHOLE_MANY : BEAM_WHOLE) ? 1 : (max_len + least - 1) / least;
+    const int64_t pieces = max_len <= (wgs >= BEAM_CUS / 2 ? BEAM_WHOLE_MANY : rows <= 16 ? BEAM_WHOLE : BEAM_WHOLE_WIDE) ? 1 : (max_len + least - 1) / least;
     p.n_splits = (int)std::max<int64_t>({1, by_list, std::min<int64_t>({want, pieces, BEAM_MAX_SPLITS})});
     return p;
 }

@@ -1143,7 +1143,40 @@ __global__ __launch_bounds__(64 * REDUCE_WAVES) void tree_reduce_kernel(TreeArgs
     if (pieces <= 1) return;
     for (int r = blockIdx.x * REDUCE_WAVES + (threadIdx.x >> 6); r < n * a.H; r += gridDim.x * REDUCE_WAVES) {
         const int64_t row = (int64_t)start * a.H + r, first = ((int64_t)part_row(a, b, start) * a.H + r) * a.n_splits;
-        merge_pieces(a.part_acc + first * D, a.part_ml + first * 2, pieces, a.out + row * D, lane);
+        float m = LOWEST, l = 0.0f;
+        if (lane < pieces) {
+            const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + (first + lane) * 2);
+            m = ml[0];
+            l = ml[1];
+        }
+        float top = m;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+        const float w = exp2f(m - top);
+        float sum = lane < pieces ? w * l : 0.0f;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+        f32x2 acc = {0.0f, 0.0f};
+        // (a sum that is infinite stays so whatever its piece weighs: the weight is not 0, also where 32 bits hold nothing of it)
+        auto add = [&](float wp, f32x2 v) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[j] += __builtin_isfinite(v[j]) ? wp * v[j] : v[j];
+        };
+        const float* part = a.part_acc + first * D + lane * 2;
+        int p = 0;
+        for (; p + 8 <= pieces; p += 8) {                         // eight at a time under way
+            f32x2 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const f32x2*>(part + (p + i) * D);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) add(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), p + i)), v[i]);
+        }
+        for (; p < pieces; ++p) {
+            const f32x2 v = *reinterpret_cast<const f32x2*>(part + p * D);
+            add(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), p)), v);
+        }
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        *reinterpret_cast<uint32_t*>(a.out + row * D + lane * 2) = (uint32_t)f32_to_bf16_rne(acc[0] * inv) | (uint32_t)f32_to_bf16_rne(acc[1] * inv) << 16;
     }
 }
 

@@ -201,7 +201,7 @@ def test_attention_over_long_lists():
 
 @pytest.mark.parametrize("rows,G", [(1, 8), (16, 8), (256, 1), (65535, 1)])
 def test_workspaces_grow_with_the_lists(rows, G):
-    """A piece for each 256 tokens and no more than 64: a workspace made for longer sequences serves shorter ones."""
+    """A piece for each 128 tokens and no more than 64: a workspace made for longer sequences serves shorter ones."""
     lib, width = cb.load(), 1
     sizes = []
     for max_len in (1, 16, 1000, 2048, 2049, 4096, 4097, 10000, 1 << 17, 1 << 20, 1 << 23):
