@@ -128,7 +128,7 @@ struct Logits {
     }
 };
 
-constexpr int BEAM_WAVES = 4;
+constexpr int BEAM_WAVES = 4, BOUND_BY_LANES = 32;
 constexpr float LOG2E = 1.4426950408889634f;
 
 __device__ __forceinline__ void lds_of_wave() {            // what the wave's other lanes wrote to LDS is there
@@ -162,7 +162,8 @@ struct Best {
 
 // A wave for a part of a row.  One pass: the largest logit and the sum of weights relative to it, a pair in every lane; the best tokens, one in every lane,
 // in falling order.  R loads of 16 bytes a lane are looked at in a step.  Of the step's logits only those above a bound matter that n logits reach; where many lanes have such
-// ones, their maxima are sorted: the n-th largest of them is the next bound, and leaves few.  Those few are gathered in LDS, and when there are enough sorted 64 at a time and merged.
+// ones, their maxima are sorted: the n-th largest of them is the next bound, and leaves few; for more than BOUND_BY_LANES places that of all loads' maxima, found bit by bit.  (64 places, where the lanes' least maximum leaves
+// hundreds: 256 rows of 32000 logits 28 us, so 13; 4 rows of 128000 21 and 9.5; 32 places 8.4 and 9.6 for 32 rows of 128000.)  Those few are gathered in LDS, and when there are enough sorted 64 at a time and merged.
 // A weight is 2^((x - ref) log2 e): the difference first, so that rows that differ by a constant have the same sums, whatever the constant.  A lane's ref is a logit of its own
 // that follows the largest when that is 8 above it.  So an exponent is 12 above 0 at most, and below 0 by as much as the row's entropy in bits and one or two more in the weighted mean: its three
 // roundings (difference, product, constant) move the sum by less than 2^-17 of itself, or 2^-16.5 with 2^31 tokens.
@@ -246,7 +247,25 @@ __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) 
         const int lanes = __popcll(__ballot(largest >= least));
         if (lanes == 0) return;
         const bool bound = lanes >= min(2 * a.n, 64);      // (fewer are not worth a sort)
-        if (bound) seen = least = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sort_lanes<true>(largest)), a.n - 1));   // (not below the old one: n lanes are)
+        if (bound && a.n <= BOUND_BY_LANES) {
+            seen = least = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sort_lanes<true>(largest)), a.n - 1));   // (not below the old one: n lanes are)
+        } else if (bound) {                                // the n-th largest of the loads' maxima, to 16 bits, bit by bit
+            uint32_t of[R], t = 0;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const uint32_t u = __float_as_uint(most[r]);
+                of[r] = ((int32_t)u < 0 ? ~u : u | 0x80000000u) >> 16;
+            }
+#pragma unroll 1
+            for (uint32_t bit = 0x8000; bit; bit >>= 1) {
+                int count = 0;
+#pragma unroll
+                for (int r = 0; r < R; ++r) count += __popcll(__ballot(of[r] >= (t | bit)));
+                if (count >= a.n) t |= bit;
+            }
+            const float by = __uint_as_float((t & 0x8000) ? (t ^ 0x8000) << 16 : ~(t << 16));   // the smallest with these 16 bits
+            seen = least = fmaxf(least, by);
+        }
         const int before = best.n;
 #pragma unroll
         for (int r = 0; r < R; ++r) {

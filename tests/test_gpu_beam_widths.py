@@ -59,7 +59,8 @@ def test_selection_of_many_equal_logits(vocab, kind):
 
 
 @pytest.mark.parametrize("kind,at", [(torch.bfloat16, 0), (torch.bfloat16, 3), (torch.float32, 1)])
-def test_selection_of_as_many_logits_as_there_is_room_for(kind, at):
+@pytest.mark.parametrize("alike", [False, True])
+def test_selection_of_as_many_logits_as_there_is_room_for(kind, at, alike):
     """Rows with 370 to 410 logits that a search keeps, and the best ones at their ends, which are looked at last."""
     vocab, rows = 64 * 8 + 9, 48
     rng = np.random.default_rng(at)
@@ -68,7 +69,7 @@ def test_selection_of_as_many_logits_as_there_is_room_for(kind, at):
         low = np.r_[200:224, 456:480]                            # a lane's, whose best is the bound: 1.0
         some = np.setdiff1d(np.arange(8, vocab - 8), low)
         some = rng.permutation(some)[: 368 + r - len(low)]
-        x[r, some], x[r, low] = 1.0 + (1 + rng.permutation(len(some))) / 64.0, 1.0
+        x[r, some], x[r, low] = 1.0 if alike else 1.0 + (1 + rng.permutation(len(some))) / 64.0, 1.0
         x[r, :3], x[r, -4:] = 9.0 + np.arange(3) / 8.0, 9.5 + np.arange(4) / 8.0
     flat = torch.zeros(rows * vocab + at, device=DEV).to(kind)
     logits = flat[at:].view(rows, vocab)
