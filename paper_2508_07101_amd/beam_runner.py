@@ -17,14 +17,18 @@ class BeamRunner:
 
     A prompt comes in by ``admit``, ``append`` for each layer, and ``spread``.  A step is ``select`` from the last tokens' logits and ``fork`` (or ``step``, which is both), then
     ``layer`` for each layer in order.  ``parents`` and ``tokens`` are what ``select`` chose, for the caller's own account; ``scores`` and ``ended`` belong to the rows as they are now.
-    Everything is enqueued on the current stream; nothing here waits for the GPU.  A row that has ended keeps its tokens and gets no new one (its slot is -1); a
-    group that found no page stays as it was (``granted`` is 0): a caller whose pool may run out looks at it after ``fork``, since ``scores`` are the chosen ones' already.
+    Everything is enqueued on the current stream; nothing here waits for the GPU.  A row that has ended keeps its tokens and gets no new one (its slot is -1).
+    A group that found no page keeps its rows (``granted`` is 0).  With ``hold`` it keeps all that belongs to them: ``fork`` puts its scores and ends back, its ``parents`` are
+    the rows themselves and its ``tokens`` -1, so that the same logits make the same choice in a later step, which finds pages or waits again; a caller's account that follows
+    ``parents`` and ``tokens`` is right either way, and a captured step needs no host in between.  That is what a pool that may run out wants.  Without it ``scores``, ``ended``,
+    ``parents`` and ``tokens`` of such a group are the chosen ones', which its rows do not have: it can be finished, but a further step would go on from scores of other rows.
     ``finish`` gives the pages of whole groups back.
     """
 
-    def __init__(self, params: cb.CusaParams, width: int, schedule: Sequence[int], n_pages: int, max_pages: int, vocab: int, end_token: int = -1, device="cuda"):
+    def __init__(self, params: cb.CusaParams, width: int, schedule: Sequence[int], n_pages: int, max_pages: int, vocab: int, end_token: int = -1, device="cuda",
+                 hold: bool = False):
         b, g = params.batch, params.n_kv_heads
-        self.params, self.width, self.schedule, self.end_token, self.n_pages = params, width, list(schedule), end_token, n_pages
+        self.params, self.width, self.schedule, self.end_token, self.n_pages, self.hold = params, width, list(schedule), end_token, n_pages, hold
 
         def ints(*shape):
             return torch.zeros(shape, dtype=torch.int32, device=device)
@@ -32,6 +36,7 @@ class BeamRunner:
         self.pool = cb.PagePool.empty(b, max_pages, n_pages, device)
         self.lens, self.kept, self.parents, self.tokens, self.ended, self.granted = ints(b), ints(b), ints(b), ints(b), ints(b), ints(b // width)
         self.scores = torch.full((b,), float("-inf"), device=device)
+        self.old_scores, self.old_ended, self.none = torch.empty_like(self.scores), ints(b), ints(b) - 1     # (with hold: before the choice)
         self.slots = torch.full((b,), -1, dtype=torch.int64, device=device)
         self.copies, self.tok_start = ints(b, 4), ints(b + 1)
         self.own = torch.arange(b, dtype=torch.int32, device=device) % width     # every row its own parent
@@ -74,6 +79,9 @@ class BeamRunner:
         """The width best continuations of every group: parents, tokens, and the rows' next scores and ends.  logits [rows, vocab]."""
         shape = (self.params.batch // self.width, self.width)
         ended = self.ended if self.end_token >= 0 else None
+        if self.hold:
+            self.old_scores.copy_(self.scores)
+            self.old_ended.copy_(self.ended)
         cb.beam_select(logits, self.scores, self.width, self.scores.view(shape), self.parents.view(shape), self.tokens.view(shape), self.beam_ws, ended,
                        None if ended is None else ended.view(shape), self.end_token)
 
@@ -81,6 +89,11 @@ class BeamRunner:
         """The caches follow the choice: tables by parents, a slot for every row's token, pages that two rows would write to copied in all layers, and
         the list of pages that the layers' attention goes by."""
         self._fork(self.parents, self.ended, True)
+        if self.hold:
+            refused = self.granted.view(-1, 1) == 0
+            for now, old in ((self.scores, self.old_scores), (self.ended, self.old_ended), (self.parents, self.own), (self.tokens, self.none)):
+                now, old = now.view(-1, self.width), old.view(-1, self.width)
+                now.copy_(torch.where(refused, old, now))
         self.copy.run(self.copies)
         self.list_pages()
 
