@@ -68,7 +68,8 @@ class BeamRunner:
 
     def spread(self, new: torch.Tensor):
         """The admitted prompts become those of all rows of their groups; new: int32 or bool [groups], which groups these are.  Their search starts with one beam:
-        the first selection takes its continuations from the logits of the group's first row."""
+        the first selection takes its continuations from the logits of the group's first row.  A group whose prompt found no room has no tokens and stays as it was."""
+        new = (new != 0) & (self.lens[:: self.width] > 0)
         rows = new.to(torch.int32).repeat_interleave(self.width)
         self._fork(torch.where(rows != 0, torch.zeros_like(self.own), self.own), None, False)
         start = torch.where(self.first != 0, torch.zeros_like(self.scores), torch.full_like(self.scores, float("-inf")))
