@@ -425,7 +425,8 @@ cusa_status cusa_shared_pages(const cusa_kv* kv, int32_t batch, const cusa_share
  * q: device bf16, row b head h at q + b * q_stride + h * 128 (q_stride a multiple of 8, >= n_q_heads * 128); out: device bf16 [batch][n_q_heads][128].  params->batch: rows, a multiple of
  * width.  kv's block_table is not read.  ws: cusa_beam_attn_workspace_bytes, 256-byte aligned, content not preserved.
  * Errors as cusa_full_attn, and UNSUPPORTED for contiguous caches, width > 32, pools of 2^31 or more rows, more than 524288 pages
- * in a group, min(max_entries, width * ceil(max_seq_len / 16)), and more than 2^24 workgroups (rows times KV heads, at most). */
+ * in a group, min(max_entries, width * ceil(max_seq_len / 16)), and 2^24 workgroups or more, of which the workspace's size depends too and which it refuses as well: KV heads times
+ * groups, times the rows of a group that share a KV head by 32 (rounded up), times the pieces that a group's list may be cut into (64 at most; of many groups one for each 8192 pages). */
 cusa_status cusa_beam_attn_workspace_bytes(const cusa_params* params, int32_t max_seq_len, const cusa_shared* shared, size_t* bytes);
 cusa_status cusa_beam_attn(const cusa_params* params, const void* q, int64_t q_stride, const cusa_kv* kv, const cusa_shared* shared, void* out,
                            void* ws, size_t ws_bytes, void* stream);

@@ -257,7 +257,9 @@ cusa_status cusa_beam_attn_workspace_bytes(const cusa_params* params, int32_t ma
     const int64_t pages = group_pages(shared, max_seq_len);
     if (!beam_pages_served(pages)) return CUSA_ERR_UNSUPPORTED;
     const int groups = params->batch / shared->width, g = params->n_q_heads / params->n_kv_heads;
-    *bytes = beam_attn_workspace(plan_beams(pages, groups, params->n_kv_heads, shared->width * g), params->batch, params->n_q_heads, groups).total;
+    const BeamPlan pl = plan_beams(pages, groups, params->n_kv_heads, shared->width * g);
+    if (!beam_units_served(beam_units(pl, groups, params->n_kv_heads))) return CUSA_ERR_UNSUPPORTED;
+    *bytes = beam_attn_workspace(pl, params->batch, params->n_q_heads, groups).total;
     return CUSA_OK;
 }
 
@@ -275,6 +277,8 @@ cusa_status cusa_beam_attn(const cusa_params* params, const void* q, int64_t q_s
     const int64_t pages = group_pages(shared, kv->max_seq_len);
     if (!beam_pages_served(pages)) return CUSA_ERR_UNSUPPORTED;
     const BeamPlan pl = plan_beams(pages, groups, G, width * g);
+    const int64_t units = beam_units(pl, groups, G);
+    if (!beam_units_served(units)) return CUSA_ERR_UNSUPPORTED;
     const BeamAttnWs w = beam_attn_workspace(pl, params->batch, params->n_q_heads, groups);
     if ((st = check_workspace(ws, ws_bytes, w.total)) != CUSA_OK) return st;
     BeamAttnArgs a = {};
@@ -296,8 +300,6 @@ cusa_status cusa_beam_attn(const cusa_params* params, const void* q, int64_t q_s
     a.g_shift = g == 1 ? 0 : g == 2 ? 1 : g == 4 ? 2 : 3;
     a.blocks = pl.blocks;
     a.n_splits = pl.n_splits;
-    const int64_t units = ((int64_t)pl.n_splits * G * groups + 7) / 8 * 8 * pl.blocks;
-    if (units * BEAM_ATTN_THREADS > 0xffffffff) return CUSA_ERR_UNSUPPORTED;   // (threads of a launch)
     const dim3 grid((unsigned)units);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (width * g <= 16) launch(KID_BEAM_ATTN, beam_attn_kernel<1>, grid, BEAM_ATTN_THREADS, 0, s, a);

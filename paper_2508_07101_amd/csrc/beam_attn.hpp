@@ -114,6 +114,7 @@ struct BeamAttnLds {
     int32_t any_odd;
 };
 static_assert(BEAM_LIST / 32 == BEAM_ATTN_THREADS, "a thread clears a word");
+static_assert(BEAM_ATTN_THREADS == 256, "beam_units_served counts a launch's threads");
 
 // A tile: two pages of the list, uniform.
 struct BeamTile {

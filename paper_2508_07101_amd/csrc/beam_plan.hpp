@@ -37,6 +37,10 @@ inline BeamPlan plan_beams(int64_t max_pages, int groups, int G, int rows) {
     return p;
 }
 
+// Workgroups of the launch: blocks of rows for each piece and KV head, rounded up to 8 XCDs.  A launch has fewer than 2^32 threads.
+inline int64_t beam_units(const BeamPlan& p, int groups, int G) { return ((int64_t)p.n_splits * G * groups + 7) / 8 * 8 * p.blocks; }
+inline bool beam_units_served(int64_t units) { return units < 1 << 24; }
+
 // Bytes of partial results: 128 sums, a maximum and a denominator per row and piece.
 struct BeamAttnWs {
     size_t acc, ml, pieces, total;
