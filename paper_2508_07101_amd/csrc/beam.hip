@@ -62,7 +62,8 @@ constexpr int64_t FORK_ALL = 4096;
 // Columns that a workgroup changes, PLAN_THREADS entries, in FORK_COLS columns at most.
 constexpr int FORK_COLS = 256;
 int fork_rows(int32_t width) { return width <= 4 ? 4 : width <= 8 ? 8 : width <= 16 ? 16 : 32; }
-int64_t chunks_of(int64_t max_pages, int cols) { return (max_pages + cols - 1) / cols; }
+// Chunks of the columns that a row can have tokens in: lengths are 31 bits, and 2^30 columns would be more threads than a launch has.
+int64_t chunks_of(int64_t max_pages, int cols) { return (std::min<int64_t>(max_pages, (0x7fffffff + (int64_t)PAGE - 1) / PAGE) + cols - 1) / cols; }
 
 struct ForkWs {
     size_t rows, counts, freed, total;

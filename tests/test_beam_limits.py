@@ -32,3 +32,9 @@ def test_attention_of_as_many_as_it_has(rows, width, G, pages):
     size, n, lib, args = _need(rows, width, G, pages)
     assert size == cb.OK and n > 0
     assert lib.cusa_beam_attn(*args, n - 1, None) == cb.ERR_WORKSPACE_TOO_SMALL
+
+
+def test_forks_of_tables_with_more_columns_than_tokens_have_numbers():
+    """A row has 2^31 - 1 tokens at most, in 2^27 pages: columns behind those are nobody's, and no launch has threads for them (2^30 columns would be 2^32 threads)."""
+    for batch, most in ((1, 0x7fffffff), (2, 0x3fffffff), (15, 0x7fffffff // 15)):
+        assert cb.fork_workspace_bytes(batch, most) == cb.fork_workspace_bytes(batch, 1 << 27) > cb.fork_workspace_bytes(batch, (1 << 27) - 256)
