@@ -370,7 +370,8 @@ typedef struct {
  * and with ended[r] != 0 (ended NULL: no row has ended) only end_token, worth s.  A row whose score is not finite proposes nothing, and neither does one
  * that has not ended with a logit that is NaN or +infinity, or with none above -infinity.  Of equal ones the lower row's comes first, then the lower token.
  * out_scores, parents, tokens, out_ended: device [rows / width][n], best first: the value rounded to binary32, the row's number in its group, the token, and 1 if
- * the row had ended or the token is end_token (NULL: not wanted).  Behind the last: -infinity, -1, -1, 0.  With n = width these are the next step's rows: out_scores may
+ * the row had ended or the token is end_token (NULL: not wanted).  Of one row's tokens the order is always that of (logit, lower token); two rows whose values differ by less than the bound
+ * below may stand either way round.  Behind the last: -infinity, -1, -1, 0.  With n = width these are the next step's rows: out_scores may
  * be scores and out_ended may be ended then.  The sum of a row: terms and sums of up to 64 of them in binary32, all else in binary64, so that a value is off by 2^-16
  * at most before it is rounded.  scores: device float [rows].  ws: cusa_beam_workspace_bytes, 256-byte aligned.  ended needs an end_token.
  * Errors: INVALID_ARG, UNSUPPORTED (width > 32, n > 64, rows > 65535), WORKSPACE_TOO_SMALL, LAUNCH. */
@@ -414,7 +415,7 @@ typedef struct {
 
 /* Each page of a group once: in order of the columns, then of the lowest row that holds it; entries of the table that name no page are left out, entries of the
  * list behind the last are not written.  Of kv, block_table, max_pages, page_size, n_pages, seq_lens and max_seq_len are read.  Once a step: the layers share their tables.
- * ws: cusa_shared_pages_workspace_bytes, 256-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL, LAUNCH. */
+ * ws: cusa_shared_pages_workspace_bytes, 256-byte aligned (no kernel of this build writes to it).  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL, LAUNCH. */
 size_t      cusa_shared_pages_workspace_bytes(int32_t batch, int32_t max_seq_len);
 cusa_status cusa_shared_pages(const cusa_kv* kv, int32_t batch, const cusa_shared* shared, void* ws, size_t ws_bytes, void* stream);
 

@@ -18,8 +18,8 @@ cusa_status check_workspace(const void* ws, size_t have, size_t need) {
     return have < need ? CUSA_ERR_WORKSPACE_TOO_SMALL : CUSA_OK;
 }
 
-// Parts of a row, a wave each: enough waves for the chip, but parts of 4 KB at least, and a lane each where they come together.  (512 rows of 131072 bf16 logits: 1024 waves 47 us,
-// 2048 35, 4096 31, 6144 35.  4 rows of 32000, selection and merge: parts of 2 KB 12.2, 4 KB 12.4, 8 KB 15.3; 52 rows of 67306 for 59 places: 20.8, 18.8, 24.5.)
+// Parts of a row, a wave each: enough waves for the chip, but parts of about 4 KB at least (3 KB where rows are little longer than a multiple of that; a last part is what is left), and a lane each where they come
+// together.  (512 rows of 131072 bf16 logits: 1024 waves 47 us, 2048 35, 4096 31, 6144 35.  Selection and merge of 4 rows of 32000 for 8 places: parts of 2 KB 12.7, 4 KB 12.3, 8 KB 12.5; 52 rows of 67306 for 59 places 21.5, 19, 24; 256 rows of 32000 for 64 places 39, 36.5, 44.)
 constexpr int PART_WAVES = 4096, PART_LEAST = 256;   // loads of 16 bytes
 struct BeamParts {
     int parts, len;                        // len: loads of 16 bytes
@@ -46,7 +46,7 @@ BeamWs beam_ws(int32_t rows, int parts, int32_t n) {
 template <int DTYPE>
 void launch_rows(hipStream_t s, const BeamArgs& a) {
     const dim3 grid((unsigned)(((int64_t)a.rows * a.parts + BEAM_WAVES - 1) / BEAM_WAVES));
-    // Eight loads a lane under way, or four where a part has no more.  (512 rows of 131072 bf16 logits: eight 31 us, four 35; 256 rows of 32000 for 64 places, parts of 4 KB: 36 and 28.)
+    // Eight loads a lane under way, or four where a part has no more.  (512 rows of 131072 bf16 logits: eight 31 us, four 35; parts of 4 KB: 256 rows of 32000 for 64 places 15 and 12.5, 52 rows of 67306 for 59 places 11.5 and 9.9.)
     if (a.part_len <= PART_LEAST) launch(KID_BEAM_ROWS, beam_rows_kernel<DTYPE, 4>, grid, 64 * BEAM_WAVES, 0, s, a);
     else launch(KID_BEAM_ROWS, beam_rows_kernel<DTYPE, 8>, grid, 64 * BEAM_WAVES, 0, s, a);
 }

@@ -146,10 +146,10 @@ __device__ __forceinline__ float of_row_max(float v) {      // over the four lan
 //   O^T += V^T P^T: the same lanes hold these tokens' weights, which is the operand's order if V's tokens are taken in it: transposing LDS reads of tokens 4 q .. of either page.
 // Weights are two bf16 numbers each, as in tree_rows for few rows.  The reference m follows the maximum when that is 2^8 above it.
 // K goes to registers, V to LDS, both for the next tile as soon as this one's scores are there; eight waves on a CU have 128 KB under way.  Waves meet at the end alone.
-// Bound by memory: 64 groups of 4 beams, prompts of 8192 to 32768 tokens, 32 query heads on 8: 5.7 GB of pages in 925 us, 6.2 TB/s (a plain read 836 us); 8 groups of 8 samples, 2048 tokens and up to 8192
-// of their own: 175 us (162).  A short search, 4 beams of 4096 tokens: 9 us and 4.3 for the merge (2.7), a chain of waits: list, pages, sums.
+// Bound by memory: 64 groups of 4 beams, prompts of 8192 to 32768 tokens, 32 query heads on 8: 5.7 GB of pages in 922 us, 6.2 TB/s (a plain read 836 us); 8 groups of 8 samples, 2048 tokens and up to 8192
+// of their own: 175 us (162), and up to 220 within the first ten milliseconds after the GPU was idle.  A short search, 4 beams of 4096 tokens: 9 us and 4 for the merge (2.7), a chain of waits: list, pages, sums.
 // Rows beyond 32 are other workgroups', which read the pages again, mostly from their XCD's L2: 4 groups of 32 samples 118 us (one workgroup for all rows that share a KV head, the tiles in LDS: 162), 8 groups of
-// 32 beams of 4096 tokens 67 (61), of 64 query heads 112 (105); the blocks one after the other in a workgroup 139, 252 and 222.
+// 32 beams of 2048 to 4096 tokens 67 (61), of 64 query heads 111 (105); the blocks one after the other in a workgroup 139, 252 and 222.
 // K past the caches 1003 us for the 965 of then; one buffer for V and three workgroups on a CU: as long; eight waves on one workgroup's pages 908 for 926, but 180 for 175 and 28 for 24 on 64 groups of 500 tokens.
 template <int NB>
 __device__ __forceinline__ void beam_rows(const BeamAttnArgs& a, const BeamSpan& s, BeamAttnLds<NB>& lds, int row0) {

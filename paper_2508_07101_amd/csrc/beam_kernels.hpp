@@ -167,9 +167,11 @@ struct Best {
 // A weight is 2^((x - ref) log2 e): the difference first, so that rows that differ by a constant have the same sums, whatever the constant.  A lane's ref is a logit of its own
 // that follows the largest when that is 8 above it.  So an exponent is 12 above 0 at most, and below 0 by as much as the row's entropy in bits and one or two more in the weighted mean: its three
 // roundings (difference, product, constant) move the sum by less than 2^-17 of itself, or 2^-16.5 with 2^31 tokens.
-// Bound by its instructions, four waves to a SIMD: 512 rows of 131072 bf16 logits, 134 MB: 30 us, 4.5 TB/s (a plain read 19.6 us), vector instructions under way for 79 % of the CUs' busy time; without the
-// search for the best 25 us.  The list sorted after each step instead of a running bound 32 us; the next step's logits asked for before this one's search 39, for the registers; by four loads 36; a bound from
-// maxima over groups of lanes instead of the sort as long, and with nine logits in ten masked 26 us for 17, for the keys that it lets through; weights by one multiply-add as long.
+// 512 rows of 131072 logits, 134 MB: bf16 30 to 33 us, 4.1 to 4.5 TB/s (a plain read 19.6 us), fp16 1 us more; 256 rows in fp32 29; with one bf16 row in 20 ended, which is not read, 29.  A wave asks for a step's logits, waits and
+// computes in turn, four waves to a SIMD: vector instructions are under way for 79 % of the CUs' busy time, and waves wait for 46 % of theirs.  Which of the two it is bound by is open: without the search for
+// the best those 29 are 25; weights by one multiply-add, an instruction less for each logit, take as long; the next step's logits asked for ahead into registers cost a wave to a SIMD (39 us; by four
+// loads 36), and past the registers they have not been tried.  The list sorted after each step instead of a running bound 2 us longer; a bound from maxima over groups of lanes instead of the sort as long, and
+// with nine logits in ten masked 26 us for 17, for the keys that it lets through.
 template <int DTYPE, int R>
 __global__ __launch_bounds__(64 * BEAM_WAVES) void beam_rows_kernel(BeamArgs a) {
     typedef Logits<DTYPE> X;
@@ -365,7 +367,7 @@ __device__ __forceinline__ Candidate merge_candidates(Candidate c, const Candida
 
 // A workgroup for a group, a wave for each of its rows at a time: the parts' sums and lists together, the tokens' worth in 64 bits.  Of the parts' q-th best, the m-th largest
 // bounds the row's best m q from below.  With m near half of the parts and m q >= n few of the lists' keys are left.  Then the rows' lists are merged, two at a time.
-// Bound by its chain of sorts and of code that runs once, a copy of which is fetched first: 64 groups of 8 rows for 8 places 6 us, 8 groups of 32 rows for 64 places 25 (each candidate counting those in
+// Bound by its chain of sorts and of code that runs once, a copy of which is fetched first: 64 groups of 8 rows for 8 places 6 us, 8 groups of 32 rows for 64 places 24 (each candidate counting those in
 // front of it: 145).  4 rows of 32000 logits: 6 us here and 6 in beam_rows_kernel, of which a launch and the way to memory and back are most.
 constexpr int MERGE_WAVES = 16;
 __global__ __launch_bounds__(64 * MERGE_WAVES) void beam_merge_kernel(BeamArgs a) {
@@ -664,7 +666,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void fork_tables_kernel(ForkArgs a) {
     if (tid == 0) a.counts[chunk] = total;
 }
 
-// The pages that go back, in order: a thread for each, which looks up its list among 1024.  4 to 6 us, a launch's own time and two ways to memory.
+// The pages that go back, in order: a thread for each, which looks up its list among 1024.  4 to 6.5 us, a launch's own time and two ways to memory.
 __global__ __launch_bounds__(PLAN_THREADS) void fork_pages_kernel(ForkArgs a) {
     __shared__ int64_t scratch[2][2][PLAN_THREADS / 64];
     __shared__ int32_t start[PLAN_THREADS];
@@ -705,8 +707,9 @@ struct CopyArgs {
 };
 static_assert(sizeof(CopyArgs) <= 4096, "a launch's arguments");
 
-// A workgroup for a copy in a layer: 16 lanes a row of 256 bytes, eight rows of theirs under way.  Bound by memory: 256 pages of 1 to 15 tokens, a quarter of them none, 8 KV heads, 32 layers, 403 MB read and
-// written: 103.5 us, 3.9 TB/s (a plain copy of a large tensor 5.08).  Four rows under way 109 us, sixteen 138; stores that the caches keep 106.  Four pages of 36 layers: 5.6 us, a launch's own time.
+// A workgroup for a copy in a layer: 16 lanes a row of 256 bytes, eight rows of theirs under way.  Bound by memory: 256 pages of 1 to 15 tokens, a quarter of them none, 8 KV heads, 32 layers, 441 MB read and
+// written: 98 and 109 us for two caches in turn, 4.3 TB/s (a plain copy of a large tensor 5.08); stores that the caches keep 109 on average for these 103.7.  One cache again and again, of whose pages the last-level
+// cache then still has some: 78 us, with stores that the caches keep 109; four rows under way 80 us, sixteen 98.  Four pages of 36 layers: 5 us, a launch's own time.
 __global__ __launch_bounds__(COPY_THREADS) void kv_copy_kernel(CopyArgs a) {
     const CopyLayer& l = a.layer[blockIdx.y];
     const i32x4 copy = *reinterpret_cast<const i32x4*>(a.copies + (int64_t)blockIdx.x * 4);

@@ -11,7 +11,7 @@ constexpr int BEAM_ROWS = 32;           // rows (row of the group, query head) o
 constexpr int BEAM_CUS = 256;
 constexpr int BEAM_LIST = 8192;         // pages of a piece: a bit each in LDS
 constexpr int BEAM_MAX_SPLITS = 64;     // pieces of a group's pages: one lane each in the merge
-constexpr int BEAM_MIN_PIECE = 128;     // tokens: a tile for each wave (4 beams of 4096 tokens 7.8 us, by 256 8.8; 8 of 2000 9.9 and 11.6; longer ones alike)
+constexpr int BEAM_MIN_PIECE = 128;     // tokens: a tile for each wave (4 beams of 4096 tokens 8.7 us, by 256 9.5; 8 of 2000 10.4 and 11.8; longer ones alike)
 constexpr int BEAM_PIECE_COST = 16;     // tiles of 32 tokens that a piece costs besides its own
 inline bool beam_pages_served(int64_t pages) { return pages <= (int64_t)BEAM_LIST * BEAM_MAX_SPLITS; }
 
