@@ -19,7 +19,7 @@ class BeamRunner:
     ``layer`` for each layer in order.  ``parents`` and ``tokens`` are what ``select`` chose, for the caller's own account; ``scores`` and ``ended`` belong to the rows as they are now.
     Everything is enqueued on the current stream; nothing here waits for the GPU.  A row that has ended keeps its tokens and gets no new one (its slot is -1).
     A group that found no page keeps its rows (``granted`` is 0).  With ``hold`` it keeps all that belongs to them: ``fork`` puts its scores and ends back, its ``parents`` are
-    the rows themselves and its ``tokens`` -1, so that the same logits make the same choice in a later step, which finds pages or waits again; a caller's account that follows
+    the rows themselves and its ``tokens`` -1, so that the same logits make the same choice in a later step, which finds pages or waits again (for ever with rows of ``16 * max_pages`` tokens); a caller's account that follows
     ``parents`` and ``tokens`` is right either way, and a captured step needs no host in between.  That is what a pool that may run out wants.  Without it ``scores``, ``ended``,
     ``parents`` and ``tokens`` of such a group are the chosen ones', which its rows do not have: it can be finished, but a further step would go on from scores of other rows.
     ``finish`` gives the pages of whole groups back.
